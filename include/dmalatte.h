@@ -519,6 +519,147 @@ int dl_token_dispatch(const void *const *in, void *const *out, int W, const uint
 int dl_token_dispatch_device(const void *const *in, void *const *out, int W, const uint32_t *tokens, size_t row_bytes,
                              const uint8_t *dest_device, void *stream);
 
+/* ------------------------------------------- a paged cache in 8 bits, and decoding with drafts */
+
+/*
+ * The operations above move the blocks of a paged cache of keys and values; the ones below fill such blocks, read them
+ * and decide which of a step's drafted tokens stay.  They compute, so they differ from the copies in this:
+ *  - every buffer, the tables, lengths, slots and random numbers included, is device memory of the caller; only the
+ *    structs that name them are host memory, and are consumed before the call returns;
+ *  - they always execute as in DL_MODE_ONESHOT, on `stream` (other modes have no effect on them), allocate nothing, use no
+ *    memory of the library's, and may be captured into a HIP graph.  Lengths and tables are read when the kernels run, so a
+ *    captured step can be replayed as they grow;
+ *  - results do not depend on the order in which workgroups run: the same inputs give the same bits;
+ *  - addresses need the alignment of one element (codes: none).
+ */
+typedef enum dl_type { DL_TYPE_F32 = 0, DL_TYPE_BF16 = 1, DL_TYPE_F16 = 2 } dl_type;
+
+/*
+ * Codes of a cache.  A row is the head_dim elements x of one token in one head of the cache, and is held as head_dim codes
+ * with one 32-bit scale.  With LIMIT = 448 (DL_KV_FP8: e4m3 without infinities) or 127 (DL_KV_INT8), in 32-bit arithmetic,
+ *   a = max(largest |x|, 2^-100),  scale = a * (1 / LIMIT),  code = x * ((1 / a) * LIMIT) rounded to nearest, ties to even,
+ * each operation rounded once,
+ * and the row stands for code * scale.  A row that holds an infinity or a NaN gets codes of zero and a scale of NaN.
+ */
+typedef enum dl_kv_format { DL_KV_FP8 = 0, DL_KV_INT8 = 1 } dl_kv_format;
+
+/*
+ * A paged cache: token t of a sequence lies in page table[t / page_tokens], at place t % page_tokens, and slot s is
+ * place s % page_tokens of page s / page_tokens.  Code d of a row lies at
+ *   base + page * page_stride + place * token_stride + head * head_stride + d     (strides in bytes)
+ * and its scale at the same place of the scale array with the scale strides (in floats), for keys and values alike.  So
+ * pages may be separate arrays of codes and of scales, or blocks that hold all four and are moved as one.
+ */
+typedef struct dl_kv_cache {
+    void *k, *v;              /* codes */
+    float *k_scale, *v_scale;
+    int32_t format;           /* dl_kv_format */
+    int32_t heads;            /* 1 .. 65535 */
+    int32_t head_dim;         /* a multiple of 16, 16 .. 256 */
+    int32_t page_tokens;      /* 1 .. 65536 */
+    int64_t pages;            /* in the pool, < 2^31 */
+    int64_t page_stride, token_stride, head_stride;
+    int64_t scale_page_stride, scale_token_stride, scale_head_stride;
+} dl_kv_cache;
+
+/*
+ * `tokens` rows per head of keys and of values outside the cache: element d of token t in head h at
+ * k[t * k_token_stride + h * k_head_stride + d] (strides in elements), likewise v.  k or v may be null: that side of the cache
+ * is left alone, and may be null itself.  Token t belongs to slot slots[t].
+ */
+typedef struct dl_kv_rows {
+    void *k, *v;
+    const int64_t *slots;
+    int64_t tokens;           /* < 2^31 */
+    int32_t type;             /* dl_type of k and v */
+    int32_t reserved;         /* 0 */
+    int64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+} dl_kv_rows;
+
+/*
+ * Quantise rows into the cache / read them back.  A slot that is negative or behind the last page is no slot: that token is not
+ * written, or reads back as zeros.  Two tokens with one slot in a call of dl_kv_write leave either row there.
+ * tokens == 0: DL_OK, no work.
+ */
+int dl_kv_write(const dl_kv_cache *cache, const dl_kv_rows *rows, void *stream);
+int dl_kv_read(const dl_kv_cache *cache, const dl_kv_rows *rows, void *stream);
+
+/*
+ * Attention of a batch of sequences that share a prefix, over a paged cache.  Sequence b has q_lens[b] queries (null: all have
+ * q_tokens), which are the last of its lens[b] own tokens; those follow the prefix_tokens tokens of the prefix.  Query j in head h
+ * attends, in head h / (q_heads / cache heads) of the cache, to the whole prefix and to own token i if
+ * i <= lens[b] - q_lens[b] + j (lens[b] counts the queries' own tokens, which have been written before):
+ *   s_i = scale * <q, k_i>,   out = sum of e^(s_i) v_i / sum of e^(s_i),   lse = ln sum of e^(s_i).
+ * The prefix is read once for all sequences.  Scores, sums and outputs are 32-bit until out is rounded to its type; the
+ * weights e^(s_i) enter the product with v in the type of q.
+ * A query with nothing to attend to, and those from q_lens[b] on, get out = 0 and lse = -infinity.  lens[b] counts as at least 0 and
+ * at most max_pages * page_tokens, q_lens[b] as 0 .. q_tokens.  A token whose page in the table is no page of the pool is not
+ * attended to.  Codes are those that dl_kv_write writes (fp8: no NaN codes); what lies behind the lengths may hold anything.
+ */
+typedef struct dl_prefix_attention_args {
+    const void *q;                /* [batch][q_tokens][q_heads][head_dim], strides in elements, head_dim contiguous */
+    void *out;                    /* the same, with strides of its own */
+    float *lse;                   /* [batch][q_tokens][q_heads], contiguous; or null */
+    const int32_t *prefix_pages;  /* pages of the prefix */
+    const int32_t *pages;         /* [batch][max_pages], pages_stride apart: pages of each sequence's own tokens */
+    const int32_t *lens;          /* [batch] */
+    const int32_t *q_lens;        /* [batch], or null */
+    void *workspace;              /* dl_prefix_attention_workspace() bytes, 16-byte aligned */
+    size_t workspace_bytes;
+    int64_t prefix_tokens;        /* 0 .. 2^30 */
+    int64_t max_pages;            /* max_pages * page_tokens <= 2^30 */
+    int64_t pages_stride;
+    int64_t q_seq_stride, q_token_stride, q_head_stride;
+    int64_t out_seq_stride, out_token_stride, out_head_stride;
+    int32_t type;                 /* of q and out: DL_TYPE_BF16 or DL_TYPE_F16 */
+    int32_t batch, q_tokens;      /* batch * q_tokens * q_heads < 2^31 */
+    int32_t q_heads;              /* a multiple of the cache's heads */
+    float scale;                  /* what the scores are multiplied with */
+    int32_t reserved;             /* 0 */
+} dl_prefix_attention_args;
+
+/* Bytes of workspace a call of these sizes needs (pointers, lens and strides play no part); negative: a dl_status.  Before its
+ * first use a workspace is filled with zeros; calls leave it fit for the next one, of any operator and size.  Calls that may
+ * run at the same time need workspaces of their own. */
+int64_t dl_prefix_attention_workspace(const dl_kv_cache *cache, const dl_prefix_attention_args *args);
+int dl_prefix_attention(const dl_kv_cache *cache, const dl_prefix_attention_args *args, void *stream);
+
+/*
+ * Verification of drafted tokens (speculative decoding) from given random numbers.  Sequence b has draft_lens[b] drafts x_i
+ * (null: all have `drafts`).  target[b][i] holds the target's probabilities of the token at draft i, target[b][draft_lens[b]] those of
+ * the token behind the last one; draft[b][i] those that x_i was drawn from.  With uniform numbers u in [0, 1),
+ *   draft x_i is accepted if u_i * draft_i(x_i) < target_i(x_i), up to the first that is not.
+ * One more token follows the a accepted ones: with w = max(target_a - draft_a, 0) after a refusal, w = target_a if all were
+ * accepted, it is the v whose w_v / race_v is largest (the lowest such v), over the v with w_v > 0.  Where race holds
+ * exponential variates of rate 1, v is drawn with a probability proportional to w_v; and as nothing is summed, the outcome
+ * does not depend on an order of summation.  Products, differences and quotients are 32-bit, each rounded once.
+ * draft == null: the drafts were not drawn; draft_i is 1 at x_i and 0 elsewhere.
+ * If no w_v is positive, target_a takes its place; if that has no positive value either, the token is -1.  NaN counts as not
+ * positive, and a draft that is no token of the vocabulary is refused (w = target_a then, if draft == null).
+ * tokens[b] becomes the accepted drafts, the token behind them, and -1 up to drafts + 1 entries; accepted[b] becomes a.
+ */
+#define DL_MAX_DRAFTS 63
+typedef struct dl_verify_draft_args {
+    const void *target;           /* [batch][drafts + 1][vocab], strides in elements, vocab contiguous */
+    const void *draft;            /* [batch][drafts][vocab], strides in elements, vocab contiguous; or null */
+    const int32_t *draft_tokens;  /* [batch][drafts], contiguous, like uniform and tokens */
+    const float *uniform;         /* [batch][drafts] */
+    const float *race;            /* [batch][vocab], race_stride apart; > 0 */
+    const int32_t *draft_lens;    /* [batch], or null; counts as 0 .. drafts */
+    int32_t *tokens;              /* [batch][drafts + 1] */
+    int32_t *accepted;            /* [batch] */
+    void *workspace;              /* dl_verify_draft_workspace() bytes, 16-byte aligned; see dl_prefix_attention_workspace */
+    size_t workspace_bytes;
+    int64_t target_seq_stride, target_row_stride, draft_seq_stride, draft_row_stride, race_stride;
+    int32_t type;                 /* dl_type of target and draft */
+    int32_t batch;                /* 0 .. 2^20 */
+    int32_t drafts;               /* 0 .. DL_MAX_DRAFTS */
+    int32_t vocab;                /* 1 .. 2^30 */
+} dl_verify_draft_args;
+
+int64_t dl_verify_draft_workspace(const dl_verify_draft_args *args);
+int dl_verify_draft(const dl_verify_draft_args *args, void *stream);
+
 /*
  * Host-only: lower a collective to the list of copies the device executes
  * (the analogue of building the command list, paper Sec. III-B2 "control").

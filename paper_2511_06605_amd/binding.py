@@ -38,6 +38,9 @@ DL_MODE_SIGNAL = 2
 DL_MODE_STANDBY = 3
 DL_MODE_AUTO = 4
 DL_OP_BATCH, DL_OP_BROADCAST, DL_OP_ALLGATHER, DL_OP_ALLTOALL, DL_OP_SWAP, DL_OP_TOKEN_DISPATCH = range(6)
+DL_TYPE_F32, DL_TYPE_BF16, DL_TYPE_F16 = range(3)
+DL_KV_FP8, DL_KV_INT8 = range(2)
+DL_MAX_DRAFTS = 63
 DL_AUTO_STANDBY_TILES = 64
 DL_AUTO_SIGNAL_MAX_BYTES = 288 << 20
 DL_AUTO_PRELAUNCH_MAX_BYTES = 288 << 20
@@ -54,6 +57,8 @@ EXPORTS = [
     "dl_plan_batch_inferred", "dl_set_trace", "dl_get_trace", "dl_trace_clock",
     "dl_last_device_error", "dl_debug_lose_next_table", "dl_batch_copy_static",
     "dl_plan_mode", "dl_last_mode", "dl_complete", "dl_parse_config", "dl_token_dispatch_device",
+    "dl_kv_write", "dl_kv_read", "dl_prefix_attention", "dl_prefix_attention_workspace", "dl_verify_draft",
+    "dl_verify_draft_workspace",
 ]
 
 
@@ -102,6 +107,53 @@ class PlanItem(ctypes.Structure):
         ("k", ctypes.c_uint32),
         ("reserved", ctypes.c_uint32),
         ("dst", ctypes.c_void_p * DL_PLAN_FANOUT),
+    ]
+
+
+class KvCacheDesc(ctypes.Structure):
+    """dl_kv_cache"""
+    _fields_ = [
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+        ("format", ctypes.c_int32), ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page_tokens", ctypes.c_int32),
+        ("pages", ctypes.c_int64),
+        ("page_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+        ("scale_page_stride", ctypes.c_int64), ("scale_token_stride", ctypes.c_int64), ("scale_head_stride", ctypes.c_int64),
+    ]
+
+
+class KvRowsDesc(ctypes.Structure):
+    """dl_kv_rows"""
+    _fields_ = [
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("slots", ctypes.c_void_p), ("tokens", ctypes.c_int64),
+        ("type", ctypes.c_int32), ("reserved", ctypes.c_int32),
+        ("k_token_stride", ctypes.c_int64), ("k_head_stride", ctypes.c_int64),
+        ("v_token_stride", ctypes.c_int64), ("v_head_stride", ctypes.c_int64),
+    ]
+
+
+class PrefixAttentionDesc(ctypes.Structure):
+    """dl_prefix_attention_args"""
+    _fields_ = [
+        ("q", ctypes.c_void_p), ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p), ("prefix_pages", ctypes.c_void_p),
+        ("pages", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("q_lens", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+        ("prefix_tokens", ctypes.c_int64), ("max_pages", ctypes.c_int64), ("pages_stride", ctypes.c_int64),
+        ("q_seq_stride", ctypes.c_int64), ("q_token_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64),
+        ("out_seq_stride", ctypes.c_int64), ("out_token_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64),
+        ("type", ctypes.c_int32), ("batch", ctypes.c_int32), ("q_tokens", ctypes.c_int32), ("q_heads", ctypes.c_int32),
+        ("scale", ctypes.c_float), ("reserved", ctypes.c_int32),
+    ]
+
+
+class VerifyDraftDesc(ctypes.Structure):
+    """dl_verify_draft_args"""
+    _fields_ = [
+        ("target", ctypes.c_void_p), ("draft", ctypes.c_void_p), ("draft_tokens", ctypes.c_void_p), ("uniform", ctypes.c_void_p),
+        ("race", ctypes.c_void_p), ("draft_lens", ctypes.c_void_p), ("tokens", ctypes.c_void_p), ("accepted", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+        ("target_seq_stride", ctypes.c_int64), ("target_row_stride", ctypes.c_int64),
+        ("draft_seq_stride", ctypes.c_int64), ("draft_row_stride", ctypes.c_int64), ("race_stride", ctypes.c_int64),
+        ("type", ctypes.c_int32), ("batch", ctypes.c_int32), ("drafts", ctypes.c_int32), ("vocab", ctypes.c_int32),
     ]
 
 
@@ -182,6 +234,12 @@ def lib() -> ctypes.CDLL:
                                                    ctypes.POINTER(PlanItem), ctypes.c_size_t]),
         "dl_plan_batch_inferred": (ctypes.c_long, [ctypes.POINTER(CopyDesc), ctypes.c_size_t, ctypes.POINTER(PlanItem),
                                                    ctypes.c_size_t]),
+        "dl_kv_write": (ctypes.c_int, [vp, vp, vp]),
+        "dl_kv_read": (ctypes.c_int, [vp, vp, vp]),
+        "dl_prefix_attention": (ctypes.c_int, [vp, vp, vp]),
+        "dl_prefix_attention_workspace": (ctypes.c_int64, [vp, vp]),
+        "dl_verify_draft": (ctypes.c_int, [vp, vp]),
+        "dl_verify_draft_workspace": (ctypes.c_int64, [vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -400,6 +458,192 @@ def dl_token_dispatch(ins, outs, tokens, row_bytes: int, dest, stream=None) -> N
 def dl_token_dispatch_device(ins, outs, tokens, row_bytes: int, dest_device, stream=None) -> None:
     """dest_device: device buffer of (total tokens) x W bytes, non-zero where a token goes to a rank."""
     _check(_native().token_dispatch_device(ins, outs, tokens, row_bytes, dest_device, stream), "dl_token_dispatch_device")
+
+
+# ------------------------------------------- a paged cache in 8 bits, and decoding with drafts
+#
+# The descriptors below take tensors (anything with data_ptr(), shape, stride() and dtype, as torch's) and hold on to them.
+# They name buffers, not contents: a program makes them once for the buffers it keeps and calls with them step after step.
+
+_TYPES = {"float32": DL_TYPE_F32, "bfloat16": DL_TYPE_BF16, "float16": DL_TYPE_F16}
+_FORMATS = {"float8_e4m3fn": DL_KV_FP8, "int8": DL_KV_INT8}
+
+
+def _dtype(t) -> str:
+    return str(t.dtype).rpartition(".")[2]
+
+
+def _expect(t, what, dtype, shape, packed=False):
+    """A tensor's address, once it is what it has to be; None in the shape: any size."""
+    if _dtype(t) not in (dtype if isinstance(dtype, (tuple, list, dict)) else (dtype,)):
+        raise ValueError(f"{what}: type {t.dtype}, expected {dtype if isinstance(dtype, str) else ' or '.join(dtype)}")
+    if len(t.shape) != len(shape) or any(w is not None and int(w) != int(n) for n, w in zip(t.shape, shape)):
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {tuple('any' if w is None else int(w) for w in shape)}")
+    if t.numel() and (getattr(t, "is_cuda", True) is False):
+        raise ValueError(f"{what}: not in device memory")
+    if packed and not t.is_contiguous():
+        raise ValueError(f"{what}: must be contiguous")
+    if not packed and t.shape[-1] > 1 and t.stride()[-1] != 1:
+        raise ValueError(f"{what}: its last dimension must be contiguous")
+    return _addr(t)
+
+
+class _Request:
+    """A descriptor of the C boundary, the tensors it names, and its address for the calls."""
+
+    def _hold(self, desc, *tensors):
+        self.desc = desc
+        self._tensors = tensors
+        self.at = ctypes.addressof(desc)
+
+    def use_workspace(self, workspace) -> None:
+        """Device memory of at least the size the *_workspace function gives, filled with zeros before its first use."""
+        if getattr(workspace, "is_cuda", True) is False or not workspace.is_contiguous():
+            raise ValueError("workspace: contiguous device memory")
+        self._workspace = workspace
+        self.desc.workspace = _addr(workspace)
+        self.desc.workspace_bytes = workspace.numel() * workspace.element_size()
+
+
+class KvCache(_Request):
+    """A paged cache (dl_kv_cache): codes of keys and values as [pages, page_tokens, heads, head_dim] tensors of float8_e4m3fn or
+    int8, scales as [pages, page_tokens, heads] tensors of float32; any strides, the same for keys and values."""
+
+    def __init__(self, k, v, k_scale, v_scale):
+        shape = tuple(int(n) for n in k.shape)
+        if len(shape) != 4:
+            raise ValueError("codes have four dimensions: pages, page_tokens, heads, head_dim")
+        d = KvCacheDesc(k=_expect(k, "k", _FORMATS, shape), v=_expect(v, "v", _dtype(k), shape), format=_FORMATS[_dtype(k)], heads=shape[2],
+                        head_dim=shape[3], page_tokens=shape[1], pages=shape[0])
+        for name, s in (("k_scale", k_scale), ("v_scale", v_scale)):
+            if _dtype(s) != "float32" or tuple(s.shape) != shape[:3] or getattr(s, "is_cuda", True) is False:
+                raise ValueError(f"{name}: float32 of shape {shape[:3]} in device memory")
+            setattr(d, name, _addr(s))
+        if tuple(k.stride()) != tuple(v.stride()) or tuple(k_scale.stride()) != tuple(v_scale.stride()):
+            raise ValueError("keys and values have different strides")
+        d.page_stride, d.token_stride, d.head_stride = k.stride()[:3]
+        d.scale_page_stride, d.scale_token_stride, d.scale_head_stride = k_scale.stride()
+        self._hold(d, k, v, k_scale, v_scale)
+
+
+class KvRows(_Request):
+    """Rows outside a cache and the slots they belong to (dl_kv_rows): k and v [tokens, heads, head_dim] of float32, bfloat16 or
+    float16, either may be None; slots [tokens] of int64."""
+
+    def __init__(self, k, v, slots):
+        some = k if k is not None else v
+        if some is None:
+            raise ValueError("neither keys nor values")
+        shape = tuple(int(n) for n in some.shape)
+        if len(shape) != 3:
+            raise ValueError("rows have three dimensions: tokens, heads, head_dim")
+        d = KvRowsDesc(slots=_expect(slots, "slots", "int64", shape[:1], packed=True), tokens=shape[0], type=_TYPES.get(_dtype(some), -1))
+        for name, t in (("k", k), ("v", v)):
+            if t is not None:
+                setattr(d, name, _expect(t, name, _TYPES if t is some else _dtype(some), shape))
+                setattr(d, name + "_token_stride", t.stride()[0])
+                setattr(d, name + "_head_stride", t.stride()[1])
+        self.shape = shape
+        self._hold(d, k, v, slots)
+
+
+class PrefixAttention(_Request):
+    """A call of dl_prefix_attention: q and out [batch, q_tokens, q_heads, head_dim] of bfloat16 or float16, pages [batch, max_pages], lens and
+    q_lens [batch] and prefix_pages [n] of int32, lse [batch, q_tokens, q_heads] of float32.  scale: 1 / sqrt(head_dim) if None."""
+
+    def __init__(self, cache, q, out, pages, lens, prefix_pages=None, prefix_tokens=0, q_lens=None, lse=None, scale=None):
+        shape = tuple(int(n) for n in q.shape)
+        if len(shape) != 4:
+            raise ValueError("q has four dimensions: batch, q_tokens, q_heads, head_dim")
+        B, M, H, D = shape
+        if D != cache.desc.head_dim:
+            raise ValueError(f"q: head_dim {D}, the cache has {cache.desc.head_dim}")
+        prefix_tokens = int(prefix_tokens)
+        have = 0 if prefix_pages is None else int(prefix_pages.shape[0]) * cache.desc.page_tokens
+        if prefix_tokens > have:
+            raise ValueError(f"prefix_tokens {prefix_tokens}, but prefix_pages hold {have}")
+        d = PrefixAttentionDesc(
+            q=_expect(q, "q", ("bfloat16", "float16"), shape), out=_expect(out, "out", _dtype(q), shape), type=_TYPES[_dtype(q)],
+            pages=_expect(pages, "pages", "int32", (B, None)), lens=_expect(lens, "lens", "int32", (B,), packed=True),
+            prefix_tokens=prefix_tokens, max_pages=int(pages.shape[1]), pages_stride=pages.stride()[0], batch=B, q_tokens=M, q_heads=H,
+            scale=D ** -0.5 if scale is None else float(scale))
+        if prefix_pages is not None:
+            d.prefix_pages = _expect(prefix_pages, "prefix_pages", "int32", (None,), packed=True)
+        if q_lens is not None:
+            d.q_lens = _expect(q_lens, "q_lens", "int32", (B,), packed=True)
+        if lse is not None:
+            d.lse = _expect(lse, "lse", "float32", (B, M, H), packed=True)
+        d.q_seq_stride, d.q_token_stride, d.q_head_stride = q.stride()[:3]
+        d.out_seq_stride, d.out_token_stride, d.out_head_stride = out.stride()[:3]
+        self.cache = cache
+        self._hold(d, q, out, pages, lens, prefix_pages, q_lens, lse)
+
+
+class DraftVerify(_Request):
+    """A call of dl_verify_draft: target [batch, drafts + 1, vocab] and draft_probs [batch, drafts, vocab] of float32, bfloat16 or float16,
+    draft_tokens [batch, drafts], draft_lens [batch], tokens [batch, drafts + 1] and accepted [batch] of int32, uniform [batch, drafts] and
+    race [batch, vocab] of float32."""
+
+    def __init__(self, target, draft_tokens, uniform, race, tokens, accepted, draft_probs=None, draft_lens=None):
+        shape = tuple(int(n) for n in target.shape)
+        if len(shape) != 3 or shape[1] < 1:
+            raise ValueError("target has three dimensions: batch, drafts + 1, vocab")
+        B, n, V = shape[0], shape[1] - 1, shape[2]
+        d = VerifyDraftDesc(
+            target=_expect(target, "target", _TYPES, shape), type=_TYPES[_dtype(target)], batch=B, drafts=n, vocab=V,
+            draft_tokens=_expect(draft_tokens, "draft_tokens", "int32", (B, n), packed=True),
+            uniform=_expect(uniform, "uniform", "float32", (B, n), packed=True), race=_expect(race, "race", "float32", (B, V)),
+            tokens=_expect(tokens, "tokens", "int32", (B, n + 1), packed=True), accepted=_expect(accepted, "accepted", "int32", (B,), packed=True))
+        if draft_probs is not None:
+            d.draft = _expect(draft_probs, "draft_probs", _dtype(target), (B, n, V))
+            d.draft_seq_stride, d.draft_row_stride = draft_probs.stride()[:2]
+        if draft_lens is not None:
+            d.draft_lens = _expect(draft_lens, "draft_lens", "int32", (B,), packed=True)
+        d.target_seq_stride, d.target_row_stride = target.stride()[:2]
+        d.race_stride = race.stride()[0]
+        self._hold(d, target, draft_tokens, uniform, race, tokens, accepted, draft_probs, draft_lens)
+
+
+def _rows_fit(cache, rows):
+    c = cache.desc
+    if rows.shape[1:] != (c.heads, c.head_dim):
+        raise ValueError(f"rows of {rows.shape[1]} heads and {rows.shape[2]} elements, the cache has {c.heads} and {c.head_dim}")
+
+
+def dl_kv_write(cache: KvCache, rows: KvRows, stream=None) -> None:
+    """Quantise rows into their slots of the cache."""
+    _rows_fit(cache, rows)
+    _check(lib().dl_kv_write(cache.at, rows.at, _stream(stream)), "dl_kv_write")
+
+
+def dl_kv_read(cache: KvCache, rows: KvRows, stream=None) -> None:
+    """What the slots of the cache hold, into rows."""
+    _rows_fit(cache, rows)
+    _check(lib().dl_kv_read(cache.at, rows.at, _stream(stream)), "dl_kv_read")
+
+
+def _size(n: int, what: str) -> int:
+    if n < 0:
+        raise DlError(int(n), what)
+    return int(n)
+
+
+def dl_prefix_attention_workspace(request: PrefixAttention) -> int:
+    """Bytes of workspace a call needs."""
+    return _size(lib().dl_prefix_attention_workspace(request.cache.at, request.at), "dl_prefix_attention_workspace")
+
+
+def dl_prefix_attention(request: PrefixAttention, stream=None) -> None:
+    _check(lib().dl_prefix_attention(request.cache.at, request.at, _stream(stream)), "dl_prefix_attention")
+
+
+def dl_verify_draft_workspace(request: DraftVerify) -> int:
+    """Bytes of workspace a call needs."""
+    return _size(lib().dl_verify_draft_workspace(request.at), "dl_verify_draft_workspace")
+
+
+def dl_verify_draft(request: DraftVerify, stream=None) -> None:
+    _check(lib().dl_verify_draft(request.at, _stream(stream)), "dl_verify_draft")
 
 
 # -------------------------------------------------------------------- prelaunch

@@ -1,0 +1,252 @@
+// Quantising a cache as it is written, and reading it back (dl_kv_write, dl_kv_read).
+//
+// A row (the head_dim elements of one token and head) becomes codes x * ((1 / a) * LIMIT), a = max(max |x|, 2^-100), and a scale
+// a * (1 / LIMIT).  The largest magnitude is needed before the first code, so a row is held in registers from its load to
+// its store: 16 elements a lane, as many lanes as that takes (the next power of two) side by side, and the maximum by
+// swaps among them.  One pass over the data either way; memory is what bounds it.
+#include "dl_codes.h"
+#include "dl_internal.h"
+
+namespace {
+
+struct kv_args {
+    dl_cache_view c;
+    char *k, *v;  // rows outside the cache
+    const int64_t *slots;
+    int64_t k_token, k_head, v_token, v_head;  // strides in bytes
+    int64_t slots_end;                         // pages * page_tokens
+    uint32_t rows;                             // tokens * heads
+    uint32_t tokens;
+    dl_divider heads;
+    int32_t shift;  // log2 of the tokens of a page, or -1
+};
+
+// 16 elements of a row as floats
+template <class T>
+__device__ __forceinline__ void load16(const char *p, float (&x)[16])
+{
+    if constexpr (T::size == 4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const dl_f32x4 w = dl_load_at<dl_f32x4>(p + 16 * i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[4 * i + j] = w[j];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const dl_u32x4 w = dl_load_at<dl_u32x4>(p + 16 * i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[8 * i + 2 * j] = T::lo(w[j]), x[8 * i + 2 * j + 1] = T::hi(w[j]);
+        }
+    }
+}
+
+template <class T>
+__device__ __forceinline__ void store16(char *p, const float (&x)[16])
+{
+    if constexpr (T::size == 4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) dl_store_at(p + 16 * i, dl_f32x4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]});
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            dl_u32x4 w;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = T::pack(x[8 * i + 2 * j], x[8 * i + 2 * j + 1]);
+            dl_store_at(p + 16 * i, w);
+        }
+    }
+}
+
+// Where a row of a slot lies: false if the slot is none.
+__device__ __forceinline__ bool place(const kv_args &a, int64_t slot, uint32_t head, int64_t *codes, int64_t *scale)
+{
+    if (slot < 0 || slot >= a.slots_end) return false;
+    int64_t page, in;
+    if (a.shift >= 0) {
+        page = slot >> a.shift;
+        in = slot & (a.c.page.d - 1u);
+    } else {
+        page = slot / a.c.page.d;
+        in = slot - page * a.c.page.d;
+    }
+    *codes = page * a.c.page_stride + in * a.c.token_stride + head * a.c.head_stride;
+    *scale = page * a.c.scale_page_stride + in * a.c.scale_token_stride + head * a.c.scale_head_stride;
+    return true;
+}
+
+constexpr uint32_t KV_THREADS = 256;
+
+// blockIdx.y: 0 keys, 1 values (a launch for one side alone has one of them).  LANES a row.
+template <class T, class C, int LANES>
+__global__ void __launch_bounds__(KV_THREADS) dl_kv_write_kernel(const kv_args a)
+{
+    const bool values = blockIdx.y != 0 || !a.k;
+    const uint32_t lane = threadIdx.x % LANES;
+    const uint32_t row = (uint32_t)(((uint64_t)blockIdx.x * KV_THREADS + threadIdx.x) / LANES);
+    if (row >= a.rows) return;  // all lanes of a row together
+    const uint32_t token = dl_divide(row, a.heads), head = row - token * a.heads.d;
+    const char *const from = values ? a.v + token * a.v_token + head * a.v_head : a.k + token * a.k_token + head * a.k_head;
+    const int64_t slot = a.slots[token];
+    const bool mine = lane * 16u < a.c.head_dim;
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = 0.0f;
+    if (mine) load16<T>(from + (size_t)lane * 16 * T::size, x);
+    // magnitudes as whole numbers: there infinities and NaN lie above all that is finite
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = max(top, dl_bits<uint32_t>(x[i]) & 0x7FFFFFFFu);
+#pragma unroll
+    for (int d = 1; d < LANES; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+    int64_t at, scale_at;
+    if (!place(a, slot, head, &at, &scale_at)) return;
+    const bool finite = top < 0x7F800000u;
+    const float most = fmaxf(dl_bits<float>(top), 0x1p-100f);
+    const float factor = 1.0f / most * C::limit;
+    dl_u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        w[i] = C::code4(x[4 * i] * factor, x[4 * i + 1] * factor, x[4 * i + 2] * factor, x[4 * i + 3] * factor);
+        if (!finite) w[i] = 0;
+    }
+    if (mine) dl_store_at((values ? a.c.v : a.c.k) + at + lane * 16u, w);
+    if (lane == 0) (values ? a.c.v_scale : a.c.k_scale)[scale_at] = finite ? most * (1.0f / C::limit) : __builtin_nanf("");
+}
+
+template <class T, class C, int LANES>
+__global__ void __launch_bounds__(KV_THREADS) dl_kv_read_kernel(const kv_args a)
+{
+    const bool values = blockIdx.y != 0 || !a.k;
+    const uint32_t lane = threadIdx.x % LANES;
+    const uint32_t row = (uint32_t)(((uint64_t)blockIdx.x * KV_THREADS + threadIdx.x) / LANES);
+    if (row >= a.rows || lane * 16u >= a.c.head_dim) return;
+    const uint32_t token = dl_divide(row, a.heads), head = row - token * a.heads.d;
+    char *const to = values ? a.v + token * a.v_token + head * a.v_head : a.k + token * a.k_token + head * a.k_head;
+    float x[16];
+    int64_t at, scale_at;
+    if (place(a, a.slots[token], head, &at, &scale_at)) {
+        const dl_u32x4 w = dl_load_at<dl_u32x4>((values ? a.c.v : a.c.k) + at + lane * 16u);
+        const float scale = (values ? a.c.v_scale : a.c.k_scale)[scale_at];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float y[4];
+            C::value4(w[i], y);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[4 * i + j] = y[j] * scale;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = 0.0f;
+    }
+    store16<T>(to + (size_t)lane * 16 * T::size, x);
+}
+
+template <class F>
+void with_lanes(uint32_t head_dim, F f)
+{
+    if (head_dim <= 16)
+        f(std::integral_constant<int, 1>{});
+    else if (head_dim <= 32)
+        f(std::integral_constant<int, 2>{});
+    else if (head_dim <= 64)
+        f(std::integral_constant<int, 4>{});
+    else if (head_dim <= 128)
+        f(std::integral_constant<int, 8>{});
+    else
+        f(std::integral_constant<int, 16>{});
+}
+
+int kv_setup(const dl_kv_cache *cache, const dl_kv_rows *rows, kv_args *a, bool *nothing)
+{
+    if (!cache || !rows) return DL_ERR_INVALID;
+    const int rc = dl_cache_check(cache, (rows->k ? 1 : 0) | (rows->v ? 2 : 0), &a->c);
+    if (rc != DL_OK) return rc;
+    if (rows->type < DL_TYPE_F32 || rows->type > DL_TYPE_F16 || rows->reserved != 0) return DL_ERR_INVALID;
+    if (rows->tokens < 0 || rows->tokens > INT32_MAX || rows->tokens * (int64_t)cache->heads > INT32_MAX) return DL_ERR_INVALID;
+    *nothing = rows->tokens == 0 || (!rows->k && !rows->v);
+    if (*nothing) return DL_OK;
+    if (!rows->slots) return DL_ERR_INVALID;
+    const int size = rows->type == DL_TYPE_F32 ? 4 : 2;
+    if (((uint64_t)rows->k | (uint64_t)rows->v) % size || (uint64_t)rows->slots % 8u) return DL_ERR_INVALID;
+    a->k = (char *)rows->k;
+    a->v = (char *)rows->v;
+    a->slots = rows->slots;
+    a->k_token = rows->k_token_stride * size;
+    a->k_head = rows->k_head_stride * size;
+    a->v_token = rows->v_token_stride * size;
+    a->v_head = rows->v_head_stride * size;
+    a->slots_end = cache->pages * cache->page_tokens;
+    a->rows = (uint32_t)(rows->tokens * cache->heads);
+    a->tokens = (uint32_t)rows->tokens;
+    a->heads = dl_make_divider((uint32_t)cache->heads);
+    a->shift = -1;
+    for (int i = 0; i < 17; ++i)
+        if (cache->page_tokens == 1 << i) a->shift = i;
+    return DL_OK;
+}
+
+template <bool WRITE>
+int kv_run(const dl_kv_cache *cache, const dl_kv_rows *rows, void *stream)
+{
+    DL_LOCKED;
+    if (!g_dl.inited) return DL_ERR_STATE;
+    if (dl_device_error_pending()) return DL_ERR_LOST;
+    kv_args a;
+    bool nothing;
+    const int rc = kv_setup(cache, rows, &a, &nothing);
+    if (rc != DL_OK || nothing) return rc;
+    dl_with_type(rows->type, [&](auto t) {
+        dl_with_format(cache->format, [&](auto c) {
+            with_lanes(a.c.head_dim, [&](auto lanes) {
+                constexpr int L = decltype(lanes)::value;
+                const uint64_t threads = (uint64_t)a.rows * L;
+                const dim3 grid((uint32_t)((threads + KV_THREADS - 1) / KV_THREADS), a.k && a.v ? 2 : 1);
+                if constexpr (WRITE)
+                    hipLaunchKernelGGL((dl_kv_write_kernel<decltype(t), decltype(c), L>), grid, dim3(KV_THREADS), 0, (hipStream_t)stream, a);
+                else
+                    hipLaunchKernelGGL((dl_kv_read_kernel<decltype(t), decltype(c), L>), grid, dim3(KV_THREADS), 0, (hipStream_t)stream, a);
+            });
+        });
+    });
+    DL_HIP(hipGetLastError());
+    t_dl_last.mode = DL_MODE_ONESHOT;
+    return DL_OK;
+}
+
+}  // namespace
+
+int dl_cache_check(const dl_kv_cache *c, int sides, dl_cache_view *w)
+{
+    if (c->format != DL_KV_FP8 && c->format != DL_KV_INT8) return DL_ERR_INVALID;
+    if (c->heads < 1 || c->heads > 65535 || c->head_dim < 16 || c->head_dim > 256 || c->head_dim % 16) return DL_ERR_INVALID;
+    if (c->page_tokens < 1 || c->page_tokens > 65536 || c->pages < 0 || c->pages > INT32_MAX) return DL_ERR_INVALID;
+    if (c->pages && (((sides & 1) && (!c->k || !c->k_scale)) || ((sides & 2) && (!c->v || !c->v_scale)))) return DL_ERR_INVALID;
+    if (((uint64_t)c->k_scale | (uint64_t)c->v_scale) % 4u) return DL_ERR_INVALID;
+    w->k = (char *)c->k;
+    w->v = (char *)c->v;
+    w->k_scale = c->k_scale;
+    w->v_scale = c->v_scale;
+    w->page_stride = c->page_stride;
+    w->token_stride = c->token_stride;
+    w->head_stride = c->head_stride;
+    w->scale_page_stride = c->scale_page_stride;
+    w->scale_token_stride = c->scale_token_stride;
+    w->scale_head_stride = c->scale_head_stride;
+    w->pages = (uint32_t)c->pages;
+    w->heads = (uint32_t)c->heads;
+    w->head_dim = (uint32_t)c->head_dim;
+    w->page = dl_make_divider((uint32_t)c->page_tokens);
+    return DL_OK;
+}
+
+extern "C" int dl_kv_write(const dl_kv_cache *cache, const dl_kv_rows *rows, void *stream)
+{
+    return kv_run<true>(cache, rows, stream);
+}
+
+extern "C" int dl_kv_read(const dl_kv_cache *cache, const dl_kv_rows *rows, void *stream)
+{
+    return kv_run<false>(cache, rows, stream);
+}

@@ -1,0 +1,241 @@
+// Verification of drafted tokens from given random numbers (dl_verify_draft).
+//
+// A draft x is accepted if u q(x) < p(x), which happens with probability min(1, p / q); behind the accepted ones the next token is
+// drawn from what p has more than q (after a refusal) or from p.  The draw is a race: with e_v exponential of rate 1,
+// the v with the largest w_v / e_v has probability w_v / sum of w.  So the draw is a maximum, and one of (quotient, lowest
+// index) pairs at that: whole numbers of 64 bits, whose maximum does not depend on the order in which it is taken.
+//
+// Which row of p (and q) is drawn from follows from at most 63 pairs of probabilities; every wavefront finds it out for
+// itself, a lane a draft.  Then one pass over that row, split over as many workgroups as fill the chip; the last one of a
+// sequence to finish writes the result.  What is read is one row of p, race and, after a refusal, q: the rows of the
+// other drafts are not touched beyond their own token.
+#include "dl_codes.h"
+#include "dl_internal.h"
+
+namespace {
+
+constexpr uint32_t VERIFY_THREADS = 256;
+
+struct verify_args {
+    const char *target, *draft;
+    const int32_t *draft_tokens, *draft_lens;
+    const float *uniform, *race;
+    int32_t *tokens, *accepted;
+    unsigned long long *best;  // per sequence: the largest pair so far; zero between calls
+    uint32_t *arrived;         // per sequence: workgroups that have finished; zero between calls
+    int64_t target_seq, target_row, draft_seq, draft_row;  // bytes
+    int64_t race_seq;                                      // floats
+    uint32_t drafts, vocab;
+    uint32_t piece;  // entries of the row for a workgroup
+};
+
+template <class T>
+__device__ __forceinline__ float probability(const char *row, uint32_t v)
+{
+    if constexpr (T::size == 4)
+        return dl_load_at<float>(row + 4 * (size_t)v);
+    else
+        return T::one(dl_load_at<uint16_t>(row + 2 * (size_t)v));
+}
+
+// four neighbours
+template <class T>
+__device__ __forceinline__ void probability4(const char *row, uint32_t v, float (&x)[4])
+{
+    if constexpr (T::size == 4) {
+        const dl_f32x4 w = dl_load_at<dl_f32x4>(row + 4 * (size_t)v);
+        x[0] = w[0], x[1] = w[1], x[2] = w[2], x[3] = w[3];
+    } else {
+        const dl_u32x2 w = dl_load_at<dl_u32x2>(row + 2 * (size_t)v);
+        x[0] = T::lo(w[0]), x[1] = T::hi(w[0]), x[2] = T::lo(w[1]), x[3] = T::hi(w[1]);
+    }
+}
+
+// The pair that stands for entry v of weight w: larger quotients first, then lower indexes; 0 for none.
+__device__ __forceinline__ unsigned long long pair_of(float w, float e, uint32_t v)
+{
+    const float score = w / e;
+    return w > 0.0f && score >= 0.0f ? (unsigned long long)dl_bits<uint32_t>(score) << 32 | (0xFFFFFFFFu - v) : 0ull;
+}
+
+__device__ __forceinline__ unsigned long long larger(unsigned long long a, unsigned long long b) { return a > b ? a : b; }
+
+// The largest pair of entries first .. end - 1, in every thread of the workgroup.  q: subtracted where it is not null;
+// without: this entry weighs nothing (vocab: all count).
+template <class T>
+__device__ unsigned long long best_of(const char *p, const char *q, const float *race, uint32_t without, uint32_t first, uint32_t end)
+{
+    __shared__ unsigned long long part[VERIFY_THREADS / 64];
+    unsigned long long best = 0;
+    uint32_t v = first + threadIdx.x * 4u;
+    for (; v + 4u <= end; v += VERIFY_THREADS * 4u) {
+        float w[4], x[4];
+        probability4<T>(p, v, w);
+        const dl_f32x4 e = dl_load_at<dl_f32x4>(race + v);
+        if (q) {
+            probability4<T>(q, v, x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] -= x[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) best = larger(best, pair_of(v + i == without ? 0.0f : w[i], e[i], v + i));
+    }
+    for (; v < end; ++v) {  // one thread's: the end of the row inside its four
+        float w = probability<T>(p, v);
+        if (q) w -= probability<T>(q, v);
+        best = larger(best, pair_of(v == without ? 0.0f : w, race[v], v));
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) best = larger(best, (unsigned long long)__shfl_xor((long long)best, d));
+    __syncthreads();  // the words may still be read from an earlier call
+    if (threadIdx.x % 64u == 0) part[threadIdx.x / 64u] = best;
+    __syncthreads();
+#pragma unroll
+    for (uint32_t i = 0; i < VERIFY_THREADS / 64; ++i) best = larger(best, part[i]);
+    return best;
+}
+
+template <class T>
+__global__ void __launch_bounds__(VERIFY_THREADS) dl_verify_kernel(const verify_args a)
+{
+    const uint32_t b = blockIdx.y, lane = threadIdx.x % 64u;
+    uint32_t n = a.drafts;
+    if (a.draft_lens) n = (uint32_t)min(max(a.draft_lens[b], 0), (int32_t)a.drafts);
+    const char *const target = a.target + b * a.target_seq;
+    const char *const draft = a.draft ? a.draft + b * a.draft_seq : nullptr;
+
+    int32_t x = -1;
+    bool refused = false;
+    if (lane < n) {
+        x = a.draft_tokens[(size_t)b * a.drafts + lane];
+        refused = true;
+        if (x >= 0 && (uint32_t)x < a.vocab) {
+            const float u = a.uniform[(size_t)b * a.drafts + lane];
+            const float p = probability<T>(target + lane * a.target_row, (uint32_t)x);
+            const float q = draft ? probability<T>(draft + lane * a.draft_row, (uint32_t)x) : 1.0f;
+            refused = !(u * q < p);
+        }
+    }
+    const unsigned long long where = __ballot(refused);
+    const uint32_t taken = where ? (uint32_t)__ffsll((long long)where) - 1u : n;
+    const bool rest = taken < n;
+
+    const char *const p = target + taken * a.target_row;
+    const char *const q = rest && draft ? draft + taken * a.draft_row : nullptr;
+    // (a draft outside the vocabulary is -1 or at least vocab as an unsigned number: no entry)
+    const uint32_t without = rest && !draft ? (uint32_t)__shfl(x, (int)taken) : 0xFFFFFFFFu;
+    const float *const race = a.race + b * a.race_seq;
+    const uint32_t first = blockIdx.x * a.piece, end = min(first + a.piece, a.vocab);
+    unsigned long long best = best_of<T>(p, q, race, without, first, end);
+
+    if (gridDim.x > 1) {
+        __shared__ unsigned long long joined;
+        __shared__ bool last;
+        if (threadIdx.x == 0) {
+            if (best) __hip_atomic_fetch_max(a.best + b, best, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            last = __hip_atomic_fetch_add(a.arrived + b, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1u;
+            if (last) {
+                joined = __hip_atomic_exchange(a.best + b, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                __hip_atomic_store(a.arrived + b, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+        }
+        __syncthreads();
+        if (!last) return;
+        best = joined;
+    }
+    // nothing left of p beyond q (both equal, say, and p zero at the draft): from p itself
+    if (!best && rest) best = best_of<T>(p, nullptr, race, 0xFFFFFFFFu, 0, a.vocab);
+    if (threadIdx.x <= a.drafts) {  // at most 64 entries: the first wavefront, whose lanes hold the drafts
+        const int32_t next = best ? (int32_t)(0xFFFFFFFFu - (uint32_t)best) : -1;
+        a.tokens[(size_t)b * (a.drafts + 1u) + threadIdx.x] = threadIdx.x < taken ? x : threadIdx.x == taken ? next : -1;
+        if (threadIdx.x == 0) a.accepted[b] = (int32_t)taken;
+    }
+}
+
+// Workgroups a sequence: enough that the chip's 256 compute units have four each, from at least 2048 entries.
+uint32_t verify_split(int32_t batch, int32_t vocab)
+{
+    const uint32_t wanted = (1024u + (uint32_t)batch - 1u) / (uint32_t)batch;
+    const uint32_t most = ((uint32_t)vocab + 2047u) / 2048u;
+    return wanted < most ? wanted : most;
+}
+
+constexpr int32_t VERIFY_MAX_BATCH = 1 << 20;
+// sequences that are split (at most 1023 of them) have a pair and a counter each in the control words
+static_assert(1024 * (sizeof(unsigned long long) + sizeof(uint32_t)) <= DL_CONTROL_BYTES, "control words of the sequences that are split");
+
+int verify_check(const dl_verify_draft_args *a)
+{
+    if (!a) return DL_ERR_INVALID;
+    if (a->type < DL_TYPE_F32 || a->type > DL_TYPE_F16) return DL_ERR_INVALID;
+    if (a->batch < 0 || a->batch > VERIFY_MAX_BATCH || a->drafts < 0 || a->drafts > DL_MAX_DRAFTS || a->vocab < 1 || a->vocab > 1 << 30)
+        return DL_ERR_INVALID;
+    return DL_OK;
+}
+
+}  // namespace
+
+extern "C" int64_t dl_verify_draft_workspace(const dl_verify_draft_args *args)
+{
+    const int rc = verify_check(args);
+    return rc != DL_OK ? rc : (int64_t)DL_CONTROL_BYTES;
+}
+
+extern "C" int dl_verify_draft(const dl_verify_draft_args *args, void *stream)
+{
+    DL_LOCKED;
+    if (!g_dl.inited) return DL_ERR_STATE;
+    if (dl_device_error_pending()) return DL_ERR_LOST;
+    const int rc = verify_check(args);
+    if (rc != DL_OK) return rc;
+    if (args->batch == 0) return DL_OK;
+    if (!args->target || !args->race || !args->tokens || !args->accepted) return DL_ERR_INVALID;
+    if (args->drafts && (!args->draft_tokens || !args->uniform)) return DL_ERR_INVALID;
+    const uint64_t size = args->type == DL_TYPE_F32 ? 4 : 2;
+    if (((uint64_t)args->target | (uint64_t)args->draft) % size) return DL_ERR_INVALID;
+    if (((uint64_t)args->race | (uint64_t)args->uniform | (uint64_t)args->draft_tokens | (uint64_t)args->draft_lens | (uint64_t)args->tokens |
+         (uint64_t)args->accepted) %
+        4u)
+        return DL_ERR_INVALID;
+    const uint32_t split = verify_split(args->batch, args->vocab);
+    if (split > 1 && (!args->workspace || args->workspace_bytes < DL_CONTROL_BYTES || (uint64_t)args->workspace % 16u)) return DL_ERR_INVALID;
+    verify_args a;
+    a.target = (const char *)args->target;
+    a.draft = (const char *)args->draft;
+    a.draft_tokens = args->draft_tokens;
+    a.draft_lens = args->draft_lens;
+    a.uniform = args->uniform;
+    a.race = args->race;
+    a.tokens = args->tokens;
+    a.accepted = args->accepted;
+    a.best = (unsigned long long *)args->workspace;
+    a.arrived = (uint32_t *)(a.best + 1024);
+    a.target_seq = args->target_seq_stride * (int64_t)size;
+    a.target_row = args->target_row_stride * (int64_t)size;
+    a.draft_seq = args->draft_seq_stride * (int64_t)size;
+    a.draft_row = args->draft_row_stride * (int64_t)size;
+    a.race_seq = args->race_stride;
+    a.drafts = (uint32_t)args->drafts;
+    a.vocab = (uint32_t)args->vocab;
+    a.piece = (((uint32_t)args->vocab + split - 1u) / split + 3u) & ~3u;
+    const dim3 grid(((uint32_t)args->vocab + a.piece - 1u) / a.piece, 1);
+    dl_with_type(args->type, [&](auto t) {
+        // (a grid is at most 65 535 high)
+        for (int32_t b0 = 0; b0 < args->batch; b0 += 65535) {
+            const uint32_t n = (uint32_t)(args->batch - b0 < 65535 ? args->batch - b0 : 65535);
+            verify_args c = a;
+            c.target += b0 * a.target_seq;
+            if (c.draft) c.draft += b0 * a.draft_seq;
+            if (c.draft_tokens) c.draft_tokens += (int64_t)b0 * args->drafts;
+            if (c.draft_lens) c.draft_lens += b0;
+            if (c.uniform) c.uniform += (int64_t)b0 * args->drafts;
+            c.race += b0 * a.race_seq;
+            c.tokens += (int64_t)b0 * (args->drafts + 1);
+            c.accepted += b0;
+            hipLaunchKernelGGL((dl_verify_kernel<decltype(t)>), dim3(grid.x, n), dim3(VERIFY_THREADS), 0, (hipStream_t)stream, c);
+        }
+    });
+    DL_HIP(hipGetLastError());
+    t_dl_last.mode = DL_MODE_ONESHOT;
+    return DL_OK;
+}
