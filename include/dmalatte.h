@@ -548,7 +548,8 @@ typedef enum dl_kv_format { DL_KV_FP8 = 0, DL_KV_INT8 = 1 } dl_kv_format;
  * place s % page_tokens of page s / page_tokens.  Code d of a row lies at
  *   base + page * page_stride + place * token_stride + head * head_stride + d     (strides in bytes)
  * and its scale at the same place of the scale array with the scale strides (in floats), for keys and values alike.  So
- * pages may be separate arrays of codes and of scales, or blocks that hold all four and are moved as one.
+ * pages may be separate arrays of codes and of scales, or blocks that hold all four and are moved as one.  Strides are not negative,
+ * and those of pages and tokens stay below 4 GiB.
  */
 typedef struct dl_kv_cache {
     void *k, *v;              /* codes */

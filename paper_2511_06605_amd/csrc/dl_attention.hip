@@ -64,20 +64,246 @@ __device__ __forceinline__ words<N> load_words(const char *p)
     return dl_load_at<words<N>>(p);
 }
 
-// NT tiles of 16 rows against the keys first .. end - 1 of one head.
-template <class Q, class C, int DP, int NT>
-__device__ void attend(const att_args &a, uint32_t head, const int32_t *table, uint32_t first, uint32_t end, const char *const (&qrow)[NT],
-                       const int32_t (&last)[NT], const uint32_t (&row)[NT], const bool (&store)[NT], uint32_t piece)
+// The largest over the lanes that hold the same query (16 and 32 apart), in all of them: halves and quarters change places.
+__device__ __forceinline__ float largest_of_quarters(float x)
 {
-    constexpr int KB = DP / 4;    // bytes of a key's row that a lane holds: dims KB * g ..
-    constexpr int VB = DP / 16;   // bytes of a value's row that a lane holds: dims VB * i ..
-    constexpr int STEPS = DP / 32;
-    const uint32_t lane = threadIdx.x % 64u, wave = threadIdx.x / 64u;
-    const uint32_t i = lane % 16u, g = lane / 16u;
-    const uint32_t D = a.c.head_dim;
+    const auto a = __builtin_amdgcn_permlane32_swap(dl_bits<uint32_t>(x), dl_bits<uint32_t>(x), false, false);
+    const float y = fmaxf(dl_bits<float>((uint32_t)a[0]), dl_bits<float>((uint32_t)a[1]));
+    const auto b = __builtin_amdgcn_permlane16_swap(dl_bits<uint32_t>(y), dl_bits<uint32_t>(y), false, false);
+    return fmaxf(dl_bits<float>((uint32_t)b[0]), dl_bits<float>((uint32_t)b[1]));
+}
+
+// What is the same for a workgroup's whole piece: NT tiles of 16 rows against the keys first .. end - 1 of one head.
+struct piece_args {
+    const int32_t *table;
+    uint32_t head, first, end, piece;
+    int32_t seen_by_all;  // keys up to this one are seen by every row
+};
+
+// Where a step's keys lie, as far as a lane (i, g) = (lane % 16, lane / 16) has to know: it holds parts of the keys 8 (i / 4) + 4 t +
+// i % 4 (t = 0, 1), of the values of 8 g .. 8 g + 7, and the scale of key 8 g + i % 8 (the keys' where i < 8, the values' else).
+// ALIGNED (pages hold a multiple of 8 tokens): eight keys 8 x .. 8 x + 7 lie in one page, and two pages are looked up, a step
+// ahead of the loads that need them.
+template <bool ALIGNED>
+struct place {
+    uint32_t base;
+    uint32_t key_page, value_page;
+
+    static __device__ __forceinline__ uint32_t clamped(const piece_args &p, uint32_t key) { return min(key, ALIGNED ? (p.end - 1u) & ~7u : p.end - 1u); }
+
+    __device__ __forceinline__ void look_up(const att_args &a, const piece_args &p, uint32_t at)
+    {
+        base = at;
+        if constexpr (ALIGNED) {
+            const uint32_t lane = threadIdx.x % 64u;
+            key_page = (uint32_t)p.table[dl_divide(clamped(p, at + 8u * (lane % 16u / 4u)), a.c.page)];
+            value_page = (uint32_t)p.table[dl_divide(clamped(p, at + 8u * (lane / 16u)), a.c.page)];
+        }
+    }
+    // key 8 x + in, in page `page` if that is known already: the offset of its row, and whether its page is one of the pool
+    __device__ __forceinline__ uint64_t offset(const att_args &a, const piece_args &p, uint32_t x, uint32_t in, uint32_t page, uint32_t page_stride,
+                                               uint32_t token_stride, uint64_t from, bool *alive) const
+    {
+        const uint32_t key = clamped(p, base + 8u * x + (ALIGNED ? 0u : in)), n = dl_divide(key, a.c.page);
+        if constexpr (!ALIGNED) page = (uint32_t)p.table[n];
+        *alive = page < a.c.pages;
+        page = *alive ? page : 0u;
+        return from + (uint64_t)page * page_stride + (uint64_t)(key - n * a.c.page.d + (ALIGNED ? in : 0u)) * token_stride;
+    }
+};
+
+template <int DP>
+struct tile_keys {
+    words<16> k[2][DP / 64];  // dims DP / 4 * g ..
+    float scale;
+};
+template <int DP>
+struct tile_values {
+    words<DP / 16> v[8];  // dims DP / 16 * i ..
+    uint32_t dead;        // bit e: the page of key 8 g + e
+};
+
+template <int DP, bool ALIGNED>
+__device__ __forceinline__ void load_keys(const att_args &a, const piece_args &p, const place<ALIGNED> &at, tile_keys<DP> &td)
+{
+    constexpr int KB = DP / 4;
+    const uint32_t lane = threadIdx.x % 64u, i = lane % 16u, g = lane / 16u, D = a.c.head_dim;
+    const uint64_t from = (uint64_t)a.c.k + (uint64_t)p.head * a.c.head_stride + KB * g;
+    bool alive;
+    uint64_t kp = 0;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        if (t == 0 || !ALIGNED)
+            kp = at.offset(a, p, i / 4u, i % 4u + 4u * t, at.key_page, a.c.page_stride, a.c.token_stride, from, &alive);
+        else
+            kp += 4ull * a.c.token_stride;
+#pragma unroll
+        for (int s = 0; s < KB / 16; ++s) td.k[t][s] = KB * g + 16u * s < D ? load_words<16>((const char *)kp + 16 * s) : words<16>{};
+    }
+    const uint64_t scales = (uint64_t)(i < 8u ? a.c.k_scale : a.c.v_scale) + (uint64_t)p.head * a.c.scale_head_stride;
+    td.scale = *(const float *)at.offset(a, p, g, i % 8u, at.value_page, a.c.scale_page_stride, a.c.scale_token_stride, scales, &alive);
+}
+
+template <int DP, bool ALIGNED>
+__device__ __forceinline__ void load_values(const att_args &a, const piece_args &p, const place<ALIGNED> &at, tile_values<DP> &td)
+{
+    constexpr int VB = DP / 16;
+    const uint32_t lane = threadIdx.x % 64u, i = lane % 16u, g = lane / 16u, D = a.c.head_dim;
+    const uint64_t from = (uint64_t)a.c.v + (uint64_t)p.head * a.c.head_stride + VB * i;
+    bool alive;
+    uint64_t vp = 0;
+    td.dead = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if (e == 0 || !ALIGNED) {
+            vp = at.offset(a, p, g, (uint32_t)e, at.value_page, a.c.page_stride, a.c.token_stride, from, &alive);
+            if (!alive) td.dead |= ALIGNED ? 0xFFu : 1u << e;
+        } else {
+            vp += a.c.token_stride;
+        }
+        td.v[e] = VB * i < D ? load_words<VB>((const char *)vp) : words<VB>{};
+    }
+}
+
+template <int DP, int NT>
+struct sums {
+    dl_f32x4 o[NT][DP / 16];  // rows of the product are dims (DP / 16 * (4 g + j) + t in lane (i, g)), its columns queries (i)
+    float r[NT], low[NT];     // the reference, the same in all lanes of a query; low: less Q::lift, finite
+    float l[NT];              // a lane's share
+};
+
+// A step: 32 keys against NT tiles of 16 rows.  whole: all of them are seen by all.  The next step's keys are loaded as
+// soon as the scores have been taken, its values after the sums, into the same registers.
+template <class Q, class C, int DP, int NT, bool ALIGNED>
+__device__ __forceinline__ void attend_tile(const att_args &a, const piece_args &p, const place<ALIGNED> &at, const place<ALIGNED> &then, bool whole,
+                                            tile_keys<DP> &tk, tile_values<DP> &tv, const dl_u32x4 (&qf)[NT][DP / 32], const int32_t (&last)[NT], sums<DP, NT> &acc,
+                                            float (&scales)[3][TILE])
+{
+    constexpr int VB = DP / 16, STEPS = DP / 32;
+    const uint32_t lane = threadIdx.x % 64u, i = lane % 16u, g = lane / 16u, base = at.base;
+    uint32_t here = 0;  // bit e: key 8 g + e is in a page of the pool, and of the piece
+    {
+        if (!whole) {
+            const uint32_t left = p.end - min(p.end, base + 8u * g);
+            here = (left >= 8u ? 0xFFu : (1u << left) - 1u) & ~tv.dead;
+        }
+        const uint32_t key = 8u * g + i % 8u;
+        if (i < 8u) {
+            scales[0][key] = tk.scale * a.scale;
+        } else {
+            // a logarithm and a reciprocal of what is no denormal number.  A scale of NaN reaches its readers' weights through
+            // the logarithm; the reciprocal is finite, so that a weight of zero takes it out.
+            const float u = tk.scale < 0x1p-120f ? 0x1p-120f : tk.scale;
+            scales[1][key] = __builtin_amdgcn_logf(u);
+            scales[2][key] = __builtin_amdgcn_rcpf(u == u ? u : 1.0f);
+        }
+    }
+    // scores: the product's rows are keys (8 g + 4 t + j in lane (i, g)), its columns queries (i)
+    dl_f32x4 s[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = dl_f32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const dl_u32x2 x = C::template spread<Q>(tk.k[t][st / 2].w[2 * (st % 2)]), y = C::template spread<Q>(tk.k[t][st / 2].w[2 * (st % 2) + 1]);
+            const dl_u32x4 kf = {x[0], x[1], y[0], y[1]};
+#pragma unroll
+            for (int n = 0; n < NT; ++n) s[n][t] = Q::mfma16(kf, qf[n][st], s[n][t]);
+        }
+    if (then.base < p.end) load_keys<DP, ALIGNED>(a, p, then, tk);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    float ks[8], lu[8], iu[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        ks[e] = scales[0][8u * g + e];
+        lu[e] = scales[1][8u * g + e];
+        iu[e] = scales[2][8u * g + e];
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    dl_u32x4 pf[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        float x[8], top = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = fmaf(s[n][e / 4][e % 4], ks[e], lu[e]);
+        if (!whole) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (!(here >> e & 1u) || (int32_t)(base + 8u * g + e) > last[n]) x[e] = -INFINITY;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = fmaxf(top, x[e]);
+        // The reference follows the largest only where that is 2^8 times above it: most steps then neither ask the other
+        // lanes nor touch the sums, and a weight is at most 2^(8 + lift), which both types hold.
+        if (__any(top > acc.r[n] + 8.0f)) {
+            const float now = fmaxf(acc.r[n], largest_of_quarters(top));
+            const float ref = now == -INFINITY ? 0.0f : now;
+            const float fade = __builtin_amdgcn_exp2f(acc.r[n] - ref);
+            acc.r[n] = now;
+            acc.low[n] = ref - Q::lift;
+            acc.l[n] *= fade;
+#pragma unroll
+            for (int t = 0; t < DP / 16; ++t) acc.o[n][t] *= fade;
+        }
+        float w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            w[e] = __builtin_amdgcn_exp2f(x[e] - acc.low[n]);
+            acc.l[n] = fmaf(w[e], iu[e], acc.l[n]);
+        }
+        pf[n] = dl_u32x4{Q::pack(w[0], w[1]), Q::pack(w[2], w[3]), Q::pack(w[4], w[5]), Q::pack(w[6], w[7])};
+    }
+    if (!whole) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (!(here >> e & 1u)) tv.v[e] = words<VB>{};
+    }
+#pragma unroll
+    for (int q4 = 0; q4 < VB / 4; ++q4) {
+        // four keys' four dims each, turned to four dims' four keys each
+        dl_u32x2 half[2][4];  // [keys 0 .. 3 and 4 .. 7][dim]: four elements
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t w0 = tv.v[4 * h].w[q4], w1 = tv.v[4 * h + 1].w[q4], w2 = tv.v[4 * h + 2].w[q4], w3 = tv.v[4 * h + 3].w[q4];
+            const uint32_t a01 = __builtin_amdgcn_perm(w1, w0, 0x05010400u), a23 = __builtin_amdgcn_perm(w3, w2, 0x05010400u);
+            const uint32_t b01 = __builtin_amdgcn_perm(w1, w0, 0x07030602u), b23 = __builtin_amdgcn_perm(w3, w2, 0x07030602u);
+            half[h][0] = C::template spread<Q>(__builtin_amdgcn_perm(a23, a01, 0x05040100u));
+            half[h][1] = C::template spread<Q>(__builtin_amdgcn_perm(a23, a01, 0x07060302u));
+            half[h][2] = C::template spread<Q>(__builtin_amdgcn_perm(b23, b01, 0x05040100u));
+            half[h][3] = C::template spread<Q>(__builtin_amdgcn_perm(b23, b01, 0x07060302u));
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const dl_u32x4 vf = {half[0][t][0], half[0][t][1], half[1][t][0], half[1][t][1]};
+#pragma unroll
+            for (int n = 0; n < NT; ++n) acc.o[n][4 * q4 + t] = Q::mfma16(vf, pf[n], acc.o[n][4 * q4 + t]);
+        }
+    }
+    if (then.base < p.end) load_values<DP, ALIGNED>(a, p, then, tv);
+}
+
+template <class Q, class C, int DP, int NT, bool ALIGNED>
+__device__ void attend(const att_args &a, const piece_args &p, const char *const (&qrow)[NT], const int32_t (&last)[NT], const uint32_t (&row)[NT],
+                       const bool (&store)[NT])
+{
+    constexpr int KB = DP / 4, VB = DP / 16, STEPS = DP / 32;
+    const uint32_t lane = threadIdx.x % 64u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
+    const uint32_t g = lane / 16u, D = a.c.head_dim;
 
     __shared__ float scales[ATT_WAVES][3][TILE];
     __shared__ float joined[2][NT * DP / 16 * 4 + 2 * NT][64];
+
+    place<ALIGNED> at, then;
+    at.look_up(a, p, p.first + wave * TILE);
+    tile_keys<DP> tk;
+    tile_values<DP> tv;
+    if (at.base < p.end) {
+        load_keys<DP, ALIGNED>(a, p, at, tk);
+        load_values<DP, ALIGNED>(a, p, at, tv);
+    }
 
     // queries: lane (i, g) holds dims KB * g .. of row i, eight a step
     dl_u32x4 qf[NT][STEPS];
@@ -89,141 +315,26 @@ __device__ void attend(const att_args &a, uint32_t head, const int32_t *table, u
             qf[n][s] = d < D ? dl_load_at<dl_u32x4>(qrow[n] + 2u * d) : dl_u32x4{0, 0, 0, 0};
         }
 
-    dl_f32x4 o[NT][DP / 16];
-    float r[NT], l[NT];
+    sums<DP, NT> acc;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        r[n] = -INFINITY;
-        l[n] = 0.0f;
+        acc.r[n] = -INFINITY;
+        acc.low[n] = -Q::lift;
+        acc.l[n] = 0.0f;
 #pragma unroll
-        for (int t = 0; t < DP / 16; ++t) o[n][t] = dl_f32x4{0, 0, 0, 0};
+        for (int t = 0; t < DP / 16; ++t) acc.o[n][t] = dl_f32x4{0, 0, 0, 0};
     }
 
-    for (uint32_t base = first + wave * TILE; base < end; base += STEP) {
-        auto locate = [&](uint32_t key, bool *ok) {
-            *ok = key < end;
-            const uint32_t k = min(key, end - 1u);
-            const uint32_t p = dl_divide(k, a.c.page);
-            uint32_t page = (uint32_t)table[p];
-            if (page >= a.c.pages) *ok = false, page = 0;
-            return (int64_t)page * a.c.page_stride + (int64_t)(k - p * a.c.page.d) * a.c.token_stride + (int64_t)head * a.c.head_stride;
-        };
-        // keys: lane (i, g) holds its part of keys 8 (i / 4) + 4 t + i % 4, t = 0, 1
-        words<16> kw[2][KB / 16];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            bool ok;
-            const char *p = a.c.k + locate(base + 8u * (i / 4u) + 4u * t + i % 4u, &ok) + KB * g;
-#pragma unroll
-            for (int s = 0; s < KB / 16; ++s) kw[t][s] = KB * g + 16u * s < D ? load_words<16>(p + 16 * s) : words<16>{};
-        }
-        // values: lane (i, g) holds its part of keys 8 g + e
-        words<VB> vw[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            bool ok;
-            const char *p = a.c.v + locate(base + 8u * g + e, &ok) + VB * i;
-            vw[e] = VB * i < D && ok ? load_words<VB>(p) : words<VB>{};
-        }
-        // scales: a lane a key, keys' in the lower half and values' in the upper
-        bool alive;
-        {
-            const uint32_t key = base + lane % TILE, k = min(key, end - 1u);
-            const uint32_t p = dl_divide(k, a.c.page);
-            uint32_t page = (uint32_t)table[p];
-            alive = key < end && page < a.c.pages;
-            if (page >= a.c.pages) page = 0;
-            const int64_t at = (int64_t)page * a.c.scale_page_stride + (int64_t)(k - p * a.c.page.d) * a.c.scale_token_stride +
-                               (int64_t)head * a.c.scale_head_stride;
-            if (lane < TILE) {
-                scales[wave][0][lane] = alive ? a.c.k_scale[at] * a.scale : 0.0f;
-            } else {
-                const float u = fmaxf(a.c.v_scale[at], 0x1p-120f);
-                const bool nan = a.c.v_scale[at] != a.c.v_scale[at];
-                scales[wave][1][lane - TILE] = !alive ? -INFINITY : nan ? __builtin_nanf("") : __builtin_amdgcn_logf(u);
-                scales[wave][2][lane - TILE] = !alive ? 0.0f : __builtin_amdgcn_rcpf(u);
-            }
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        float ks[8], lu[8], iu[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            ks[e] = scales[wave][0][8u * g + e];
-            lu[e] = scales[wave][1][8u * g + e];
-            iu[e] = scales[wave][2][8u * g + e];
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        // scores: the product's rows are keys (8 g + 4 t + j in lane (i, g)), its columns queries (i)
-        dl_f32x4 s[NT][2];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = dl_f32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int st = 0; st < STEPS; ++st) {
-                const dl_u32x2 x = C::template spread<Q>(kw[t][st / 2].w[2 * (st % 2)]), y = C::template spread<Q>(kw[t][st / 2].w[2 * (st % 2) + 1]);
-                const dl_u32x4 kf = {x[0], x[1], y[0], y[1]};
-#pragma unroll
-                for (int n = 0; n < NT; ++n) s[n][t] = Q::mfma16(kf, qf[n][st], s[n][t]);
-            }
-        dl_u32x4 pf[NT];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            float x[8], top = -INFINITY;
-            bool seen[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                seen[e] = (int32_t)(base + 8u * g + e) <= last[n] && lu[e] != -INFINITY;
-                x[e] = seen[e] ? fmaf(s[n][e / 4][e % 4], ks[e], lu[e]) : -INFINITY;
-                top = fmaxf(top, x[e]);
-            }
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float now = fmaxf(r[n], top);
-            const float ref = now == -INFINITY ? 0.0f : now;
-            const float fade = __builtin_amdgcn_exp2f(r[n] - ref);
-            r[n] = now;
-            const float low = ref - Q::lift;
-            float w[8], sum = 0.0f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                w[e] = __builtin_amdgcn_exp2f(x[e] - low);
-                sum += seen[e] ? w[e] * iu[e] : 0.0f;
-            }
-            l[n] = l[n] * fade + sum;
-#pragma unroll
-            for (int t = 0; t < DP / 16; ++t) o[n][t] *= fade;
-            pf[n] = dl_u32x4{Q::pack(w[0], w[1]), Q::pack(w[2], w[3]), Q::pack(w[4], w[5]), Q::pack(w[6], w[7])};
-        }
-        // sums: the product's rows are dims (VB * (4 g + j) + t in lane (i, g)), its columns queries (i)
-#pragma unroll
-        for (int q4 = 0; q4 < VB / 4; ++q4) {
-            // four keys' four dims each, turned to four dims' four keys each
-            dl_u32x2 half[2][4];  // [keys 0 .. 3 and 4 .. 7][dim]: four elements
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const uint32_t w0 = vw[4 * h].w[q4], w1 = vw[4 * h + 1].w[q4], w2 = vw[4 * h + 2].w[q4], w3 = vw[4 * h + 3].w[q4];
-                const uint32_t a01 = __builtin_amdgcn_perm(w1, w0, 0x05010400u), a23 = __builtin_amdgcn_perm(w3, w2, 0x05010400u);
-                const uint32_t b01 = __builtin_amdgcn_perm(w1, w0, 0x07030602u), b23 = __builtin_amdgcn_perm(w3, w2, 0x07030602u);
-                half[h][0] = C::template spread<Q>(__builtin_amdgcn_perm(a23, a01, 0x05040100u));
-                half[h][1] = C::template spread<Q>(__builtin_amdgcn_perm(a23, a01, 0x07060302u));
-                half[h][2] = C::template spread<Q>(__builtin_amdgcn_perm(b23, b01, 0x05040100u));
-                half[h][3] = C::template spread<Q>(__builtin_amdgcn_perm(b23, b01, 0x07060302u));
-            }
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const dl_u32x4 vf = {half[0][t][0], half[0][t][1], half[1][t][0], half[1][t][1]};
-#pragma unroll
-                for (int n = 0; n < NT; ++n) o[n][4 * q4 + t] = Q::mfma16(vf, pf[n], o[n][4 * q4 + t]);
-            }
-        }
+    for (; at.base < p.end; at = then) {
+        then.look_up(a, p, at.base + STEP);
+        bool whole = false;
+        if (ALIGNED && (int32_t)(at.base + TILE - 1u) <= p.seen_by_all) whole = !__any(at.key_page >= a.c.pages);
+        attend_tile<Q, C, DP, NT, ALIGNED>(a, p, at, then, whole, tk, tv, qf, last, acc, scales[wave]);
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        l[n] += __shfl_xor(l[n], 16);
-        l[n] += __shfl_xor(l[n], 32);
+        acc.l[n] += __shfl_xor(acc.l[n], 16);
+        acc.l[n] += __shfl_xor(acc.l[n], 32);
     }
     // the wavefronts' sums, two by two: 2 and 3 to 0 and 1, then 1 to 0
 #pragma unroll
@@ -232,12 +343,12 @@ __device__ void attend(const att_args &a, uint32_t head, const int32_t *table, u
             float(*to)[64] = joined[wave - half];
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                to[2 * n][lane] = r[n];
-                to[2 * n + 1][lane] = l[n];
+                to[2 * n][lane] = acc.r[n];
+                to[2 * n + 1][lane] = acc.l[n];
 #pragma unroll
                 for (int t = 0; t < DP / 16; ++t)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) to[2 * NT + (n * (DP / 16) + t) * 4 + j][lane] = o[n][t][j];
+                    for (int j = 0; j < 4; ++j) to[2 * NT + (n * (DP / 16) + t) * 4 + j][lane] = acc.o[n][t][j];
             }
         }
         __syncthreads();
@@ -245,14 +356,14 @@ __device__ void attend(const att_args &a, uint32_t head, const int32_t *table, u
             const float(*from)[64] = joined[wave];
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const float r2 = from[2 * n][lane], now = fmaxf(r[n], r2), ref = now == -INFINITY ? 0.0f : now;
-                const float f = __builtin_amdgcn_exp2f(r[n] - ref), f2 = __builtin_amdgcn_exp2f(r2 - ref);
-                r[n] = now;
-                l[n] = l[n] * f + from[2 * n + 1][lane] * f2;
+                const float r2 = from[2 * n][lane], now = fmaxf(acc.r[n], r2), ref = now == -INFINITY ? 0.0f : now;
+                const float f = __builtin_amdgcn_exp2f(acc.r[n] - ref), f2 = __builtin_amdgcn_exp2f(r2 - ref);
+                acc.r[n] = now;
+                acc.l[n] = acc.l[n] * f + from[2 * n + 1][lane] * f2;
 #pragma unroll
                 for (int t = 0; t < DP / 16; ++t)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) o[n][t][j] = o[n][t][j] * f + from[2 * NT + (n * (DP / 16) + t) * 4 + j][lane] * f2;
+                    for (int j = 0; j < 4; ++j) acc.o[n][t][j] = acc.o[n][t][j] * f + from[2 * NT + (n * (DP / 16) + t) * 4 + j][lane] * f2;
             }
         }
         __syncthreads();
@@ -261,21 +372,22 @@ __device__ void attend(const att_args &a, uint32_t head, const int32_t *table, u
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         if (!store[n]) continue;
-        const uint64_t at = (uint64_t)piece * a.rows + row[n];
-        if (g == 0) a.rl[at] = dl_f32x2{r[n], l[n]};
+        const uint64_t at = (uint64_t)p.piece * a.rows + row[n];
+        if (g == 0) a.rl[at] = dl_f32x2{acc.r[n], acc.l[n]};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const uint32_t d = VB * (4u * g + j);
             if (d >= D) continue;
             float *to = a.partial + at * D + d;
 #pragma unroll
-            for (int t = 0; t < VB; t += 4) *(dl_f32x4 *)(to + t) = dl_f32x4{o[n][t][j], o[n][t + 1][j], o[n][t + 2][j], o[n][t + 3][j]};
+            for (int t = 0; t < VB; t += 4)
+                *(dl_f32x4 *)(to + t) = dl_f32x4{acc.o[n][t][j], acc.o[n][t + 1][j], acc.o[n][t + 2][j], acc.o[n][t + 3][j]};
         }
     }
 }
 
-template <class Q, class C, int DP, int NT>
-__global__ void __launch_bounds__(ATT_THREADS) dl_attention_kernel(const att_args a)
+template <class Q, class C, int DP, int NT, bool ALIGNED>
+__global__ void __launch_bounds__(ATT_THREADS, DP * NT <= 128 ? 2 : 1) dl_attention_kernel(const att_args a)
 {
     const uint32_t i = threadIdx.x % 16u;
     const char *qrow[NT];
@@ -287,26 +399,30 @@ __global__ void __launch_bounds__(ATT_THREADS) dl_attention_kernel(const att_arg
     const bool prefix = blockIdx.x < shared;
     const uint32_t x = prefix ? blockIdx.x : blockIdx.x - shared;
     const uint32_t head = x % heads, tiles = prefix ? a.prefix_tiles : a.own_tiles, tile = x / heads % tiles;
-    uint32_t piece = x / heads / tiles, b0 = 0, first, end, rows;
-    const int32_t *table;
+    uint32_t piece = x / heads / tiles, b0 = 0, rows;
     int32_t own_last = 0;  // of query 0
+    piece_args p;
+    p.head = head;
     if (prefix) {
-        first = piece * a.prefix_piece;
-        end = min(first + a.prefix_piece, a.prefix_tokens);
-        table = a.prefix_pages;
+        p.first = piece * a.prefix_piece;
+        p.end = min(p.first + a.prefix_piece, a.prefix_tokens);
+        p.table = a.prefix_pages;
+        p.seen_by_all = (int32_t)p.end - 1;
         rows = a.batch * seq_rows;
     } else {
         b0 = piece % a.batch;
         piece /= a.batch;
         const uint32_t len = own_len(a, b0), step = own_piece(a, len);
-        first = piece * step;
-        if (first >= len) return;
-        end = min(first + step, len);
-        table = a.pages + b0 * a.pages_stride;
+        p.first = piece * step;
+        if (p.first >= len) return;
+        p.end = min(p.first + step, len);
+        p.table = a.pages + b0 * a.pages_stride;
         rows = seq_rows;
         own_last = (int32_t)len - (int32_t)queries(a, b0);
+        p.seen_by_all = min((int32_t)p.end - 1, own_last + (int32_t)(tile * NT * 16u / a.group));
         piece += a.prefix_splits;
     }
+    p.piece = piece;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         uint32_t at = (tile * NT + n) * 16u + i;
@@ -315,16 +431,19 @@ __global__ void __launch_bounds__(ATT_THREADS) dl_attention_kernel(const att_arg
         const uint32_t b = b0 + at / seq_rows, in = at % seq_rows, j = in / a.group, h = head * a.group + in - j * a.group;
         qrow[n] = a.q + b * a.q_seq + j * a.q_token + h * a.q_head;
         row[n] = (b * a.q_tokens + j) * a.q_heads + h;
-        last[n] = prefix ? (int32_t)end - 1 : min((int32_t)end - 1, own_last + (int32_t)j);
+        last[n] = prefix ? (int32_t)p.end - 1 : min((int32_t)p.end - 1, own_last + (int32_t)j);
     }
-    attend<Q, C, DP, NT>(a, head, table, first, end, qrow, last, row, store, piece);
+    attend<Q, C, DP, NT, ALIGNED>(a, p, qrow, last, row, store);
 }
 
-// Joins the pieces of a row, a wavefront a row.
-template <class Q>
+// Joins the pieces of a row.  WAVES wavefronts a row share them out; in a wavefront DP / 4 lanes hold a piece's sums, four
+// each, so 256 / DP pieces are looked at together and four times as many are on their way.
+template <class Q, int DP, int WAVES>
 __global__ void __launch_bounds__(ATT_THREADS) dl_attention_join_kernel(const att_args a)
 {
-    const uint32_t row = (blockIdx.x * ATT_THREADS + threadIdx.x) / 64u, lane = threadIdx.x % 64u;
+    constexpr uint32_t LANES = DP / 4, SIDE = 64 / LANES, AHEAD = 4;
+    const uint32_t lane = threadIdx.x % 64u, wave = threadIdx.x / 64u, part = lane / LANES + (WAVES > 1 ? wave * SIDE : 0u);
+    const uint32_t row = WAVES > 1 ? blockIdx.x : blockIdx.x * ATT_WAVES + wave;
     if (row >= a.rows) return;
     const uint32_t h = row % a.q_heads, bj = row / a.q_heads, b = bj / a.q_tokens, j = bj - b * a.q_tokens, D = a.c.head_dim;
     uint32_t pieces = 0;
@@ -332,31 +451,69 @@ __global__ void __launch_bounds__(ATT_THREADS) dl_attention_join_kernel(const at
         const uint32_t len = own_len(a, b), step = own_piece(a, len);
         pieces = a.prefix_splits + (len ? (len + step - 1u) / step : 0u);
     }
-    float r = -INFINITY;
-    for (uint32_t p = lane; p < pieces; p += 64u) r = fmaxf(r, a.rl[(uint64_t)p * a.rows + row][0]);
+    const uint32_t d0 = 4u * (lane % LANES);
+    float r = -INFINITY, l = 0.0f;
+    dl_f32x4 o = {0, 0, 0, 0};
+    for (uint32_t p0 = part; p0 < pieces; p0 += SIDE * WAVES * AHEAD) {
+        dl_f32x2 rl[AHEAD];
+        dl_f32x4 x[AHEAD];
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) r = fmaxf(r, __shfl_xor(r, d));
-    const float ref = r == -INFINITY ? 0.0f : r;
-    float l = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    const uint32_t d0 = 4u * lane;
-    for (uint32_t p = 0; p < pieces; ++p) {
-        const uint64_t at = (uint64_t)p * a.rows + row;
-        const dl_f32x2 rl = a.rl[at];
-        const float f = __builtin_amdgcn_exp2f(rl[0] - ref);
-        l += rl[1] * f;
-        if (d0 < D) {
-            const dl_f32x4 x = *(const dl_f32x4 *)(a.partial + at * D + d0);
+        for (uint32_t k = 0; k < AHEAD; ++k) {
+            const uint32_t p = p0 + k * SIDE * WAVES;
+            const uint64_t at = (uint64_t)min(p, pieces - 1u) * a.rows + row;
+            rl[k] = a.rl[at];
+            x[k] = d0 < D ? *(const dl_f32x4 *)(a.partial + at * D + d0) : dl_f32x4{0, 0, 0, 0};
+            if (p >= pieces) rl[k] = dl_f32x2{-INFINITY, 0.0f}, x[k] = dl_f32x4{0, 0, 0, 0};
+        }
+        float now = r;
 #pragma unroll
-            for (int t = 0; t < 4; ++t) o[t] += x[t] * f;
+        for (uint32_t k = 0; k < AHEAD; ++k) now = fmaxf(now, rl[k][0]);
+        const float ref = now == -INFINITY ? 0.0f : now, fade = __builtin_amdgcn_exp2f(r - ref);
+        r = now;
+        l *= fade;
+        o *= fade;
+#pragma unroll
+        for (uint32_t k = 0; k < AHEAD; ++k) {
+            const float f = __builtin_amdgcn_exp2f(rl[k][0] - ref);
+            l = fmaf(rl[k][1], f, l);
+            o += x[k] * f;
         }
     }
+    auto merge = [&](float r2, float l2, dl_f32x4 o2) {
+        const float now = fmaxf(r, r2), ref = now == -INFINITY ? 0.0f : now;
+        const float f = __builtin_amdgcn_exp2f(r - ref), f2 = __builtin_amdgcn_exp2f(r2 - ref);
+        r = now;
+        l = l * f + l2 * f2;
+        o = o * f + o2 * f2;
+    };
+#pragma unroll
+    for (uint32_t d = LANES; d < 64u; d *= 2) {
+        dl_f32x4 o2;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) o2[t] = __shfl_xor(o[t], (int)d);
+        merge(__shfl_xor(r, (int)d), __shfl_xor(l, (int)d), o2);
+    }
+    if constexpr (WAVES > 1) {
+        __shared__ float joined[WAVES][6][64];
+        float(*mine)[64] = joined[wave];
+        mine[0][lane] = r, mine[1][lane] = l;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) mine[2 + t][lane] = o[t];
+        __syncthreads();
+        if (wave) return;
+        for (int w = 1; w < WAVES; ++w) {
+            float(*from)[64] = joined[w];
+            merge(from[0][lane], from[1][lane], dl_f32x4{from[2][lane], from[3][lane], from[4][lane], from[5][lane]});
+        }
+    }
+    if (lane >= LANES) return;
     const bool none = l == 0.0f;
     if (d0 < D) {
         char *to = a.out + b * a.out_seq + j * a.out_token + h * a.out_head + 2u * d0;
         const float f = none ? 0.0f : 1.0f / l;
         dl_store_at(to, none ? dl_u32x2{0, 0} : dl_u32x2{Q::pack(o[0] * f, o[1] * f), Q::pack(o[2] * f, o[3] * f)});
     }
-    if (a.lse && lane == 0) a.lse[row] = none ? -INFINITY : (ref - Q::lift + log2f(l)) * 0.69314718055994530942f;
+    if (a.lse && lane == 0) a.lse[row] = none ? -INFINITY : ((r == -INFINITY ? 0.0f : r) - Q::lift + log2f(l)) * 0.69314718055994530942f;
 }
 
 uint32_t ceil_div(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); }
@@ -469,27 +626,35 @@ extern "C" int dl_prefix_attention(const dl_kv_cache *cache, const dl_prefix_att
     const uint64_t grid = shared + (uint64_t)a.c.heads * sh.own_tiles * a.batch * sh.own_splits;
     if (grid > INT32_MAX) return DL_ERR_INVALID;
     hipStream_t hs = (hipStream_t)stream;
+    // eight keys in a row lie in one page: looked up together, by the scalar unit
+    const bool aligned = cache->page_tokens % 8 == 0;
+    // a row's pieces: a wavefront's work while the rows alone fill the chip or the pieces are few
+    const bool wide = att_pieces(sh) > 16u && sh.rows < 4096u;
     dl_with_16bit(args->type, [&](auto q) {
-        if (grid)
-            dl_with_format(cache->format, [&](auto c) {
-                auto go = [&](auto dp, auto nt) {
-                    hipLaunchKernelGGL((dl_attention_kernel<decltype(q), decltype(c), decltype(dp)::value, decltype(nt)::value>), dim3((uint32_t)grid),
-                                       dim3(ATT_THREADS), 0, hs, a);
-                };
-                auto with_rows = [&](auto dp) {
+        auto with_dim = [&](auto dp) {
+            constexpr int DP = decltype(dp)::value;
+            if (grid)
+                dl_with_format(cache->format, [&](auto c) {
+                    auto go = [&](auto nt, auto al) {
+                        hipLaunchKernelGGL((dl_attention_kernel<decltype(q), decltype(c), DP, decltype(nt)::value, decltype(al)::value>), dim3((uint32_t)grid),
+                                           dim3(ATT_THREADS), 0, hs, a);
+                    };
                     if (sh.nt == 1)
-                        go(dp, std::integral_constant<int, 1>{});
+                        aligned ? go(std::integral_constant<int, 1>{}, std::true_type{}) : go(std::integral_constant<int, 1>{}, std::false_type{});
                     else
-                        go(dp, std::integral_constant<int, 2>{});
-                };
-                if (a.c.head_dim <= 64)
-                    with_rows(std::integral_constant<int, 64>{});
-                else if (a.c.head_dim <= 128)
-                    with_rows(std::integral_constant<int, 128>{});
-                else
-                    with_rows(std::integral_constant<int, 256>{});
-            });
-        hipLaunchKernelGGL((dl_attention_join_kernel<decltype(q)>), dim3(ceil_div(sh.rows, ATT_WAVES)), dim3(ATT_THREADS), 0, hs, a);
+                        aligned ? go(std::integral_constant<int, 2>{}, std::true_type{}) : go(std::integral_constant<int, 2>{}, std::false_type{});
+                });
+            if (wide)
+                hipLaunchKernelGGL((dl_attention_join_kernel<decltype(q), DP, 4>), dim3((uint32_t)sh.rows), dim3(ATT_THREADS), 0, hs, a);
+            else
+                hipLaunchKernelGGL((dl_attention_join_kernel<decltype(q), DP, 1>), dim3(ceil_div(sh.rows, ATT_WAVES)), dim3(ATT_THREADS), 0, hs, a);
+        };
+        if (a.c.head_dim <= 64)
+            with_dim(std::integral_constant<int, 64>{});
+        else if (a.c.head_dim <= 128)
+            with_dim(std::integral_constant<int, 128>{});
+        else
+            with_dim(std::integral_constant<int, 256>{});
     });
     DL_HIP(hipGetLastError());
     t_dl_last.mode = DL_MODE_ONESHOT;

@@ -65,8 +65,8 @@ struct dl_f32 {
 };
 struct dl_bf16 {
     static constexpr int size = 2;
-    // Weights of at most 1 are held as 2^lift times as much.  Floats of 16 bits lose bits below 2^-14, so there they use the
-    // whole range: what is 2^-29 of the largest weight still has all of its bits.
+    // Weights relative to a reference, at most 2^8, are held as 2^lift times as much.  Floats of 16 bits lose bits below 2^-14,
+    // so there they use the range above as well: what is 2^-21 of the reference still has all of its bits.
     static constexpr float lift = 0.0f;
     typedef dl_bf16x2 pair;
     static __device__ __forceinline__ float lo(uint32_t w) { return dl_bits<float>(w << 16); }
@@ -84,7 +84,7 @@ struct dl_bf16 {
 };
 struct dl_f16 {
     static constexpr int size = 2;
-    static constexpr float lift = 15.0f;
+    static constexpr float lift = 7.0f;
     typedef dl_f16x2 pair;
     static __device__ __forceinline__ float lo(uint32_t w) { return (float)dl_bits<dl_f16x2>(w)[0]; }
     static __device__ __forceinline__ float hi(uint32_t w) { return (float)dl_bits<dl_f16x2>(w)[1]; }
@@ -187,7 +187,8 @@ static inline void dl_with_type(int32_t type, F f)
 struct dl_cache_view {
     char *k, *v;
     float *k_scale, *v_scale;
-    int64_t page_stride, token_stride, head_stride, scale_page_stride, scale_token_stride, scale_head_stride;
+    int64_t head_stride, scale_head_stride;                                          // bytes, all of them
+    uint32_t page_stride, token_stride, scale_page_stride, scale_token_stride;
     uint32_t pages, heads, head_dim;
     dl_divider page;
 };

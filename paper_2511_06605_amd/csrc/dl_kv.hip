@@ -71,8 +71,8 @@ __device__ __forceinline__ bool place(const kv_args &a, int64_t slot, uint32_t h
         page = slot / a.c.page.d;
         in = slot - page * a.c.page.d;
     }
-    *codes = page * a.c.page_stride + in * a.c.token_stride + head * a.c.head_stride;
-    *scale = page * a.c.scale_page_stride + in * a.c.scale_token_stride + head * a.c.scale_head_stride;
+    *codes = (uint64_t)(uint32_t)page * a.c.page_stride + (uint64_t)(uint32_t)in * a.c.token_stride + head * a.c.head_stride;
+    *scale = (uint64_t)(uint32_t)page * a.c.scale_page_stride + (uint64_t)(uint32_t)in * a.c.scale_token_stride + head * a.c.scale_head_stride;
     return true;
 }
 
@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(KV_THREADS) dl_kv_write_kernel(const kv_args a
         if (!finite) w[i] = 0;
     }
     if (mine) dl_store_at((values ? a.c.v : a.c.k) + at + lane * 16u, w);
-    if (lane == 0) (values ? a.c.v_scale : a.c.k_scale)[scale_at] = finite ? most * (1.0f / C::limit) : __builtin_nanf("");
+    if (lane == 0) *(float *)((char *)(values ? a.c.v_scale : a.c.k_scale) + scale_at) = finite ? most * (1.0f / C::limit) : __builtin_nanf("");
 }
 
 template <class T, class C, int LANES>
@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(KV_THREADS) dl_kv_read_kernel(const kv_args a)
     int64_t at, scale_at;
     if (place(a, a.slots[token], head, &at, &scale_at)) {
         const dl_u32x4 w = dl_load_at<dl_u32x4>((values ? a.c.v : a.c.k) + at + lane * 16u);
-        const float scale = (values ? a.c.v_scale : a.c.k_scale)[scale_at];
+        const float scale = *(const float *)((const char *)(values ? a.c.v_scale : a.c.k_scale) + scale_at);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             float y[4];
@@ -228,12 +228,16 @@ int dl_cache_check(const dl_kv_cache *c, int sides, dl_cache_view *w)
     w->v = (char *)c->v;
     w->k_scale = c->k_scale;
     w->v_scale = c->v_scale;
-    w->page_stride = c->page_stride;
-    w->token_stride = c->token_stride;
+    if (c->page_stride < 0 || c->page_stride > UINT32_MAX || c->token_stride < 0 || c->token_stride > UINT32_MAX || c->scale_page_stride < 0 ||
+        c->scale_page_stride > UINT32_MAX / 4 || c->scale_token_stride < 0 || c->scale_token_stride > UINT32_MAX / 4)
+        return DL_ERR_INVALID;
+    if (c->head_stride < 0 || c->head_stride > 1ll << 46 || c->scale_head_stride < 0 || c->scale_head_stride > 1ll << 44) return DL_ERR_INVALID;
+    w->page_stride = (uint32_t)c->page_stride;
+    w->token_stride = (uint32_t)c->token_stride;
     w->head_stride = c->head_stride;
-    w->scale_page_stride = c->scale_page_stride;
-    w->scale_token_stride = c->scale_token_stride;
-    w->scale_head_stride = c->scale_head_stride;
+    w->scale_page_stride = (uint32_t)(4 * c->scale_page_stride);
+    w->scale_token_stride = (uint32_t)(4 * c->scale_token_stride);
+    w->scale_head_stride = 4 * c->scale_head_stride;
     w->pages = (uint32_t)c->pages;
     w->heads = (uint32_t)c->heads;
     w->head_dim = (uint32_t)c->head_dim;
