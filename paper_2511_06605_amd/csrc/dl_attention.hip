@@ -35,6 +35,7 @@ struct att_args {
     uint32_t rows;                     // batch * q_tokens * q_heads
     uint32_t prefix_tiles, prefix_splits, prefix_piece;
     uint32_t own_tiles, own_splits;
+    uint32_t narrow_shared;            // workgroups of dl_attention_kernel that have a piece of the prefix
     float scale;                       // times log2 e
 };
 
@@ -395,7 +396,7 @@ __global__ void __launch_bounds__(ATT_THREADS, DP * NT <= 128 ? 2 : 1) dl_attent
     uint32_t row[NT];
     bool store[NT];
     const uint32_t heads = a.c.heads, seq_rows = a.q_tokens * a.group;
-    const uint32_t shared = heads * a.prefix_tiles * a.prefix_splits;
+    const uint32_t shared = a.narrow_shared;
     const bool prefix = blockIdx.x < shared;
     const uint32_t x = prefix ? blockIdx.x : blockIdx.x - shared;
     const uint32_t head = x % heads, tiles = prefix ? a.prefix_tiles : a.own_tiles, tile = x / heads % tiles;
@@ -434,6 +435,259 @@ __global__ void __launch_bounds__(ATT_THREADS, DP * NT <= 128 ? 2 : 1) dl_attent
         last[n] = prefix ? (int32_t)p.end - 1 : min((int32_t)p.end - 1, own_last + (int32_t)j);
     }
     attend<Q, C, DP, NT, ALIGNED>(a, p, qrow, last, row, store);
+}
+
+// The prefix against many queries, bound by the matrix units.  A workgroup has WIDE_ROWS rows of the batch (32 NB a wavefront)
+// and walks the keys of its piece in tiles of 64, which its wavefronts share: the codes are turned into elements of Q once, on
+// their way into LDS, keys as rows and values transposed (by byte permutes while they are bytes), so that every operand of the
+// 32 x 32 x 16 products is one 16-byte read.  While a tile is worked on, the next one's codes are on their way to registers and the
+// pages of the one after it are looked up; a barrier a tile.
+//
+// Operands lie in rows of 16-byte pieces, whose places are exchanged (by an exclusive or with the row's number) so that eight
+// neighbouring lanes use all banks, in reads and in writes.
+constexpr uint32_t WIDE_KEYS = 64;
+
+template <class Q, class C, int DP, int NB>
+struct wide_tile {
+    uint32_t k[WIDE_KEYS * DP / 2];  // key, dim
+    uint32_t v[WIDE_KEYS * DP / 2];  // dim, key: of each 16 keys 0 - 3, 8 - 11, 4 - 7, 12 - 15
+    float ks[WIDE_KEYS], lu[WIDE_KEYS], iu[WIDE_KEYS];
+};
+
+template <class Q, class C, int DP, int NB>
+__global__ void __launch_bounds__(ATT_THREADS, DP * NB <= 128 ? 2 : 1) dl_attention_wide_kernel(const att_args a)
+{
+    constexpr uint32_t PIECES = DP / 8;                          // 16-byte pieces of a key's row
+    constexpr uint32_t K_LOADS = WIDE_KEYS * PIECES / ATT_THREADS;  // of 8 codes
+    constexpr uint32_t V_ITEMS = 8 * (DP / 4);                   // 8 keys (half of 16) x 4 dims
+    constexpr uint32_t V_LOADS = (V_ITEMS + ATT_THREADS - 1) / ATT_THREADS;
+    __shared__ wide_tile<Q, C, DP, NB> tiles[2];
+    __shared__ uint64_t rows_at[2][WIDE_KEYS];  // offsets of the codes' rows
+    __shared__ uint64_t alive_at[2];            // bit k: key k is one of the piece, in a page of the pool
+
+    const uint32_t lane = threadIdx.x % 64u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
+    const uint32_t i = lane % 32u, half = lane / 32u, D = a.c.head_dim;
+    const uint32_t heads = a.c.heads, seq_rows = a.q_tokens * a.group, all_rows = a.batch * seq_rows;
+    const uint32_t head = blockIdx.x % heads, piece = blockIdx.x / heads % a.prefix_splits, tile = blockIdx.x / heads / a.prefix_splits;
+    const uint32_t first = piece * a.prefix_piece, end = min(first + a.prefix_piece, a.prefix_tokens);
+    const char *const k_from = a.c.k + (int64_t)head * a.c.head_stride, *const v_from = a.c.v + (int64_t)head * a.c.head_stride;
+
+    uint32_t row[NB];
+    bool store[NB];
+    dl_u32x4 qf[NB][DP / 16];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+        uint32_t at = ((tile * ATT_WAVES + wave) * NB + n) * 32u + i;
+        store[n] = at < all_rows;
+        at = min(at, all_rows - 1u);
+        const uint32_t b = at / seq_rows, in = at - b * seq_rows, j = in / a.group, h = head * a.group + in - j * a.group;
+        const char *const q = a.q + b * a.q_seq + j * a.q_token + h * a.q_head;
+        row[n] = (b * a.q_tokens + j) * a.q_heads + h;
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s) qf[n][s] = 16u * s < D ? dl_load_at<dl_u32x4>(q + 2u * (16u * s + 8u * half)) : dl_u32x4{0, 0, 0, 0};
+    }
+
+    // a key's page: looked up by the first two wavefronts, for the keys' and the values' scales; the first hands the rows on
+    uint32_t looked_up = 0;
+    auto look_up = [&](uint32_t base) {
+        if (wave < 2) looked_up = (uint32_t)a.prefix_pages[dl_divide(min(base + lane, end - 1u), a.c.page)];
+    };
+    float scale = 0.0f;
+    bool alive = false;
+    auto hand_on = [&](uint32_t base, uint32_t to) {  // what was looked up for the tile at base
+        if (wave < 2) {
+            const uint32_t key = min(base + lane, end - 1u), in = key - dl_divide(key, a.c.page) * a.c.page.d;
+            alive = base + lane < end && looked_up < a.c.pages;
+            const uint64_t page = looked_up < a.c.pages ? looked_up : 0u;
+            if (wave == 0) {
+                rows_at[to][lane] = page * a.c.page_stride + (uint64_t)in * a.c.token_stride;
+                const unsigned long long all = __ballot(alive);
+                if (lane == 0) alive_at[to] = all;
+            }
+            scale = *(const float *)((const char *)(wave == 0 ? a.c.k_scale : a.c.v_scale) + (int64_t)head * a.c.scale_head_stride +
+                                     page * a.c.scale_page_stride + (uint64_t)in * a.c.scale_token_stride);
+        }
+    };
+    words<8> kw[K_LOADS];
+    uint32_t vw[V_LOADS][8];
+    auto load = [&](uint32_t from) {
+#pragma unroll
+        for (uint32_t x = 0; x < K_LOADS; ++x) {
+            const uint32_t at = threadIdx.x + x * ATT_THREADS, key = at / PIECES, d = at % PIECES * 8u;
+            kw[x] = d < D ? load_words<8>(k_from + rows_at[from][key] + d) : words<8>{};
+        }
+#pragma unroll
+        for (uint32_t x = 0; x < V_LOADS; ++x) {
+            const uint32_t at = threadIdx.x + x * ATT_THREADS, d = at % (DP / 4) * 4u, part = at / (DP / 4) % 8u;
+            const uint32_t key = part / 2u * 16u + part % 2u * 4u;
+#pragma unroll
+            for (uint32_t e = 0; e < 8; ++e)
+                vw[x][e] = d < D ? dl_load_at<uint32_t>(v_from + rows_at[from][key + (e & 3u) + (e >> 2) * 8u] + d) : 0u;
+        }
+    };
+    auto put = [&](uint32_t from) {  // what has been loaded, into the tile
+        wide_tile<Q, C, DP, NB> &to = tiles[from];
+        const uint64_t all = alive_at[from];
+        if (all != ~0ull) {  // what is none counts as zero
+#pragma unroll
+            for (uint32_t x = 0; x < K_LOADS; ++x)
+                if (!(all >> ((threadIdx.x + x * ATT_THREADS) / PIECES) & 1u)) kw[x] = words<8>{};
+#pragma unroll
+            for (uint32_t x = 0; x < V_LOADS; ++x) {
+                const uint32_t part = (threadIdx.x + x * ATT_THREADS) / (DP / 4) % 8u, key = part / 2u * 16u + part % 2u * 4u;
+#pragma unroll
+                for (uint32_t e = 0; e < 8; ++e)
+                    if (!(all >> (key + (e & 3u) + (e >> 2) * 8u) & 1u)) vw[x][e] = 0;
+            }
+        }
+#pragma unroll
+        for (uint32_t x = 0; x < K_LOADS; ++x) {
+            const uint32_t at = threadIdx.x + x * ATT_THREADS, key = at / PIECES, c = at % PIECES;
+            const dl_u32x2 p = C::template spread<Q>(kw[x].w[0]), q = C::template spread<Q>(kw[x].w[1]);
+            *(dl_u32x4 *)&to.k[(key * PIECES + (c ^ (key & 7u))) * 4u] = dl_u32x4{p[0], p[1], q[0], q[1]};
+        }
+#pragma unroll
+        for (uint32_t x = 0; x < V_LOADS; ++x) {
+            const uint32_t at = threadIdx.x + x * ATT_THREADS, d = at % (DP / 4) * 4u, part = at / (DP / 4) % 8u;
+            if (V_ITEMS % ATT_THREADS && at >= V_ITEMS) continue;
+            dl_u32x2 four[2][4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t w0 = vw[x][4 * h], w1 = vw[x][4 * h + 1], w2 = vw[x][4 * h + 2], w3 = vw[x][4 * h + 3];
+                const uint32_t a01 = __builtin_amdgcn_perm(w1, w0, 0x05010400u), a23 = __builtin_amdgcn_perm(w3, w2, 0x05010400u);
+                const uint32_t b01 = __builtin_amdgcn_perm(w1, w0, 0x07030602u), b23 = __builtin_amdgcn_perm(w3, w2, 0x07030602u);
+                four[h][0] = C::template spread<Q>(__builtin_amdgcn_perm(a23, a01, 0x05040100u));
+                four[h][1] = C::template spread<Q>(__builtin_amdgcn_perm(a23, a01, 0x07060302u));
+                four[h][2] = C::template spread<Q>(__builtin_amdgcn_perm(b23, b01, 0x05040100u));
+                four[h][3] = C::template spread<Q>(__builtin_amdgcn_perm(b23, b01, 0x07060302u));
+            }
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) {
+                const uint32_t r = d + j, c = part ^ ((r & 7u) ^ (r >> 3 & 3u));
+                *(dl_u32x4 *)&to.v[(r * 8u + c) * 4u] = dl_u32x4{four[0][j][0], four[0][j][1], four[1][j][0], four[1][j][1]};
+            }
+        }
+        if (wave == 0) {
+            to.ks[lane] = alive ? scale * a.scale : 0.0f;
+        } else if (wave == 1) {
+            const float u = scale < 0x1p-120f ? 0x1p-120f : scale;  // (as in attend_tile)
+            to.lu[lane] = alive ? __builtin_amdgcn_logf(u) : -INFINITY;
+            to.iu[lane] = alive ? __builtin_amdgcn_rcpf(u == u ? u : 1.0f) : 0.0f;
+        }
+    };
+
+    dl_f32x16 o[NB][DP / 32];
+    float r[NB], low[NB], l[NB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+        r[n] = -INFINITY;
+        low[n] = -Q::lift;
+        l[n] = 0.0f;
+#pragma unroll
+        for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[n][t][e] = 0.0f;
+    }
+
+    look_up(first);
+    hand_on(first, 0);
+    __syncthreads();
+    load(0);
+    look_up(first + WIDE_KEYS);
+    put(0);
+    hand_on(first + WIDE_KEYS, 1);
+    __syncthreads();
+    uint32_t now = 0;
+    for (uint32_t base = first; base < end; base += WIDE_KEYS, now ^= 1u) {
+        const bool more = base + WIDE_KEYS < end;
+        if (more) {
+            load(now ^ 1u);
+            look_up(base + 2 * WIDE_KEYS);
+        }
+        const wide_tile<Q, C, DP, NB> &in = tiles[now];
+#pragma unroll 1
+        for (uint32_t kb = 0; kb < 2; ++kb) {
+            // scores: rows of the product are keys (32 kb + 8 (e / 4) + 4 half + e % 4), its columns queries (i)
+            dl_f32x16 s[NB];
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[n][e] = 0.0f;
+            const uint32_t key = 32u * kb + i;
+#pragma unroll
+            for (uint32_t st = 0; st < DP / 16; ++st) {
+                const dl_u32x4 kf = *(const dl_u32x4 *)&in.k[(key * PIECES + ((2u * st + half) ^ (key & 7u))) * 4u];
+#pragma unroll
+                for (int n = 0; n < NB; ++n) s[n] = Q::mfma32(kf, qf[n][st], s[n]);
+            }
+            float ks[16], lu[16], iu[16];
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                const uint32_t k4 = 32u * kb + 2u * e + 4u * half;
+                const dl_f32x4 x = *(const dl_f32x4 *)&in.ks[k4], y = *(const dl_f32x4 *)&in.lu[k4], z = *(const dl_f32x4 *)&in.iu[k4];
+#pragma unroll
+                for (int f = 0; f < 4; ++f) ks[e + f] = x[f], lu[e + f] = y[f], iu[e + f] = z[f];
+            }
+            dl_u32x4 pf[NB][2];
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                float top = -INFINITY;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    s[n][e] = fmaf(s[n][e], ks[e], lu[e]);
+                    top = fmaxf(top, s[n][e]);
+                }
+                if (__any(top > r[n] + 8.0f)) {
+                    const auto swapped = __builtin_amdgcn_permlane32_swap(dl_bits<uint32_t>(top), dl_bits<uint32_t>(top), false, false);
+                    top = fmaxf(dl_bits<float>((uint32_t)swapped[0]), dl_bits<float>((uint32_t)swapped[1]));
+                    const float most = fmaxf(r[n], top), ref = most == -INFINITY ? 0.0f : most, fade = __builtin_amdgcn_exp2f(r[n] - ref);
+                    r[n] = most;
+                    low[n] = ref - Q::lift;
+                    l[n] *= fade;
+#pragma unroll
+                    for (int t = 0; t < DP / 32; ++t) o[n][t] *= fade;
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    s[n][e] = __builtin_amdgcn_exp2f(s[n][e] - low[n]);
+                    l[n] = fmaf(s[n][e], iu[e], l[n]);
+                }
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) pf[n][t][e] = Q::pack(s[n][8 * t + 2 * e], s[n][8 * t + 2 * e + 1]);
+            }
+            // sums: rows of the product are dims, its columns queries
+#pragma unroll
+            for (uint32_t t = 0; t < 2; ++t)
+#pragma unroll
+                for (uint32_t dt = 0; dt < DP / 32; ++dt) {
+                    const uint32_t d = 32u * dt + i, c = (4u * kb + 2u * t + half) ^ ((d & 7u) ^ (d >> 3 & 3u));
+                    const dl_u32x4 vf = *(const dl_u32x4 *)&in.v[(d * 8u + c) * 4u];
+#pragma unroll
+                    for (int n = 0; n < NB; ++n) o[n][dt] = Q::mfma32(vf, pf[n][t], o[n][dt]);
+                }
+        }
+        if (more) {
+            put(now ^ 1u);
+            hand_on(base + 2 * WIDE_KEYS, now);
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+        l[n] += __shfl_xor(l[n], 32);
+        if (!store[n]) continue;
+        const uint64_t at = (uint64_t)piece * a.rows + row[n];
+        if (half == 0) a.rl[at] = dl_f32x2{r[n], l[n]};
+#pragma unroll
+        for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                const uint32_t d = 32u * t + 2u * e + 4u * half;
+                if (d < D) *(dl_f32x4 *)(a.partial + at * D + d) = dl_f32x4{o[n][t][e], o[n][t][e + 1], o[n][t][e + 2], o[n][t][e + 3]};
+            }
+    }
 }
 
 // Joins the pieces of a row.  WAVES wavefronts a row share them out; in a wavefront DP / 4 lanes hold a piece's sums, four
@@ -520,6 +774,7 @@ uint32_t ceil_div(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); 
 
 struct att_shape {
     uint32_t nt;
+    uint32_t wide;  // 32-row tiles of a wavefront in the kernel for many queries on a prefix; 0: the prefix goes with the rest
     uint32_t prefix_tiles, prefix_splits, prefix_piece, own_tiles, own_splits;
     uint64_t rows;
 };
@@ -549,7 +804,8 @@ int att_setup(const dl_kv_cache *cache, const dl_prefix_attention_args *args, dl
         return (uint32_t)(wanted < most ? wanted : most);
     };
     const uint64_t prefix = cache->pages ? (uint64_t)args->prefix_tokens : 0u, own = cache->pages ? (uint64_t)args->max_pages * cache->page_tokens : 0u;
-    sh->prefix_tiles = ceil_div(all_rows, 16u * sh->nt);
+    sh->wide = all_rows >= 64u && prefix >= 256u ? 1 : 0;
+    sh->prefix_tiles = ceil_div(all_rows, sh->wide ? 32u * ATT_WAVES * sh->wide : 16u * sh->nt);
     sh->own_tiles = ceil_div(seq_rows, 16u * sh->nt);
     sh->prefix_splits = cut((uint64_t)cache->heads * sh->prefix_tiles, prefix);
     if (sh->prefix_splits) {
@@ -623,8 +879,9 @@ extern "C" int dl_prefix_attention(const dl_kv_cache *cache, const dl_prefix_att
     a.own_splits = sh.own_splits ? sh.own_splits : 1u;
     a.scale = args->scale * 1.44269504088896340736f;
     const uint64_t shared = (uint64_t)a.c.heads * sh.prefix_tiles * sh.prefix_splits;
-    const uint64_t grid = shared + (uint64_t)a.c.heads * sh.own_tiles * a.batch * sh.own_splits;
-    if (grid > INT32_MAX) return DL_ERR_INVALID;
+    const uint64_t grid = (sh.wide ? 0u : shared) + (uint64_t)a.c.heads * sh.own_tiles * a.batch * sh.own_splits;
+    if (grid > INT32_MAX || shared > INT32_MAX) return DL_ERR_INVALID;
+    a.narrow_shared = sh.wide ? 0u : (uint32_t)shared;
     hipStream_t hs = (hipStream_t)stream;
     // eight keys in a row lie in one page: looked up together, by the scalar unit
     const bool aligned = cache->page_tokens % 8 == 0;
@@ -633,6 +890,10 @@ extern "C" int dl_prefix_attention(const dl_kv_cache *cache, const dl_prefix_att
     dl_with_16bit(args->type, [&](auto q) {
         auto with_dim = [&](auto dp) {
             constexpr int DP = decltype(dp)::value;
+            if (sh.wide)
+                dl_with_format(cache->format, [&](auto c) {
+                    hipLaunchKernelGGL((dl_attention_wide_kernel<decltype(q), decltype(c), DP, 1>), dim3((uint32_t)shared), dim3(ATT_THREADS), 0, hs, a);
+                });
             if (grid)
                 dl_with_format(cache->format, [&](auto c) {
                     auto go = [&](auto nt, auto al) {
