@@ -7,6 +7,8 @@ import shutil
 import subprocess
 import sys
 import sysconfig
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -55,7 +57,12 @@ def _build_marshal(verbose) -> None:
 def build(verbose: bool = False) -> str:
     """The library, then the extension module for Python."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    _run([hipcc, *HIPCC_FLAGS, *[os.path.join(CSRC, s) for s in SOURCES], "-o", LIB], verbose)
+    with tempfile.TemporaryDirectory() as tmp:  # the sources side by side, then one link
+        objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
+        compile_flags = [f for f in HIPCC_FLAGS if f != "-shared"]
+        with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:
+            list(pool.map(lambda so: _run([hipcc, *compile_flags, "-c", os.path.join(CSRC, so[0]), "-o", so[1]], verbose), zip(SOURCES, objects)))
+        _run([hipcc, "--offload-arch=gfx950", "-fno-gpu-rdc", "-shared", "-fPIC", *objects, "-o", LIB], verbose)
     _build_marshal(verbose)
     return LIB
 

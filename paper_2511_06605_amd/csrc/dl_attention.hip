@@ -35,7 +35,7 @@ struct att_args {
     uint32_t rows;                     // batch * q_tokens * q_heads
     uint32_t prefix_tiles, prefix_splits, prefix_piece;
     uint32_t own_tiles, own_splits;
-    uint32_t narrow_shared;            // workgroups of dl_attention_kernel that have a piece of the prefix
+    uint32_t narrow_shared, wide_shared;  // workgroups with a piece of the prefix, of either kind
     float scale;                       // times log2 e
 };
 
@@ -286,16 +286,19 @@ __device__ __forceinline__ void attend_tile(const att_args &a, const piece_args 
     if (then.base < p.end) load_values<DP, ALIGNED>(a, p, then, tv);
 }
 
+template <int DP, int NT>
+struct narrow_lds {
+    float scales[ATT_WAVES][3][TILE];
+    float joined[2][NT * DP / 16 * 4 + 2 * NT][64];
+};
+
 template <class Q, class C, int DP, int NT, bool ALIGNED>
-__device__ void attend(const att_args &a, const piece_args &p, const char *const (&qrow)[NT], const int32_t (&last)[NT], const uint32_t (&row)[NT],
-                       const bool (&store)[NT])
+__device__ __forceinline__ void attend(const att_args &a, const piece_args &p, const char *const (&qrow)[NT], const int32_t (&last)[NT],
+                                       const uint32_t (&row)[NT], const bool (&store)[NT], narrow_lds<DP, NT> &lds)
 {
     constexpr int KB = DP / 4, VB = DP / 16, STEPS = DP / 32;
     const uint32_t lane = threadIdx.x % 64u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
     const uint32_t g = lane / 16u, D = a.c.head_dim;
-
-    __shared__ float scales[ATT_WAVES][3][TILE];
-    __shared__ float joined[2][NT * DP / 16 * 4 + 2 * NT][64];
 
     place<ALIGNED> at, then;
     at.look_up(a, p, p.first + wave * TILE);
@@ -330,7 +333,7 @@ __device__ void attend(const att_args &a, const piece_args &p, const char *const
         then.look_up(a, p, at.base + STEP);
         bool whole = false;
         if (ALIGNED && (int32_t)(at.base + TILE - 1u) <= p.seen_by_all) whole = !__any(at.key_page >= a.c.pages);
-        attend_tile<Q, C, DP, NT, ALIGNED>(a, p, at, then, whole, tk, tv, qf, last, acc, scales[wave]);
+        attend_tile<Q, C, DP, NT, ALIGNED>(a, p, at, then, whole, tk, tv, qf, last, acc, lds.scales[wave]);
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -341,7 +344,7 @@ __device__ void attend(const att_args &a, const piece_args &p, const char *const
 #pragma unroll
     for (uint32_t half = ATT_WAVES / 2; half; half /= 2) {
         if (wave >= half && wave < 2 * half) {
-            float(*to)[64] = joined[wave - half];
+            float(*to)[64] = lds.joined[wave - half];
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 to[2 * n][lane] = acc.r[n];
@@ -354,7 +357,7 @@ __device__ void attend(const att_args &a, const piece_args &p, const char *const
         }
         __syncthreads();
         if (wave < half) {
-            const float(*from)[64] = joined[wave];
+            const float(*from)[64] = lds.joined[wave];
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const float r2 = from[2 * n][lane], now = fmaxf(acc.r[n], r2), ref = now == -INFINITY ? 0.0f : now;
@@ -387,8 +390,9 @@ __device__ void attend(const att_args &a, const piece_args &p, const char *const
     }
 }
 
+// A workgroup's piece where few queries share it: NT * 16 rows, each wavefront every fourth tile of 32 keys.
 template <class Q, class C, int DP, int NT, bool ALIGNED>
-__global__ void __launch_bounds__(ATT_THREADS, DP * NT <= 128 ? 2 : 1) dl_attention_kernel(const att_args a)
+__device__ __forceinline__ void narrow_piece(const att_args &a, uint32_t block, narrow_lds<DP, NT> &lds)
 {
     const uint32_t i = threadIdx.x % 16u;
     const char *qrow[NT];
@@ -397,8 +401,8 @@ __global__ void __launch_bounds__(ATT_THREADS, DP * NT <= 128 ? 2 : 1) dl_attent
     bool store[NT];
     const uint32_t heads = a.c.heads, seq_rows = a.q_tokens * a.group;
     const uint32_t shared = a.narrow_shared;
-    const bool prefix = blockIdx.x < shared;
-    const uint32_t x = prefix ? blockIdx.x : blockIdx.x - shared;
+    const bool prefix = block < shared;
+    const uint32_t x = prefix ? block : block - shared;
     const uint32_t head = x % heads, tiles = prefix ? a.prefix_tiles : a.own_tiles, tile = x / heads % tiles;
     uint32_t piece = x / heads / tiles, b0 = 0, rows;
     int32_t own_last = 0;  // of query 0
@@ -434,7 +438,7 @@ __global__ void __launch_bounds__(ATT_THREADS, DP * NT <= 128 ? 2 : 1) dl_attent
         row[n] = (b * a.q_tokens + j) * a.q_heads + h;
         last[n] = prefix ? (int32_t)p.end - 1 : min((int32_t)p.end - 1, own_last + (int32_t)j);
     }
-    attend<Q, C, DP, NT, ALIGNED>(a, p, qrow, last, row, store);
+    attend<Q, C, DP, NT, ALIGNED>(a, p, qrow, last, row, store, lds);
 }
 
 // The prefix against many queries, bound by the matrix units.  A workgroup has WIDE_ROWS rows of the batch (32 NB a wavefront)
@@ -447,28 +451,33 @@ __global__ void __launch_bounds__(ATT_THREADS, DP * NT <= 128 ? 2 : 1) dl_attent
 // neighbouring lanes use all banks, in reads and in writes.
 constexpr uint32_t WIDE_KEYS = 64;
 
-template <class Q, class C, int DP, int NB>
+template <int DP>
 struct wide_tile {
     uint32_t k[WIDE_KEYS * DP / 2];  // key, dim
     uint32_t v[WIDE_KEYS * DP / 2];  // dim, key: of each 16 keys 0 - 3, 8 - 11, 4 - 7, 12 - 15
     float ks[WIDE_KEYS], lu[WIDE_KEYS], iu[WIDE_KEYS];
 };
+template <int DP>
+struct wide_lds {
+    wide_tile<DP> tiles[2];
+    uint64_t rows_at[2][WIDE_KEYS];  // offsets of the codes' rows
+    uint64_t alive_at[2];            // bit k: key k is one of the piece, in a page of the pool
+};
 
 template <class Q, class C, int DP, int NB>
-__global__ void __launch_bounds__(ATT_THREADS, DP * NB <= 128 ? 2 : 1) dl_attention_wide_kernel(const att_args a)
+__device__ __forceinline__ void wide_piece(const att_args &a, uint32_t block, wide_lds<DP> &lds)
 {
     constexpr uint32_t PIECES = DP / 8;                          // 16-byte pieces of a key's row
     constexpr uint32_t K_LOADS = WIDE_KEYS * PIECES / ATT_THREADS;  // of 8 codes
     constexpr uint32_t V_ITEMS = 8 * (DP / 4);                   // 8 keys (half of 16) x 4 dims
     constexpr uint32_t V_LOADS = (V_ITEMS + ATT_THREADS - 1) / ATT_THREADS;
-    __shared__ wide_tile<Q, C, DP, NB> tiles[2];
-    __shared__ uint64_t rows_at[2][WIDE_KEYS];  // offsets of the codes' rows
-    __shared__ uint64_t alive_at[2];            // bit k: key k is one of the piece, in a page of the pool
-
+    auto &tiles = lds.tiles;
+    auto &rows_at = lds.rows_at;
+    auto &alive_at = lds.alive_at;
     const uint32_t lane = threadIdx.x % 64u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
     const uint32_t i = lane % 32u, half = lane / 32u, D = a.c.head_dim;
     const uint32_t heads = a.c.heads, seq_rows = a.q_tokens * a.group, all_rows = a.batch * seq_rows;
-    const uint32_t head = blockIdx.x % heads, piece = blockIdx.x / heads % a.prefix_splits, tile = blockIdx.x / heads / a.prefix_splits;
+    const uint32_t head = block % heads, piece = block / heads % a.prefix_splits, tile = block / heads / a.prefix_splits;
     const uint32_t first = piece * a.prefix_piece, end = min(first + a.prefix_piece, a.prefix_tokens);
     const char *const k_from = a.c.k + (int64_t)head * a.c.head_stride, *const v_from = a.c.v + (int64_t)head * a.c.head_stride;
 
@@ -526,7 +535,7 @@ __global__ void __launch_bounds__(ATT_THREADS, DP * NB <= 128 ? 2 : 1) dl_attent
         }
     };
     auto put = [&](uint32_t from) {  // what has been loaded, into the tile
-        wide_tile<Q, C, DP, NB> &to = tiles[from];
+        wide_tile<DP> &to = tiles[from];
         const uint64_t all = alive_at[from];
         if (all != ~0ull) {  // what is none counts as zero
 #pragma unroll
@@ -604,7 +613,7 @@ __global__ void __launch_bounds__(ATT_THREADS, DP * NB <= 128 ? 2 : 1) dl_attent
             load(now ^ 1u);
             look_up(base + 2 * WIDE_KEYS);
         }
-        const wide_tile<Q, C, DP, NB> &in = tiles[now];
+        const wide_tile<DP> &in = tiles[now];
 #pragma unroll 1
         for (uint32_t kb = 0; kb < 2; ++kb) {
             // scores: rows of the product are keys (32 kb + 8 (e / 4) + 4 half + e % 4), its columns queries (i)
@@ -690,6 +699,20 @@ __global__ void __launch_bounds__(ATT_THREADS, DP * NB <= 128 ? 2 : 1) dl_attent
     }
 }
 
+// All pieces, of the prefix and of the sequences' own tokens.  WIDE: those of the prefix are wide ones (a.wide_shared workgroups).
+template <class Q, class C, int DP, int NT, bool ALIGNED, bool WIDE>
+__global__ void __launch_bounds__(ATT_THREADS, DP <= 128 ? 2 : 1) dl_attention_kernel(const att_args a)
+{
+    constexpr size_t NARROW = sizeof(narrow_lds<DP, NT>), BYTES = WIDE && sizeof(wide_lds<DP>) > NARROW ? sizeof(wide_lds<DP>) : NARROW;
+    __shared__ __align__(16) char lds[BYTES];
+    if constexpr (WIDE) {
+        if (blockIdx.x < a.wide_shared) return wide_piece<Q, C, DP, 1>(a, blockIdx.x, *(wide_lds<DP> *)lds);
+        narrow_piece<Q, C, DP, NT, ALIGNED>(a, blockIdx.x - a.wide_shared, *(narrow_lds<DP, NT> *)lds);
+    } else {
+        narrow_piece<Q, C, DP, NT, ALIGNED>(a, blockIdx.x, *(narrow_lds<DP, NT> *)lds);
+    }
+}
+
 // Joins the pieces of a row.  WAVES wavefronts a row share them out; in a wavefront DP / 4 lanes hold a piece's sums, four
 // each, so 256 / DP pieces are looked at together and four times as many are on their way.
 template <class Q, int DP, int WAVES>
@@ -772,12 +795,37 @@ __global__ void __launch_bounds__(ATT_THREADS) dl_attention_join_kernel(const at
 
 uint32_t ceil_div(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); }
 
+template <class F>
+void with_bool(bool b, F f)
+{
+    if (b)
+        f(std::true_type{});
+    else
+        f(std::false_type{});
+}
+
 struct att_shape {
     uint32_t nt;
-    uint32_t wide;  // 32-row tiles of a wavefront in the kernel for many queries on a prefix; 0: the prefix goes with the rest
+    bool wide;  // pieces of the prefix are wide ones
     uint32_t prefix_tiles, prefix_splits, prefix_piece, own_tiles, own_splits;
     uint64_t rows;
 };
+
+// In how many pieces to cut an axis of `steps`, where there are `units` such axes and room for `slots` workgroups at once: a
+// round of workgroups takes as long as the steps of one and about START more, and a piece costs the join about JOIN.
+uint32_t cut(uint64_t units, uint64_t steps, uint64_t slots)
+{
+    constexpr double START = 3.0, JOIN = 0.1;
+    if (!steps) return 0;
+    uint32_t best = 1;
+    double least = 0.0;
+    for (uint32_t n = 1; n <= 64u && n <= steps; ++n) {
+        const double rounds = (double)ceil_div(units * n, slots);
+        const double cost = rounds * ((double)ceil_div(steps, n) + START) + JOIN * n;
+        if (n == 1 || cost < least) best = n, least = cost;
+    }
+    return best;
+}
 
 // How the work is cut, from sizes alone.
 int att_setup(const dl_kv_cache *cache, const dl_prefix_attention_args *args, dl_cache_view *view, att_shape *sh)
@@ -798,21 +846,18 @@ int att_setup(const dl_kv_cache *cache, const dl_prefix_attention_args *args, dl
     const uint32_t group = (uint32_t)(args->q_heads / cache->heads), seq_rows = (uint32_t)args->q_tokens * group;
     const uint64_t all_rows = (uint64_t)args->batch * seq_rows;
     sh->nt = seq_rows > 16u ? 2 : 1;
-    auto cut = [&](uint64_t units, uint64_t keys) {  // pieces of an axis of `keys`, where there are `units` such axes
-        if (!keys) return 0u;
-        const uint64_t wanted = units >= 1024u ? 1u : (1024u + units - 1u) / units, most = (keys + STEP - 1u) / STEP;
-        return (uint32_t)(wanted < most ? wanted : most);
-    };
     const uint64_t prefix = cache->pages ? (uint64_t)args->prefix_tokens : 0u, own = cache->pages ? (uint64_t)args->max_pages * cache->page_tokens : 0u;
-    sh->wide = all_rows >= 64u && prefix >= 256u ? 1 : 0;
-    sh->prefix_tiles = ceil_div(all_rows, sh->wide ? 32u * ATT_WAVES * sh->wide : 16u * sh->nt);
+    sh->wide = all_rows >= 64u && prefix >= 256u;
+    sh->prefix_tiles = ceil_div(all_rows, sh->wide ? 32u * ATT_WAVES : 16u * sh->nt);
     sh->own_tiles = ceil_div(seq_rows, 16u * sh->nt);
-    sh->prefix_splits = cut((uint64_t)cache->heads * sh->prefix_tiles, prefix);
+    const uint32_t step = sh->wide ? WIDE_KEYS : STEP;
+    const uint32_t slots = cache->head_dim > 128 ? 256u : sh->wide || sh->nt == 2u ? 512u : 768u;  // what registers and LDS leave room for
+    sh->prefix_splits = cut((uint64_t)cache->heads * sh->prefix_tiles, ceil_div(prefix, step), slots);
     if (sh->prefix_splits) {
-        sh->prefix_piece = ceil_div(ceil_div(prefix, sh->prefix_splits), STEP) * STEP;
+        sh->prefix_piece = ceil_div(ceil_div(prefix, sh->prefix_splits), step) * step;
         sh->prefix_splits = ceil_div(prefix, sh->prefix_piece);
     }
-    sh->own_splits = cut((uint64_t)cache->heads * sh->own_tiles * (uint32_t)args->batch, own);
+    sh->own_splits = cut((uint64_t)cache->heads * sh->own_tiles * (uint32_t)args->batch, ceil_div(own, STEP), slots);
     return DL_OK;
 }
 
@@ -879,8 +924,9 @@ extern "C" int dl_prefix_attention(const dl_kv_cache *cache, const dl_prefix_att
     a.own_splits = sh.own_splits ? sh.own_splits : 1u;
     a.scale = args->scale * 1.44269504088896340736f;
     const uint64_t shared = (uint64_t)a.c.heads * sh.prefix_tiles * sh.prefix_splits;
-    const uint64_t grid = (sh.wide ? 0u : shared) + (uint64_t)a.c.heads * sh.own_tiles * a.batch * sh.own_splits;
-    if (grid > INT32_MAX || shared > INT32_MAX) return DL_ERR_INVALID;
+    const uint64_t grid = shared + (uint64_t)a.c.heads * sh.own_tiles * a.batch * sh.own_splits;
+    if (grid > INT32_MAX) return DL_ERR_INVALID;
+    a.wide_shared = sh.wide ? (uint32_t)shared : 0u;
     a.narrow_shared = sh.wide ? 0u : (uint32_t)shared;
     hipStream_t hs = (hipStream_t)stream;
     // eight keys in a row lie in one page: looked up together, by the scalar unit
@@ -890,20 +936,17 @@ extern "C" int dl_prefix_attention(const dl_kv_cache *cache, const dl_prefix_att
     dl_with_16bit(args->type, [&](auto q) {
         auto with_dim = [&](auto dp) {
             constexpr int DP = decltype(dp)::value;
-            if (sh.wide)
-                dl_with_format(cache->format, [&](auto c) {
-                    hipLaunchKernelGGL((dl_attention_wide_kernel<decltype(q), decltype(c), DP, 1>), dim3((uint32_t)shared), dim3(ATT_THREADS), 0, hs, a);
-                });
             if (grid)
                 dl_with_format(cache->format, [&](auto c) {
-                    auto go = [&](auto nt, auto al) {
-                        hipLaunchKernelGGL((dl_attention_kernel<decltype(q), decltype(c), DP, decltype(nt)::value, decltype(al)::value>), dim3((uint32_t)grid),
-                                           dim3(ATT_THREADS), 0, hs, a);
-                    };
-                    if (sh.nt == 1)
-                        aligned ? go(std::integral_constant<int, 1>{}, std::true_type{}) : go(std::integral_constant<int, 1>{}, std::false_type{});
-                    else
-                        aligned ? go(std::integral_constant<int, 2>{}, std::true_type{}) : go(std::integral_constant<int, 2>{}, std::false_type{});
+                    with_bool(aligned, [&](auto al) {
+                        with_bool(sh.wide, [&](auto wd) {
+                            with_bool(sh.nt == 2, [&](auto two) {
+                                hipLaunchKernelGGL((dl_attention_kernel<decltype(q), decltype(c), DP, decltype(two)::value ? 2 : 1, decltype(al)::value,
+                                                                        decltype(wd)::value>),
+                                                   dim3((uint32_t)grid), dim3(ATT_THREADS), 0, hs, a);
+                            });
+                        });
+                    });
                 });
             if (wide)
                 hipLaunchKernelGGL((dl_attention_join_kernel<decltype(q), DP, 4>), dim3((uint32_t)sh.rows), dim3(ATT_THREADS), 0, hs, a);
