@@ -26,25 +26,22 @@ struct att_args {
     char *out;
     float *lse;
     const int32_t *prefix_pages, *pages, *lens, *q_lens;
-    dl_f32x2 *rl;    // per piece and row: r and l
-    float *partial;  // per piece and row: head_dim sums
+    // What a piece leaves behind for the join, by part: part = piece * rows + row for a piece of the prefix, and behind those
+    // (prefix_splits * rows) + unit * (rows of a sequence) + row in it for one of a sequence's own tokens.
+    dl_f32x2 *rl;    // r and l
+    float *partial;  // head_dim sums
+    uint32_t *units; // per sequence with tokens of its own: its first unit, and how many it has
     int64_t q_seq, q_token, q_head, out_seq, out_token, out_head;  // bytes
     int64_t pages_stride;
     uint32_t prefix_tokens, own_most;  // own_most: max_pages * page_tokens
     uint32_t batch, q_tokens, q_heads, group;
     uint32_t rows;                     // batch * q_tokens * q_heads
     uint32_t prefix_tiles, prefix_splits, prefix_piece;
-    uint32_t own_tiles, own_splits;
+    uint32_t own_tiles, own_units, own_target;  // own_units: at most so many pieces of own tokens, over all sequences; own_target: see own_unit
     uint32_t narrow_shared, wide_shared;  // workgroups with a piece of the prefix, of either kind
     float scale;                       // times log2 e
 };
 
-// How a sequence's own tokens are cut: pieces of this many.
-__device__ __forceinline__ uint32_t own_piece(const att_args &a, uint32_t len)
-{
-    const uint32_t even = (len + a.own_splits - 1u) / a.own_splits;
-    return (even + STEP - 1u) / STEP * STEP;
-}
 __device__ __forceinline__ uint32_t own_len(const att_args &a, uint32_t b)
 {
     return a.own_most ? min((uint32_t)max(a.lens[b], 0), a.own_most) : 0u;
@@ -52,6 +49,62 @@ __device__ __forceinline__ uint32_t own_len(const att_args &a, uint32_t b)
 __device__ __forceinline__ uint32_t queries(const att_args &a, uint32_t b)
 {
     return a.q_lens ? min((uint32_t)max(a.q_lens[b], 0), a.q_tokens) : a.q_tokens;
+}
+
+// x + the lanes before it; lane 63 ends with the sum of all.
+__device__ __forceinline__ uint32_t sum_up_to(uint32_t x)
+{
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xF, 0xF, false);  // row_shr:1, 2, 4, 8
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xF, 0xF, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xF, 0xF, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xF, 0xF, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xA, 0xF, false);  // row_bcast:15, 31
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xC, 0xF, false);
+    return x;
+}
+
+// The sequences' own tokens are cut by their lengths, which only the device knows: into pieces of as many steps (of STEP keys)
+// as share the steps of all sequences out over own_target pieces.  Sequences are then of one or more pieces, own_target + batch
+// in all at most, and unit n is the n-th of them.  Every wavefront works this out from the lengths for itself.
+// (Batches of more than OWN_EVEN_MAX sequences have workgroups enough without: a piece a sequence.)
+constexpr uint32_t OWN_EVEN_MAX = 1024;
+constexpr uint32_t OWN_LEAST_STEPS = 2;
+
+struct own_place {
+    uint32_t b, piece, pieces, keys;  // sequence, which of its pieces, how many it has, and keys of one
+};
+// false: there is no such unit
+__device__ __forceinline__ bool own_unit(const att_args &a, uint32_t unit, own_place *at)
+{
+    auto steps_of = [&](uint32_t b) { return (own_len(a, b) + STEP - 1u) / STEP; };
+    if (a.batch > OWN_EVEN_MAX) {
+        if (unit >= a.batch || !own_len(a, unit)) return false;
+        *at = {unit, 0, 1, 1u << 31};
+        return true;
+    }
+    const uint32_t lane = threadIdx.x % 64u;
+    uint32_t all = 0, here = 0;
+    for (uint32_t b0 = 0; b0 < a.batch; b0 += 64u) {
+        here = b0 + lane < a.batch ? steps_of(b0 + lane) : 0u;
+        all += (uint32_t)__builtin_amdgcn_readlane((int)sum_up_to(here), 63);
+    }
+    const uint32_t size = max((all + a.own_target - 1u) / a.own_target, OWN_LEAST_STEPS);
+    uint32_t before = 0;
+    for (uint32_t b0 = 0; b0 < a.batch; b0 += 64u) {
+        if (a.batch > 64u) here = b0 + lane < a.batch ? steps_of(b0 + lane) : 0u;
+        const uint32_t pieces = (here + size - 1u) / size, up_to = before + sum_up_to(pieces);
+        const unsigned long long where = __ballot(up_to > unit);
+        if (where) {
+            const int l = __ffsll((long long)where) - 1;
+            at->b = b0 + (uint32_t)l;
+            at->pieces = (uint32_t)__builtin_amdgcn_readlane((int)pieces, l);
+            at->piece = unit - ((uint32_t)__builtin_amdgcn_readlane((int)up_to, l) - at->pieces);
+            at->keys = size * STEP;
+            return true;
+        }
+        before = (uint32_t)__builtin_amdgcn_readlane((int)up_to, 63);
+    }
+    return false;
 }
 
 // A vector of N bytes, N = 4, 8, 16, as words
@@ -77,7 +130,8 @@ __device__ __forceinline__ float largest_of_quarters(float x)
 // What is the same for a workgroup's whole piece: NT tiles of 16 rows against the keys first .. end - 1 of one head.
 struct piece_args {
     const int32_t *table;
-    uint32_t head, first, end, piece;
+    uint64_t part;  // of row 0
+    uint32_t head, first, end;
     int32_t seen_by_all;  // keys up to this one are seen by every row
 };
 
@@ -300,8 +354,11 @@ __device__ __forceinline__ void attend(const att_args &a, const piece_args &p, c
     const uint32_t lane = threadIdx.x % 64u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
     const uint32_t g = lane / 16u, D = a.c.head_dim;
 
-    place<ALIGNED> at, then;
+    // (pages are looked up two steps ahead: loads come back in order, so one that is issued behind the last values' would
+    // be known only once those have arrived)
+    place<ALIGNED> at, then, after;
     at.look_up(a, p, p.first + wave * TILE);
+    then.look_up(a, p, p.first + wave * TILE + STEP);
     tile_keys<DP> tk;
     tile_values<DP> tv;
     if (at.base < p.end) {
@@ -329,8 +386,8 @@ __device__ __forceinline__ void attend(const att_args &a, const piece_args &p, c
         for (int t = 0; t < DP / 16; ++t) acc.o[n][t] = dl_f32x4{0, 0, 0, 0};
     }
 
-    for (; at.base < p.end; at = then) {
-        then.look_up(a, p, at.base + STEP);
+    for (; at.base < p.end; at = then, then = after) {
+        after.look_up(a, p, at.base + 2 * STEP);
         bool whole = false;
         if (ALIGNED && (int32_t)(at.base + TILE - 1u) <= p.seen_by_all) whole = !__any(at.key_page >= a.c.pages);
         attend_tile<Q, C, DP, NT, ALIGNED>(a, p, at, then, whole, tk, tv, qf, last, acc, lds.scales[wave]);
@@ -376,7 +433,7 @@ __device__ __forceinline__ void attend(const att_args &a, const piece_args &p, c
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         if (!store[n]) continue;
-        const uint64_t at = (uint64_t)p.piece * a.rows + row[n];
+        const uint64_t at = p.part + row[n];
         if (g == 0) a.rl[at] = dl_f32x2{acc.r[n], acc.l[n]};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -400,34 +457,41 @@ __device__ __forceinline__ void narrow_piece(const att_args &a, uint32_t block, 
     uint32_t row[NT];
     bool store[NT];
     const uint32_t heads = a.c.heads, seq_rows = a.q_tokens * a.group;
-    const uint32_t shared = a.narrow_shared;
-    const bool prefix = block < shared;
-    const uint32_t x = prefix ? block : block - shared;
-    const uint32_t head = x % heads, tiles = prefix ? a.prefix_tiles : a.own_tiles, tile = x / heads % tiles;
-    uint32_t piece = x / heads / tiles, b0 = 0, rows;
+    // Workgroups go to the eight XCDs in turn.  All heads of a piece go to the same one, next to each other: the heads' rows of
+    // a token share lines of scales and lie in other channels of its L2.
+    const bool prefix = block < a.narrow_shared;
+    const uint32_t x = prefix ? block : block - a.narrow_shared;
+    const uint32_t tiles = prefix ? a.prefix_tiles : a.own_tiles, inner = x / 8u % (tiles * heads), unit = x / 8u / (tiles * heads) * 8u + x % 8u;
+    const uint32_t tile = inner % tiles, head = inner / tiles;
+    uint32_t b0 = 0, rows;
     int32_t own_last = 0;  // of query 0
     piece_args p;
     p.head = head;
     if (prefix) {
-        p.first = piece * a.prefix_piece;
+        if (unit >= a.prefix_splits) return;
+        p.first = unit * a.prefix_piece;
         p.end = min(p.first + a.prefix_piece, a.prefix_tokens);
         p.table = a.prefix_pages;
         p.seen_by_all = (int32_t)p.end - 1;
+        p.part = (uint64_t)unit * a.rows;
         rows = a.batch * seq_rows;
     } else {
-        b0 = piece % a.batch;
-        piece /= a.batch;
-        const uint32_t len = own_len(a, b0), step = own_piece(a, len);
-        p.first = piece * step;
-        if (p.first >= len) return;
-        p.end = min(p.first + step, len);
+        own_place own;
+        if (unit >= a.own_units || !own_unit(a, unit, &own)) return;
+        b0 = own.b;
+        const uint32_t len = own_len(a, b0);
+        p.first = own.piece * own.keys;
+        p.end = min(p.first + own.keys, len);
         p.table = a.pages + b0 * a.pages_stride;
+        p.part = (uint64_t)a.prefix_splits * a.rows + (uint64_t)unit * (a.q_tokens * a.q_heads);
         rows = seq_rows;
         own_last = (int32_t)len - (int32_t)queries(a, b0);
         p.seen_by_all = min((int32_t)p.end - 1, own_last + (int32_t)(tile * NT * 16u / a.group));
-        piece += a.prefix_splits;
+        if (inner == 0 && own.piece == 0 && threadIdx.x == 0) {
+            a.units[2 * b0] = unit;
+            a.units[2 * b0 + 1] = own.pieces;
+        }
     }
-    p.piece = piece;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         uint32_t at = (tile * NT + n) * 16u + i;
@@ -435,7 +499,7 @@ __device__ __forceinline__ void narrow_piece(const att_args &a, uint32_t block, 
         at = min(at, rows - 1u);
         const uint32_t b = b0 + at / seq_rows, in = at % seq_rows, j = in / a.group, h = head * a.group + in - j * a.group;
         qrow[n] = a.q + b * a.q_seq + j * a.q_token + h * a.q_head;
-        row[n] = (b * a.q_tokens + j) * a.q_heads + h;
+        row[n] = ((b - b0) * a.q_tokens + j) * a.q_heads + h;
         last[n] = prefix ? (int32_t)p.end - 1 : min((int32_t)p.end - 1, own_last + (int32_t)j);
     }
     attend<Q, C, DP, NT, ALIGNED>(a, p, qrow, last, row, store, lds);
@@ -724,9 +788,14 @@ __global__ void __launch_bounds__(ATT_THREADS) dl_attention_join_kernel(const at
     if (row >= a.rows) return;
     const uint32_t h = row % a.q_heads, bj = row / a.q_heads, b = bj / a.q_tokens, j = bj - b * a.q_tokens, D = a.c.head_dim;
     uint32_t pieces = 0;
+    uint64_t own_part = 0;  // that of the first piece of own tokens, less prefix_splits pieces
     if (j < queries(a, b)) {
-        const uint32_t len = own_len(a, b), step = own_piece(a, len);
-        pieces = a.prefix_splits + (len ? (len + step - 1u) / step : 0u);
+        pieces = a.prefix_splits;
+        if (own_len(a, b)) {
+            own_part = (uint64_t)a.prefix_splits * a.rows + (row - b * a.q_tokens * a.q_heads) +
+                       ((uint64_t)a.units[2 * b] - a.prefix_splits) * (a.q_tokens * a.q_heads);
+            pieces += a.units[2 * b + 1];
+        }
     }
     const uint32_t d0 = 4u * (lane % LANES);
     float r = -INFINITY, l = 0.0f;
@@ -736,8 +805,8 @@ __global__ void __launch_bounds__(ATT_THREADS) dl_attention_join_kernel(const at
         dl_f32x4 x[AHEAD];
 #pragma unroll
         for (uint32_t k = 0; k < AHEAD; ++k) {
-            const uint32_t p = p0 + k * SIDE * WAVES;
-            const uint64_t at = (uint64_t)min(p, pieces - 1u) * a.rows + row;
+            const uint32_t p = p0 + k * SIDE * WAVES, q = min(p, pieces - 1u);
+            const uint64_t at = q < a.prefix_splits ? (uint64_t)q * a.rows + row : own_part + (uint64_t)q * (a.q_tokens * a.q_heads);
             rl[k] = a.rl[at];
             x[k] = d0 < D ? *(const dl_f32x4 *)(a.partial + at * D + d0) : dl_f32x4{0, 0, 0, 0};
             if (p >= pieces) rl[k] = dl_f32x2{-INFINITY, 0.0f}, x[k] = dl_f32x4{0, 0, 0, 0};
@@ -807,7 +876,7 @@ void with_bool(bool b, F f)
 struct att_shape {
     uint32_t nt;
     bool wide;  // pieces of the prefix are wide ones
-    uint32_t prefix_tiles, prefix_splits, prefix_piece, own_tiles, own_splits;
+    uint32_t prefix_tiles, prefix_splits, prefix_piece, own_tiles, own_units, own_target;
     uint64_t rows;
 };
 
@@ -857,11 +926,21 @@ int att_setup(const dl_kv_cache *cache, const dl_prefix_attention_args *args, dl
         sh->prefix_piece = ceil_div(ceil_div(prefix, sh->prefix_splits), step) * step;
         sh->prefix_splits = ceil_div(prefix, sh->prefix_piece);
     }
-    sh->own_splits = cut((uint64_t)cache->heads * sh->own_tiles * (uint32_t)args->batch, ceil_div(own, STEP), slots);
+    if (own) {
+        // Own tokens: as many pieces as make one round of workgroups; where the sequences alone are more than half of that, pieces of a
+        // quarter of a round's share, which even out what the lengths do not.
+        const uint32_t batch = (uint32_t)args->batch, round = slots / (uint32_t)cache->heads / sh->own_tiles;
+        sh->own_target = round > 2u * batch ? round - batch : round ? 4u * round : 1u;
+        const uint64_t most = (uint64_t)batch * ceil_div(own, STEP * OWN_LEAST_STEPS);  // no piece is smaller, but a sequence's last
+        sh->own_units = batch > OWN_EVEN_MAX ? batch : (uint32_t)((uint64_t)sh->own_target + batch < most ? sh->own_target + batch : most);
+    }
     return DL_OK;
 }
 
-uint64_t att_pieces(const att_shape &sh) { return (uint64_t)sh.prefix_splits + sh.own_splits; }
+// Parts that the pieces leave behind.
+uint64_t att_parts(const att_shape &sh, uint32_t batch) { return sh.rows * sh.prefix_splits + sh.rows / (batch ? batch : 1u) * sh.own_units; }
+// Where things lie in the workspace, behind the control words.
+constexpr size_t align16(uint64_t n) { return (n + 15u) / 16u * 16u; }
 
 }  // namespace
 
@@ -871,8 +950,8 @@ extern "C" int64_t dl_prefix_attention_workspace(const dl_kv_cache *cache, const
     att_shape sh;
     const int rc = att_setup(cache, args, &view, &sh);
     if (rc != DL_OK) return rc;
-    const uint64_t at = att_pieces(sh) * sh.rows;
-    return (int64_t)(DL_CONTROL_BYTES + (at * sizeof(dl_f32x2) + 15u) / 16u * 16u + at * view.head_dim * sizeof(float));
+    const uint64_t parts = att_parts(sh, (uint32_t)args->batch);
+    return (int64_t)(DL_CONTROL_BYTES + align16(8ull * (uint32_t)args->batch) + align16(parts * sizeof(dl_f32x2)) + parts * view.head_dim * sizeof(float));
 }
 
 extern "C" int dl_prefix_attention(const dl_kv_cache *cache, const dl_prefix_attention_args *args, void *stream)
@@ -901,8 +980,9 @@ extern "C" int dl_prefix_attention(const dl_kv_cache *cache, const dl_prefix_att
     a.pages = args->pages;
     a.lens = args->lens;
     a.q_lens = args->q_lens;
-    a.rl = (dl_f32x2 *)((char *)args->workspace + DL_CONTROL_BYTES);
-    a.partial = (float *)((char *)a.rl + (att_pieces(sh) * sh.rows * sizeof(dl_f32x2) + 15u) / 16u * 16u);
+    a.units = (uint32_t *)((char *)args->workspace + DL_CONTROL_BYTES);
+    a.rl = (dl_f32x2 *)((char *)a.units + align16(8ull * (uint32_t)args->batch));
+    a.partial = (float *)((char *)a.rl + align16(att_parts(sh, (uint32_t)args->batch) * sizeof(dl_f32x2)));
     a.q_seq = 2 * args->q_seq_stride;
     a.q_token = 2 * args->q_token_stride;
     a.q_head = 2 * args->q_head_stride;
@@ -921,10 +1001,11 @@ extern "C" int dl_prefix_attention(const dl_kv_cache *cache, const dl_prefix_att
     a.prefix_splits = sh.prefix_splits;
     a.prefix_piece = sh.prefix_piece;
     a.own_tiles = sh.own_tiles;
-    a.own_splits = sh.own_splits ? sh.own_splits : 1u;
+    a.own_units = sh.own_units;
+    a.own_target = sh.own_target;
     a.scale = args->scale * 1.44269504088896340736f;
-    const uint64_t shared = (uint64_t)a.c.heads * sh.prefix_tiles * sh.prefix_splits;
-    const uint64_t grid = shared + (uint64_t)a.c.heads * sh.own_tiles * a.batch * sh.own_splits;
+    const uint64_t shared = (uint64_t)a.c.heads * sh.prefix_tiles * (sh.wide ? sh.prefix_splits : (sh.prefix_splits + 7u) / 8u * 8u);
+    const uint64_t grid = shared + (uint64_t)a.c.heads * sh.own_tiles * ceil_div(sh.own_units, 8) * 8u;
     if (grid > INT32_MAX) return DL_ERR_INVALID;
     a.wide_shared = sh.wide ? (uint32_t)shared : 0u;
     a.narrow_shared = sh.wide ? 0u : (uint32_t)shared;
@@ -932,7 +1013,7 @@ extern "C" int dl_prefix_attention(const dl_kv_cache *cache, const dl_prefix_att
     // eight keys in a row lie in one page: looked up together, by the scalar unit
     const bool aligned = cache->page_tokens % 8 == 0;
     // a row's pieces: a wavefront's work while the rows alone fill the chip or the pieces are few
-    const bool wide = att_pieces(sh) > 16u && sh.rows < 4096u;
+    const bool wide = sh.prefix_splits + sh.own_units / a.batch > 16u && sh.rows < 4096u;
     dl_with_16bit(args->type, [&](auto q) {
         auto with_dim = [&](auto dp) {
             constexpr int DP = decltype(dp)::value;
