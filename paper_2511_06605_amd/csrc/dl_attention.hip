@@ -117,7 +117,6 @@ __device__ __forceinline__ words<N> load_words(const char *p)
 {
     return dl_load_at<words<N>>(p);
 }
-
 // The largest over the lanes that hold the same query (16 and 32 apart), in all of them: halves and quarters change places.
 __device__ __forceinline__ float largest_of_quarters(float x)
 {
@@ -169,7 +168,7 @@ struct place {
 
 template <int DP>
 struct tile_keys {
-    words<16> k[2][DP / 64];  // dims DP / 4 * g ..
+    words<16> k[2][DP / 64];  // dims 64 s + 16 g ..
     float scale;
 };
 template <int DP>
@@ -181,9 +180,8 @@ struct tile_values {
 template <int DP, bool ALIGNED>
 __device__ __forceinline__ void load_keys(const att_args &a, const piece_args &p, const place<ALIGNED> &at, tile_keys<DP> &td)
 {
-    constexpr int KB = DP / 4;
     const uint32_t lane = threadIdx.x % 64u, i = lane % 16u, g = lane / 16u, D = a.c.head_dim;
-    const uint64_t from = (uint64_t)a.c.k + (uint64_t)p.head * a.c.head_stride + KB * g;
+    const uint64_t from = (uint64_t)a.c.k + (uint64_t)p.head * a.c.head_stride + 16u * g;
     bool alive;
     uint64_t kp = 0;
 #pragma unroll
@@ -193,7 +191,7 @@ __device__ __forceinline__ void load_keys(const att_args &a, const piece_args &p
         else
             kp += 4ull * a.c.token_stride;
 #pragma unroll
-        for (int s = 0; s < KB / 16; ++s) td.k[t][s] = KB * g + 16u * s < D ? load_words<16>((const char *)kp + 16 * s) : words<16>{};
+        for (int s = 0; s < DP / 64; ++s) td.k[t][s] = 16u * g + 64u * s < D ? load_words<16>((const char *)kp + 64 * s) : words<16>{};
     }
     const uint64_t scales = (uint64_t)(i < 8u ? a.c.k_scale : a.c.v_scale) + (uint64_t)p.head * a.c.scale_head_stride;
     td.scale = *(const float *)at.offset(a, p, g, i % 8u, at.value_page, a.c.scale_page_stride, a.c.scale_token_stride, scales, &alive);
@@ -350,7 +348,7 @@ template <class Q, class C, int DP, int NT, bool ALIGNED>
 __device__ __forceinline__ void attend(const att_args &a, const piece_args &p, const char *const (&qrow)[NT], const int32_t (&last)[NT],
                                        const uint32_t (&row)[NT], const bool (&store)[NT], narrow_lds<DP, NT> &lds)
 {
-    constexpr int KB = DP / 4, VB = DP / 16, STEPS = DP / 32;
+    constexpr int VB = DP / 16, STEPS = DP / 32;
     const uint32_t lane = threadIdx.x % 64u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
     const uint32_t g = lane / 16u, D = a.c.head_dim;
 
@@ -366,13 +364,13 @@ __device__ __forceinline__ void attend(const att_args &a, const piece_args &p, c
         load_values<DP, ALIGNED>(a, p, at, tv);
     }
 
-    // queries: lane (i, g) holds dims KB * g .. of row i, eight a step
+    // queries: lane (i, g) holds dims 64 s + 16 g .. of row i, eight a step
     dl_u32x4 qf[NT][STEPS];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
-            const uint32_t d = KB * g + 8u * s;
+            const uint32_t d = 64u * (s / 2u) + 16u * g + 8u * (s % 2u);
             qf[n][s] = d < D ? dl_load_at<dl_u32x4>(qrow[n] + 2u * d) : dl_u32x4{0, 0, 0, 0};
         }
 
@@ -927,10 +925,10 @@ int att_setup(const dl_kv_cache *cache, const dl_prefix_attention_args *args, dl
         sh->prefix_splits = ceil_div(prefix, sh->prefix_piece);
     }
     if (own) {
-        // Own tokens: as many pieces as make one round of workgroups; where the sequences alone are more than half of that, pieces of a
-        // quarter of a round's share, which even out what the lengths do not.
+        // Own tokens: pieces for two rounds of workgroups; where the sequences alone are a round, of a quarter of a round's share,
+        // which even out what the lengths do not.
         const uint32_t batch = (uint32_t)args->batch, round = slots / (uint32_t)cache->heads / sh->own_tiles;
-        sh->own_target = round > 2u * batch ? round - batch : round ? 4u * round : 1u;
+        sh->own_target = round > batch ? 2u * round - batch : round ? 4u * round : 1u;
         const uint64_t most = (uint64_t)batch * ceil_div(own, STEP * OWN_LEAST_STEPS);  // no piece is smaller, but a sequence's last
         sh->own_units = batch > OWN_EVEN_MAX ? batch : (uint32_t)((uint64_t)sh->own_target + batch < most ? sh->own_target + batch : most);
     }

@@ -132,9 +132,12 @@ struct dl_int8 {
     static constexpr float limit = 127.0f;
     static __device__ __forceinline__ uint32_t code4(float a, float b, float c, float d)
     {
-        const uint32_t p = (uint32_t)(int)rintf(a) & 0xFFu, q = (uint32_t)(int)rintf(b) & 0xFFu;
-        const uint32_t r = (uint32_t)(int)rintf(c) & 0xFFu, s = (uint32_t)(int)rintf(d);
-        return p | q << 8 | r << 16 | s << 24;
+        // 1.5 * 2^23 + x is x rounded to a whole number, ties to even, in the low bits (the sums are kept apart from the products
+        // that x comes from: one rounding each)
+        asm("" : "+v"(a), "+v"(b), "+v"(c), "+v"(d));
+        const uint32_t p = dl_bits<uint32_t>(a + 12582912.0f), q = dl_bits<uint32_t>(b + 12582912.0f);
+        const uint32_t r = dl_bits<uint32_t>(c + 12582912.0f), s = dl_bits<uint32_t>(d + 12582912.0f);
+        return __builtin_amdgcn_perm(__builtin_amdgcn_perm(s, r, 0x0C0C0400u), __builtin_amdgcn_perm(q, p, 0x0C0C0400u), 0x05040100u);
     }
     static __device__ __forceinline__ void value4(uint32_t w, float (&x)[4])
     {

@@ -2,7 +2,7 @@
 //
 // A row (the head_dim elements of one token and head) becomes codes x * ((1 / a) * LIMIT), a = max(max |x|, 2^-100), and a scale
 // a * (1 / LIMIT).  The largest magnitude is needed before the first code, so a row is held in registers from its load to
-// its store: 16 elements a lane, as many lanes as that takes (the next power of two) side by side, and the maximum by
+// its store, as many lanes as that takes (the next power of two) side by side, and the maximum by
 // swaps among them.  One pass over the data either way; memory is what bounds it.
 #include "dl_codes.h"
 #include "dl_internal.h"
@@ -21,20 +21,20 @@ struct kv_args {
     int32_t shift;  // log2 of the tokens of a page, or -1
 };
 
-// 16 elements of a row as floats
-template <class T>
-__device__ __forceinline__ void load16(const char *p, float (&x)[16])
+// N elements of a row as floats
+template <class T, int N>
+__device__ __forceinline__ void load_row(const char *p, float (&x)[N])
 {
     if constexpr (T::size == 4) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < N / 4; ++i) {
             const dl_f32x4 w = dl_load_at<dl_f32x4>(p + 16 * i);
 #pragma unroll
             for (int j = 0; j < 4; ++j) x[4 * i + j] = w[j];
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < N / 8; ++i) {
             const dl_u32x4 w = dl_load_at<dl_u32x4>(p + 16 * i);
 #pragma unroll
             for (int j = 0; j < 4; ++j) x[8 * i + 2 * j] = T::lo(w[j]), x[8 * i + 2 * j + 1] = T::hi(w[j]);
@@ -42,19 +42,30 @@ __device__ __forceinline__ void load16(const char *p, float (&x)[16])
     }
 }
 
-template <class T>
-__device__ __forceinline__ void store16(char *p, const float (&x)[16])
+// STREAM: past the caches
+template <bool STREAM, class V>
+__device__ __forceinline__ void put(char *p, V v)
+{
+    typedef V anywhere __attribute__((aligned(1)));
+    if constexpr (STREAM)
+        __builtin_nontemporal_store(v, (anywhere *)p);
+    else
+        dl_store_at(p, v);
+}
+
+template <class T, bool STREAM, int N>
+__device__ __forceinline__ void store_row(char *p, const float (&x)[N])
 {
     if constexpr (T::size == 4) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) dl_store_at(p + 16 * i, dl_f32x4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]});
+        for (int i = 0; i < N / 4; ++i) put<STREAM>(p + 16 * i, dl_f32x4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]});
     } else {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < N / 8; ++i) {
             dl_u32x4 w;
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[j] = T::pack(x[8 * i + 2 * j], x[8 * i + 2 * j + 1]);
-            dl_store_at(p + 16 * i, w);
+            put<STREAM>(p + 16 * i, w);
         }
     }
 }
@@ -77,85 +88,120 @@ __device__ __forceinline__ bool place(const kv_args &a, int64_t slot, uint32_t h
 }
 
 constexpr uint32_t KV_THREADS = 256;
+// Elements a lane: its store is then 16 bytes, next to its neighbours' (16-bit rows; a store that lies 16 bytes from the next
+// one leaves half-written lines, which cost the read of 16384 tokens of 8 x 128 more than half: 16.6 : 29.7 us).
+constexpr int WRITE_ELEMENTS = 16, READ_ELEMENTS = 8;
+// Requests of more than two rounds of workgroups: two rows of a lane on their way at once, and stores past the caches, which would
+// not hold the result anyway.  Plain stores and one row : this, three sets of buffers in turn, write of 20001 tokens (8 x 128, float16 to
+// int8) 25.6 : 21.7 us, read of 16384 (fp8 to bfloat16) 25.2 : 16.6; four rows 23.4 and 17.0.  Smaller requests stay in the caches, for
+// the attention that follows.
+constexpr uint64_t KV_MANY_THREADS = 1ull << 20;
 
-// blockIdx.y: 0 keys, 1 values (a launch for one side alone has one of them).  LANES a row.
-template <class T, class C, int LANES>
+// blockIdx.y: 0 keys, 1 values (a launch for one side alone has one of them).  LANES a row; MANY: two rows of a thread, both on their way before
+// the first is looked at (a row's chain is its slot, then, where codes are read, the codes, then the store).
+template <class T, class C, int LANES, bool MANY>
 __global__ void __launch_bounds__(KV_THREADS) dl_kv_write_kernel(const kv_args a)
 {
+    constexpr int ROWS = MANY ? 2 : 1, N = WRITE_ELEMENTS;
     const bool values = blockIdx.y != 0 || !a.k;
-    const uint32_t lane = threadIdx.x % LANES;
-    const uint32_t row = (uint32_t)(((uint64_t)blockIdx.x * KV_THREADS + threadIdx.x) / LANES);
-    if (row >= a.rows) return;  // all lanes of a row together
-    const uint32_t token = dl_divide(row, a.heads), head = row - token * a.heads.d;
-    const char *const from = values ? a.v + token * a.v_token + head * a.v_head : a.k + token * a.k_token + head * a.k_head;
-    const int64_t slot = a.slots[token];
-    const bool mine = lane * 16u < a.c.head_dim;
-    float x[16];
+    const uint32_t lane = threadIdx.x % LANES, row0 = blockIdx.x * (KV_THREADS / LANES * ROWS) + threadIdx.x / LANES;
+    const bool mine = lane * (uint32_t)N < a.c.head_dim;
+    float x[ROWS][N];
+    int64_t slot[ROWS];
+    uint32_t head[ROWS];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = 0.0f;
-    if (mine) load16<T>(from + (size_t)lane * 16 * T::size, x);
-    // magnitudes as whole numbers: there infinities and NaN lie above all that is finite
-    uint32_t top = 0;
+    for (int r = 0; r < ROWS; ++r) {
+        const uint32_t row = min(row0 + r * (KV_THREADS / LANES), a.rows - 1u), token = dl_divide(row, a.heads);
+        head[r] = row - token * a.heads.d;
+        const char *const from = values ? a.v + token * a.v_token + head[r] * a.v_head : a.k + token * a.k_token + head[r] * a.k_head;
+        slot[r] = a.slots[token];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) top = max(top, dl_bits<uint32_t>(x[i]) & 0x7FFFFFFFu);
-#pragma unroll
-    for (int d = 1; d < LANES; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d));
-    int64_t at, scale_at;
-    if (!place(a, slot, head, &at, &scale_at)) return;
-    const bool finite = top < 0x7F800000u;
-    const float most = fmaxf(dl_bits<float>(top), 0x1p-100f);
-    const float factor = 1.0f / most * C::limit;
-    dl_u32x4 w;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        w[i] = C::code4(x[4 * i] * factor, x[4 * i + 1] * factor, x[4 * i + 2] * factor, x[4 * i + 3] * factor);
-        if (!finite) w[i] = 0;
+        for (int i = 0; i < N; ++i) x[r][i] = 0.0f;
+        if (mine) load_row<T>(from + (size_t)lane * N * T::size, x[r]);
     }
-    if (mine) dl_store_at((values ? a.c.v : a.c.k) + at + lane * 16u, w);
-    if (lane == 0) *(float *)((char *)(values ? a.c.v_scale : a.c.k_scale) + scale_at) = finite ? most * (1.0f / C::limit) : __builtin_nanf("");
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        if (row0 + r * (KV_THREADS / LANES) >= a.rows) return;  // all lanes of a row together
+        // magnitudes as whole numbers: there infinities and NaN lie above all that is finite
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) top = max(top, dl_bits<uint32_t>(x[r][i]) & 0x7FFFFFFFu);
+#pragma unroll
+        for (int d = 1; d < LANES; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+        int64_t at, scale_at;
+        if (!place(a, slot[r], head[r], &at, &scale_at)) continue;
+        const bool finite = top < 0x7F800000u;
+        const float most = fmaxf(dl_bits<float>(top), 0x1p-100f);
+        const float factor = 1.0f / most * C::limit;
+        dl_u32x4 w;
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) {
+            w[i] = C::code4(x[r][4 * i] * factor, x[r][4 * i + 1] * factor, x[r][4 * i + 2] * factor, x[r][4 * i + 3] * factor);
+            if (!finite) w[i] = 0;
+        }
+        if (mine) put<MANY>((values ? a.c.v : a.c.k) + at + lane * (uint32_t)N, w);
+        if (lane == 0) *(float *)((char *)(values ? a.c.v_scale : a.c.k_scale) + scale_at) = finite ? most * (1.0f / C::limit) : __builtin_nanf("");
+    }
 }
 
-template <class T, class C, int LANES>
+template <class T, class C, int LANES, bool MANY>
 __global__ void __launch_bounds__(KV_THREADS) dl_kv_read_kernel(const kv_args a)
 {
+    constexpr int ROWS = MANY ? 2 : 1, N = READ_ELEMENTS;
     const bool values = blockIdx.y != 0 || !a.k;
-    const uint32_t lane = threadIdx.x % LANES;
-    const uint32_t row = (uint32_t)(((uint64_t)blockIdx.x * KV_THREADS + threadIdx.x) / LANES);
-    if (row >= a.rows || lane * 16u >= a.c.head_dim) return;
-    const uint32_t token = dl_divide(row, a.heads), head = row - token * a.heads.d;
-    char *const to = values ? a.v + token * a.v_token + head * a.v_head : a.k + token * a.k_token + head * a.k_head;
-    float x[16];
-    int64_t at, scale_at;
-    if (place(a, a.slots[token], head, &at, &scale_at)) {
-        const dl_u32x4 w = dl_load_at<dl_u32x4>((values ? a.c.v : a.c.k) + at + lane * 16u);
-        const float scale = *(const float *)((const char *)(values ? a.c.v_scale : a.c.k_scale) + scale_at);
+    const uint32_t lane = threadIdx.x % LANES, row0 = blockIdx.x * (KV_THREADS / LANES * ROWS) + threadIdx.x / LANES;
+    if (lane * (uint32_t)N >= a.c.head_dim) return;
+    dl_u32x2 w[ROWS];
+    float scale[ROWS];
+    uint32_t token[ROWS], head[ROWS];
+    int64_t slot[ROWS];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float y[4];
-            C::value4(w[i], y);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[4 * i + j] = y[j] * scale;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = 0.0f;
+    for (int r = 0; r < ROWS; ++r) {
+        const uint32_t row = min(row0 + r * (KV_THREADS / LANES), a.rows - 1u);
+        token[r] = dl_divide(row, a.heads);
+        head[r] = row - token[r] * a.heads.d;
+        slot[r] = a.slots[token[r]];
     }
-    store16<T>(to + (size_t)lane * 16 * T::size, x);
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        int64_t at, scale_at;
+        w[r] = dl_u32x2{0, 0};
+        scale[r] = 0.0f;
+        if (place(a, slot[r], head[r], &at, &scale_at)) {
+            w[r] = dl_load_at<dl_u32x2>((values ? a.c.v : a.c.k) + at + lane * (uint32_t)N);
+            scale[r] = *(const float *)((const char *)(values ? a.c.v_scale : a.c.k_scale) + scale_at);
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        if (row0 + r * (KV_THREADS / LANES) >= a.rows) return;
+        char *const to = values ? a.v + token[r] * a.v_token + head[r] * a.v_head : a.k + token[r] * a.k_token + head[r] * a.k_head;
+        float x[N];
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) {
+            float y[4];
+            C::value4(w[r][i], y);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[4 * i + j] = y[j] * scale[r];
+        }
+        store_row<T, MANY>(to + (size_t)lane * N * T::size, x);
+    }
 }
 
-template <class F>
+// The lanes that a row takes, a power of two.
+template <int N, class F>
 void with_lanes(uint32_t head_dim, F f)
 {
     if (head_dim <= 16)
-        f(std::integral_constant<int, 1>{});
+        f(std::integral_constant<int, 16 / N>{});
     else if (head_dim <= 32)
-        f(std::integral_constant<int, 2>{});
+        f(std::integral_constant<int, 32 / N>{});
     else if (head_dim <= 64)
-        f(std::integral_constant<int, 4>{});
+        f(std::integral_constant<int, 64 / N>{});
     else if (head_dim <= 128)
-        f(std::integral_constant<int, 8>{});
+        f(std::integral_constant<int, 128 / N>{});
     else
-        f(std::integral_constant<int, 16>{});
+        f(std::integral_constant<int, 256 / N>{});
 }
 
 int kv_setup(const dl_kv_cache *cache, const dl_kv_rows *rows, kv_args *a, bool *nothing)
@@ -199,14 +245,21 @@ int kv_run(const dl_kv_cache *cache, const dl_kv_rows *rows, void *stream)
     if (rc != DL_OK || nothing) return rc;
     dl_with_type(rows->type, [&](auto t) {
         dl_with_format(cache->format, [&](auto c) {
-            with_lanes(a.c.head_dim, [&](auto lanes) {
+            with_lanes<WRITE ? WRITE_ELEMENTS : READ_ELEMENTS>(a.c.head_dim, [&](auto lanes) {
                 constexpr int L = decltype(lanes)::value;
-                const uint64_t threads = (uint64_t)a.rows * L;
-                const dim3 grid((uint32_t)((threads + KV_THREADS - 1) / KV_THREADS), a.k && a.v ? 2 : 1);
-                if constexpr (WRITE)
-                    hipLaunchKernelGGL((dl_kv_write_kernel<decltype(t), decltype(c), L>), grid, dim3(KV_THREADS), 0, (hipStream_t)stream, a);
+                auto go = [&](auto many) {
+                    constexpr bool MANY = decltype(many)::value;
+                    const uint64_t threads = ((uint64_t)a.rows + MANY) / (MANY ? 2u : 1u) * L;
+                    const dim3 grid((uint32_t)((threads + KV_THREADS - 1) / KV_THREADS), a.k && a.v ? 2 : 1);
+                    if constexpr (WRITE)
+                        hipLaunchKernelGGL((dl_kv_write_kernel<decltype(t), decltype(c), L, MANY>), grid, dim3(KV_THREADS), 0, (hipStream_t)stream, a);
+                    else
+                        hipLaunchKernelGGL((dl_kv_read_kernel<decltype(t), decltype(c), L, MANY>), grid, dim3(KV_THREADS), 0, (hipStream_t)stream, a);
+                };
+                if ((uint64_t)a.rows * L >= KV_MANY_THREADS)
+                    go(std::true_type{});
                 else
-                    hipLaunchKernelGGL((dl_kv_read_kernel<decltype(t), decltype(c), L>), grid, dim3(KV_THREADS), 0, (hipStream_t)stream, a);
+                    go(std::false_type{});
             });
         });
     });
