@@ -166,6 +166,8 @@ struct place {
     }
 };
 
+// (Where head_dim ends before DP, the lanes behind it load its end once more: those dims meet zeros in the queries, and sums that
+// nobody stores.)
 template <int DP>
 struct tile_keys {
     words<16> k[2][DP / 64];  // dims 64 s + 16 g ..
@@ -181,7 +183,7 @@ template <int DP, bool ALIGNED>
 __device__ __forceinline__ void load_keys(const att_args &a, const piece_args &p, const place<ALIGNED> &at, tile_keys<DP> &td)
 {
     const uint32_t lane = threadIdx.x % 64u, i = lane % 16u, g = lane / 16u, D = a.c.head_dim;
-    const uint64_t from = (uint64_t)a.c.k + (uint64_t)p.head * a.c.head_stride + 16u * g;
+    const uint64_t from = (uint64_t)a.c.k + (uint64_t)p.head * a.c.head_stride;
     bool alive;
     uint64_t kp = 0;
 #pragma unroll
@@ -191,7 +193,7 @@ __device__ __forceinline__ void load_keys(const att_args &a, const piece_args &p
         else
             kp += 4ull * a.c.token_stride;
 #pragma unroll
-        for (int s = 0; s < DP / 64; ++s) td.k[t][s] = 16u * g + 64u * s < D ? load_words<16>((const char *)kp + 64 * s) : words<16>{};
+        for (int s = 0; s < DP / 64; ++s) td.k[t][s] = load_words<16>((const char *)kp + min(16u * g + 64u * s, D - 16u));
     }
     const uint64_t scales = (uint64_t)(i < 8u ? a.c.k_scale : a.c.v_scale) + (uint64_t)p.head * a.c.scale_head_stride;
     td.scale = *(const float *)at.offset(a, p, g, i % 8u, at.value_page, a.c.scale_page_stride, a.c.scale_token_stride, scales, &alive);
@@ -202,7 +204,7 @@ __device__ __forceinline__ void load_values(const att_args &a, const piece_args 
 {
     constexpr int VB = DP / 16;
     const uint32_t lane = threadIdx.x % 64u, i = lane % 16u, g = lane / 16u, D = a.c.head_dim;
-    const uint64_t from = (uint64_t)a.c.v + (uint64_t)p.head * a.c.head_stride + VB * i;
+    const uint64_t from = (uint64_t)a.c.v + (uint64_t)p.head * a.c.head_stride + min(VB * i, D - VB);
     bool alive;
     uint64_t vp = 0;
     td.dead = 0;
@@ -214,7 +216,7 @@ __device__ __forceinline__ void load_values(const att_args &a, const piece_args 
         } else {
             vp += a.c.token_stride;
         }
-        td.v[e] = VB * i < D ? load_words<VB>((const char *)vp) : words<VB>{};
+        td.v[e] = load_words<VB>((const char *)vp);
     }
 }
 
@@ -585,7 +587,7 @@ __device__ __forceinline__ void wide_piece(const att_args &a, uint32_t block, wi
 #pragma unroll
         for (uint32_t x = 0; x < K_LOADS; ++x) {
             const uint32_t at = threadIdx.x + x * ATT_THREADS, key = at / PIECES, d = at % PIECES * 8u;
-            kw[x] = d < D ? load_words<8>(k_from + rows_at[from][key] + d) : words<8>{};
+            kw[x] = load_words<8>(k_from + rows_at[from][key] + min(d, D - 8u));
         }
 #pragma unroll
         for (uint32_t x = 0; x < V_LOADS; ++x) {
@@ -593,12 +595,14 @@ __device__ __forceinline__ void wide_piece(const att_args &a, uint32_t block, wi
             const uint32_t key = part / 2u * 16u + part % 2u * 4u;
 #pragma unroll
             for (uint32_t e = 0; e < 8; ++e)
-                vw[x][e] = d < D ? dl_load_at<uint32_t>(v_from + rows_at[from][key + (e & 3u) + (e >> 2) * 8u] + d) : 0u;
+                vw[x][e] = dl_load_at<uint32_t>(v_from + rows_at[from][key + (e & 3u) + (e >> 2) * 8u] + min(d, D - 4u));
         }
     };
     auto put = [&](uint32_t from) {  // what has been loaded, into the tile
         wide_tile<DP> &to = tiles[from];
-        const uint64_t all = alive_at[from];
+        const uint32_t all_lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)alive_at[from]);
+        const uint32_t all_hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(alive_at[from] >> 32));
+        const uint64_t all = (uint64_t)all_hi << 32 | all_lo;
         if (all != ~0ull) {  // what is none counts as zero
 #pragma unroll
             for (uint32_t x = 0; x < K_LOADS; ++x)
