@@ -457,18 +457,14 @@ __device__ __forceinline__ void narrow_piece(const att_args &a, uint32_t block, 
     uint32_t row[NT];
     bool store[NT];
     const uint32_t heads = a.c.heads, seq_rows = a.q_tokens * a.group;
-    // Workgroups go to the eight XCDs in turn.  All heads of a piece go to the same one, next to each other: the heads' rows of
-    // a token share lines of scales and lie in other channels of its L2.
     const bool prefix = block < a.narrow_shared;
     const uint32_t x = prefix ? block : block - a.narrow_shared;
-    const uint32_t tiles = prefix ? a.prefix_tiles : a.own_tiles, inner = x / 8u % (tiles * heads), unit = x / 8u / (tiles * heads) * 8u + x % 8u;
-    const uint32_t tile = inner % tiles, head = inner / tiles;
+    const uint32_t tiles = prefix ? a.prefix_tiles : a.own_tiles, head = x % heads, tile = x / heads % tiles, unit = x / heads / tiles;
     uint32_t b0 = 0, rows;
     int32_t own_last = 0;  // of query 0
     piece_args p;
     p.head = head;
     if (prefix) {
-        if (unit >= a.prefix_splits) return;
         p.first = unit * a.prefix_piece;
         p.end = min(p.first + a.prefix_piece, a.prefix_tokens);
         p.table = a.prefix_pages;
@@ -477,7 +473,7 @@ __device__ __forceinline__ void narrow_piece(const att_args &a, uint32_t block, 
         rows = a.batch * seq_rows;
     } else {
         own_place own;
-        if (unit >= a.own_units || !own_unit(a, unit, &own)) return;
+        if (!own_unit(a, unit, &own)) return;
         b0 = own.b;
         const uint32_t len = own_len(a, b0);
         p.first = own.piece * own.keys;
@@ -487,7 +483,7 @@ __device__ __forceinline__ void narrow_piece(const att_args &a, uint32_t block, 
         rows = seq_rows;
         own_last = (int32_t)len - (int32_t)queries(a, b0);
         p.seen_by_all = min((int32_t)p.end - 1, own_last + (int32_t)(tile * NT * 16u / a.group));
-        if (inner == 0 && own.piece == 0 && threadIdx.x == 0) {
+        if (head == 0 && tile == 0 && own.piece == 0 && threadIdx.x == 0) {
             a.units[2 * b0] = unit;
             a.units[2 * b0 + 1] = own.pieces;
         }
@@ -791,12 +787,13 @@ __global__ void __launch_bounds__(ATT_THREADS) dl_attention_join_kernel(const at
     const uint32_t h = row % a.q_heads, bj = row / a.q_heads, b = bj / a.q_tokens, j = bj - b * a.q_tokens, D = a.c.head_dim;
     uint32_t pieces = 0;
     uint64_t own_part = 0;  // that of the first piece of own tokens, less prefix_splits pieces
+    const uint32_t unit = a.units[2 * b], units = a.units[2 * b + 1];  // (on their way with the length that says whether they are anything)
     if (j < queries(a, b)) {
         pieces = a.prefix_splits;
         if (own_len(a, b)) {
             own_part = (uint64_t)a.prefix_splits * a.rows + (row - b * a.q_tokens * a.q_heads) +
-                       ((uint64_t)a.units[2 * b] - a.prefix_splits) * (a.q_tokens * a.q_heads);
-            pieces += a.units[2 * b + 1];
+                       ((uint64_t)unit - a.prefix_splits) * (a.q_tokens * a.q_heads);
+            pieces += units;
         }
     }
     const uint32_t d0 = 4u * (lane % LANES);
@@ -918,7 +915,10 @@ int att_setup(const dl_kv_cache *cache, const dl_prefix_attention_args *args, dl
     const uint64_t all_rows = (uint64_t)args->batch * seq_rows;
     sh->nt = seq_rows > 16u ? 2 : 1;
     const uint64_t prefix = cache->pages ? (uint64_t)args->prefix_tokens : 0u, own = cache->pages ? (uint64_t)args->max_pages * cache->page_tokens : 0u;
-    sh->wide = all_rows >= 64u && prefix >= 256u;
+    // Wide pieces of the prefix from 2^20 scores on, and 64 rows.  Narrow : wide, rows x prefix x heads of the cache: 84 x 2048 x 4 (0.7 M)
+    // 13.3 : 14.5 us, 126 x 2048 x 4 (1.0 M) 15.0 : 16.5, 168 x 2048 x 4 (1.4 M) 17.9 : 17.0, 128 x 2048 x 8 (2.1 M) 20.3 : 17.7, 84 x 10000 x 4
+    // (3.4 M) 20.6 : 20.1, 2048 x 32768 x 8 885 : 393; but 42 x 20000 x 4 (3.4 M) 18.7 : 23.0.
+    sh->wide = all_rows >= 64u && (uint64_t)all_rows * prefix * (uint32_t)cache->heads >= 1u << 20;
     sh->prefix_tiles = ceil_div(all_rows, sh->wide ? 32u * ATT_WAVES : 16u * sh->nt);
     sh->own_tiles = ceil_div(seq_rows, 16u * sh->nt);
     const uint32_t step = sh->wide ? WIDE_KEYS : STEP;
@@ -1006,8 +1006,8 @@ extern "C" int dl_prefix_attention(const dl_kv_cache *cache, const dl_prefix_att
     a.own_units = sh.own_units;
     a.own_target = sh.own_target;
     a.scale = args->scale * 1.44269504088896340736f;
-    const uint64_t shared = (uint64_t)a.c.heads * sh.prefix_tiles * (sh.wide ? sh.prefix_splits : (sh.prefix_splits + 7u) / 8u * 8u);
-    const uint64_t grid = shared + (uint64_t)a.c.heads * sh.own_tiles * ceil_div(sh.own_units, 8) * 8u;
+    const uint64_t shared = (uint64_t)a.c.heads * sh.prefix_tiles * sh.prefix_splits;
+    const uint64_t grid = shared + (uint64_t)a.c.heads * sh.own_tiles * sh.own_units;
     if (grid > INT32_MAX) return DL_ERR_INVALID;
     a.wide_shared = sh.wide ? (uint32_t)shared : 0u;
     a.narrow_shared = sh.wide ? 0u : (uint32_t)shared;
