@@ -4,7 +4,9 @@
  * The library executes the data movement behind DMA-offloaded collectives
  * (all-gather, all-to-all, broadcast, batched back-to-back copies) on the
  * compute units of one GPU.  W "virtual ranks" are W send buffers and W receive
- * buffers that all live in that GPU's memory.
+ * buffers that all live in that GPU's memory.  Beside it stand the operators that
+ * work on what such copies move in serving: a paged cache in 8 bits, attention
+ * over it, and the verification of drafted tokens (a section of their own below).
  *
  * Conventions for every entry point
  *  - Data pointers (src, dst, in[r], out[r], dsts[d]) are DEVICE pointers owned
@@ -564,14 +566,15 @@ typedef struct dl_kv_cache {
 } dl_kv_cache;
 
 /*
- * `tokens` rows per head of keys and of values outside the cache: element d of token t in head h at
+ * `tokens` rows (tokens * heads <= DL_MAX_ROWS) per head of keys and of values outside the cache: element d of token t in head h at
  * k[t * k_token_stride + h * k_head_stride + d] (strides in elements), likewise v.  k or v may be null: that side of the cache
  * is left alone, and may be null itself.  Token t belongs to slot slots[t].
  */
+#define DL_MAX_ROWS (1 << 27)
 typedef struct dl_kv_rows {
     void *k, *v;
     const int64_t *slots;
-    int64_t tokens;           /* < 2^31 */
+    int64_t tokens;
     int32_t type;             /* dl_type of k and v */
     int32_t reserved;         /* 0 */
     int64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;
@@ -595,7 +598,10 @@ int dl_kv_read(const dl_kv_cache *cache, const dl_kv_rows *rows, void *stream);
  * weights e^(s_i) enter the product with v in the type of q.
  * A query with nothing to attend to, and those from q_lens[b] on, get out = 0 and lse = -infinity.  lens[b] counts as at least 0 and
  * at most max_pages * page_tokens, q_lens[b] as 0 .. q_tokens.  A token whose page in the table is no page of the pool is not
- * attended to.  Codes are those that dl_kv_write writes (fp8: no NaN codes); what lies behind the lengths may hold anything.
+ * attended to.  A row of the cache whose scale is NaN (see dl_kv_format) makes out and lse NaN for the queries that attend to it, and for
+ * no other.  Codes are those that dl_kv_write writes (fp8: no NaN codes); what lies behind the lengths may hold anything.
+ * Work is cut for few queries a sequence (a decoding step, with drafts or without); any number gives the result, and a call
+ * that would need 2^24 workgroups or more is DL_ERR_INVALID.
  */
 typedef struct dl_prefix_attention_args {
     const void *q;                /* [batch][q_tokens][q_heads][head_dim], strides in elements, head_dim contiguous */
@@ -613,7 +619,7 @@ typedef struct dl_prefix_attention_args {
     int64_t q_seq_stride, q_token_stride, q_head_stride;
     int64_t out_seq_stride, out_token_stride, out_head_stride;
     int32_t type;                 /* of q and out: DL_TYPE_BF16 or DL_TYPE_F16 */
-    int32_t batch, q_tokens;      /* batch * q_tokens * q_heads < 2^31 */
+    int32_t batch, q_tokens;      /* batch * q_tokens * q_heads <= DL_MAX_ROWS / 2 */
     int32_t q_heads;              /* a multiple of the cache's heads */
     float scale;                  /* what the scores are multiplied with */
     int32_t reserved;             /* 0 */

@@ -18,5 +18,5 @@ from .binding import (  # noqa: F401
     dl_plan_token_dispatch, dl_plan_batch_inferred, dl_set_trace, dl_get_trace, dl_trace_clock,
     dl_last_device_error, dl_debug_lose_next_table, dl_batch_copy_static, dl_plan_mode, dl_last_mode,
     dl_complete, dl_parse_config, dl_token_dispatch_device, DL_TYPE_F32, DL_TYPE_BF16, DL_TYPE_F16, DL_KV_FP8,
-    DL_KV_INT8, DL_MAX_DRAFTS, KvCache, KvRows, PrefixAttention, DraftVerify, dl_kv_write, dl_kv_read, dl_prefix_attention,
+    DL_KV_INT8, DL_MAX_DRAFTS, DL_MAX_ROWS, KvCache, KvRows, PrefixAttention, DraftVerify, dl_kv_write, dl_kv_read, dl_prefix_attention,
     dl_prefix_attention_workspace, dl_verify_draft, dl_verify_draft_workspace)

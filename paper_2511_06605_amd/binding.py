@@ -41,6 +41,7 @@ DL_OP_BATCH, DL_OP_BROADCAST, DL_OP_ALLGATHER, DL_OP_ALLTOALL, DL_OP_SWAP, DL_OP
 DL_TYPE_F32, DL_TYPE_BF16, DL_TYPE_F16 = range(3)
 DL_KV_FP8, DL_KV_INT8 = range(2)
 DL_MAX_DRAFTS = 63
+DL_MAX_ROWS = 1 << 27
 DL_AUTO_STANDBY_TILES = 64
 DL_AUTO_SIGNAL_MAX_BYTES = 288 << 20
 DL_AUTO_PRELAUNCH_MAX_BYTES = 288 << 20

