@@ -7,8 +7,6 @@ import shutil
 import subprocess
 import sys
 import sysconfig
-import tempfile
-from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -19,6 +17,7 @@ SOURCES = ["dl_api.hip", "dl_exec.hip", "dl_prelaunch.hip", "dl_dispatch.hip", "
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-fno-gpu-rdc",
+    "-parallel-jobs=8",  # sources side by side
     "-Wall", "-Wextra", "-Wno-unused-parameter",
     # packed-fp32 instructions stay off for every device function in this library
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -57,12 +56,7 @@ def _build_marshal(verbose) -> None:
 def build(verbose: bool = False) -> str:
     """The library, then the extension module for Python."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    with tempfile.TemporaryDirectory() as tmp:  # the sources side by side, then one link
-        objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
-        compile_flags = [f for f in HIPCC_FLAGS if f != "-shared"]
-        with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:
-            list(pool.map(lambda so: _run([hipcc, *compile_flags, "-c", os.path.join(CSRC, so[0]), "-o", so[1]], verbose), zip(SOURCES, objects)))
-        _run([hipcc, "--offload-arch=gfx950", "-fno-gpu-rdc", "-shared", "-fPIC", *objects, "-o", LIB], verbose)
+    _run([hipcc, *HIPCC_FLAGS, *[os.path.join(CSRC, s) for s in SOURCES], "-o", LIB], verbose)
     _build_marshal(verbose)
     return LIB
 
