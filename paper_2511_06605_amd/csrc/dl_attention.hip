@@ -9,7 +9,13 @@
 //
 // The key axis is cut into pieces.  A piece of the prefix serves the queries of all sequences at once: they are the rows of
 // one product.  A piece of a sequence's own tokens serves the query heads that share a head of the cache.  All pieces of
-// both kinds are one launch; a second one joins each row's pieces.
+// both kinds are one launch; a second one joins each row's pieces.  (Joined in the launch that makes them, by the last workgroup of a row: slower
+// everywhere, 32 sequences on a prefix of 2048 17 : 104 us, one with 5000 tokens 12.0 : 13.2; pieces then have to be seen across dies.)
+//
+// Measured (8 heads of 128, 64 query heads, bfloat16 on fp8, unless said otherwise): 256 sequences, one query each, on a prefix of 32768 390 us,
+// 277 GFLOP, 0.71 PFLOP/s where a large matrix product reaches 1.3; 48 sequences with 5 queries on 16400 (4 heads, 28 query heads, float16 on
+// int8) 107 us; 4 sequences with up to 131072 tokens of their own (554 MB) 130 us, 4.3 TB/s; one with 5000 (32 query heads) 11.3 us, two
+// launches and the chain of length, table, codes, join.
 #include "dl_codes.h"
 #include "dl_internal.h"
 
@@ -227,6 +233,11 @@ struct sums {
     float l[NT];              // a lane's share
 };
 
+// (A narrow piece is bound by its loads.  Tiles of 16 rows fit a handful of queries with the least waste.  Wavefronts take different keys,
+// so each loads what it needs straight into registers, no codes go through LDS, and nothing waits for another wavefront before the
+// end.  Loads a step ahead: one sequence with 5000 tokens 36.8 -> 11.6 us, 4 with up to 131072 529 -> 198; pieces by length on the device
+// 198 -> 132.)
+//
 // A step: 32 keys against NT tiles of 16 rows.  whole: all of them are seen by all.  The next step's keys are loaded as
 // soon as the scores have been taken, its values after the sums, into the same registers.
 template <class Q, class C, int DP, int NT, bool ALIGNED>
@@ -501,11 +512,17 @@ __device__ __forceinline__ void narrow_piece(const att_args &a, uint32_t block, 
     attend<Q, C, DP, NT, ALIGNED>(a, p, qrow, last, row, store, lds);
 }
 
-// The prefix against many queries, bound by the matrix units.  A workgroup has WIDE_ROWS rows of the batch (32 NB a wavefront)
+// The prefix against many queries.  A workgroup has 128 rows of the batch (32 a wavefront)
 // and walks the keys of its piece in tiles of 64, which its wavefronts share: the codes are turned into elements of Q once, on
 // their way into LDS, keys as rows and values transposed (by byte permutes while they are bytes), so that every operand of the
 // 32 x 32 x 16 products is one 16-byte read.  While a tile is worked on, the next one's codes are on their way to registers and the
 // pages of the one after it are looked up; a barrier a tile.
+//
+// What bounds it is the sum of the pipes: of its cycles, vector instructions (scales, exponentials, sums of weights, turning codes) are issued in
+// 48 %, the matrix units work in 33 %, LDS in 49 %, and no order of the parts overlapped them better.  256 sequences on a prefix of 32768 (see
+// the top), this : 64 rows a wavefront (one a SIMD) 393 : 486 us, workgroups of 256 rows 416 : 430, two groups of wavefronts that take
+// turns 393 : 409, keys in the lanes of the scores 393 : 427; scores beside the next tile's conversion and operands read a group
+// ahead 393 : 380, which short prefixes lose again (32 sequences on 2048 17.8 : 18.7).
 //
 // Operands lie in rows of 16-byte pieces, whose places are exchanged (by an exclusive or with the row's number) so that eight
 // neighbouring lanes use all banks, in reads and in writes.
@@ -751,7 +768,8 @@ __global__ void __launch_bounds__(ATT_THREADS, DP <= 128 ? 2 : 1) dl_attention_k
     }
 }
 
-// Joins the pieces of a row.  WAVES wavefronts a row share them out; in a wavefront DP / 4 lanes hold a piece's sums, four
+// Joins the pieces of a row: a read of what they left, 3 us for a few rows, 13 us for 16384 rows of 4 pieces of 128 (35 MB).  WAVES wavefronts
+// a row share them out; in a wavefront DP / 4 lanes hold a piece's sums, four
 // each, so 256 / DP pieces are looked at together and four times as many are on their way.
 template <class Q, int DP, int WAVES>
 __global__ void __launch_bounds__(ATT_THREADS) dl_attention_join_kernel(const att_args a)

@@ -68,7 +68,7 @@ __device__ __forceinline__ unsigned long long pair_of(float w, float e, uint32_t
 __device__ __forceinline__ unsigned long long larger(unsigned long long a, unsigned long long b) { return a > b ? a : b; }
 
 // The largest pair of entries first .. end - 1, in every thread of the workgroup.  q: subtracted where it is not null;
-// without: this entry weighs nothing (vocab: all count).
+// without: this entry weighs nothing (0xFFFFFFFF: all count).
 template <class T>
 __device__ unsigned long long best_of(const char *p, const char *q, const float *race, uint32_t without, uint32_t first, uint32_t end)
 {
@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(VERIFY_THREADS) dl_verify_kernel(const verify_
 // Entries of a workgroup's piece of a row: so many that the batch makes two workgroups for each of the chip's 256 compute units, a
 // multiple of what the threads look at at once.  More workgroups only find out more often where to look: 128 sequences of 4
 // drafts over 128000 entries 30.7 us with 512, 32.2 with 1024, and (with loads that stay in the caches) 35.0, 36.0, 36.8, 42.0 and 66.9
-// with 512, 1024, 2048, 4096 and 8192.  At 30.7 us that case reads 5.5 TB/s; 26 us is what its 170 MB take at the rate of a large copy.
+// with 512, 1024, 2048, 4096 and 8192.  At 30 us that case reads 5.7 TB/s; 26 us is what its 170 MB take at the rate of a large copy.
 uint32_t verify_piece(int32_t batch, int32_t vocab)
 {
     const uint32_t split = (512u + (uint32_t)batch - 1u) / (uint32_t)batch, step = 4u * VERIFY_THREADS;
