@@ -1,11 +1,15 @@
 // Attention of a batch that shares a prefix, over a paged cache in 8 bits (dl_prefix_attention).
 //
 // With s the scores in units of ln 2 and u the scales of the values, a query's output is sum of 2^s u V / sum of 2^s over the codes V
-// of what it sees.  The sums are taken piece by piece with a running reference r = largest s + log2 u so far:
-//   w = 2^(s + log2 u - r) <= 1,   O += w V,   l += w / u,
-// both multiplied by 2^(r before - r) when r grows.  So the weights that go to the matrix units in 16 bits are at most 1
-// (times 2^15 for float16, see lift) whatever the scales are, and the codes go there as they are (each is a value of both
-// 16-bit types): the only rounding on the way is that of w.  Pieces of the same row are joined in the same manner, in a fixed order.
+// of what it sees.  A scale is taken apart, u = c d, with c within 2^-40 .. 2^40 (2^50 for float16) and d = 1 for all but rows
+// of zeros and values of very unusual sizes (see value_scale).  The sums are taken piece by piece with a running reference r, within 2^8 of
+// the largest s + log2 c so far:
+//   w = 2^(s + log2 c - r) <= 2^8,   O += w d V,   l += w / c,
+// both multiplied by 2^(r before - r) when r grows.  So the weights that go to the matrix units in 16 bits are at most 2^8 (times 2^lift,
+// see there) whatever the scales are, and the codes go there as they are (each is a value of both 16-bit types): the only rounding on
+// the way is that of w d.  As c is bounded, l is: a key adds at most 2^(8 + lift + 40) to it, 2^30 keys no more than 2^85; and as
+// 32-bit numbers are whole down to 2^-126, no key drops out of l whose 2^s is above 2^-42 of the largest.
+// Pieces of the same row are joined in the same manner, in a fixed order.
 //
 // The key axis is cut into pieces.  A piece of the prefix serves the queries of all sequences at once: they are the rows of
 // one product.  A piece of a sequence's own tokens serves the query heads that share a head of the cache.  All pieces of
@@ -132,6 +136,29 @@ __device__ __forceinline__ float largest_of_quarters(float x)
     return fmaxf(dl_bits<float>((uint32_t)b[0]), dl_bits<float>((uint32_t)b[1]));
 }
 
+// A value's scale u = c d for the sums, d a power of two.  c: what log2 u and 1 / u are taken of, so that neither they nor a product with
+// 2^(log2 u) or 1 / u leave the range of 32 bits, however far apart the scales of the rows are that a query sees.  d: 1, or what that
+// leaves out; it goes to the product with the values alone (never to l), and is finite, so that a weight of zero takes it out.
+// Scales below 2^-126 (dl_kv_write gives 2^-100 / 448 and more) count as zero, and so do negative ones.  A NaN stays in c.
+template <class Q>
+struct value_scale {
+    float c, d;
+    __device__ __forceinline__ explicit value_scale(float u)
+    {
+        constexpr float LOW = 0x1p-40f, HIGH = Q::scale_most;
+        // u's power of two (none for what is no positive number, infinite for infinities), and what it is more than the limit's
+        const float power = dl_bits<float>(dl_bits<uint32_t>(fmaxf(u, 0.0f)) & 0x7F800000u);
+        const bool low = u < LOW, high = u >= 2.0f * HIGH;
+        d = low ? power * (1.0f / LOW) : high ? fminf(power, 0x1p127f) * (1.0f / HIGH) : 1.0f;
+        // (the mantissa of u with the limit's power)
+        const float c_limit = dl_bits<float>((dl_bits<uint32_t>(u) & 0x007FFFFFu) | dl_bits<uint32_t>(low ? LOW : HIGH));
+        c = low || high ? c_limit : u;
+    }
+    __device__ __forceinline__ float log2_c() const { return __builtin_amdgcn_logf(c); }
+    // (finite for a NaN as well: its readers' weights have it from the logarithm)
+    __device__ __forceinline__ float over_c() const { return __builtin_amdgcn_rcpf(c == c ? c : 1.0f); }
+};
+
 // What is the same for a workgroup's whole piece: NT tiles of 16 rows against the keys first .. end - 1 of one head.
 struct piece_args {
     const int32_t *table;
@@ -243,26 +270,27 @@ struct sums {
 template <class Q, class C, int DP, int NT, bool ALIGNED>
 __device__ __forceinline__ void attend_tile(const att_args &a, const piece_args &p, const place<ALIGNED> &at, const place<ALIGNED> &then, bool whole,
                                             tile_keys<DP> &tk, tile_values<DP> &tv, const dl_u32x4 (&qf)[NT][DP / 32], const int32_t (&last)[NT], sums<DP, NT> &acc,
-                                            float (&scales)[3][TILE])
+                                            float (&scales)[4][TILE])
 {
     constexpr int VB = DP / 16, STEPS = DP / 32;
     const uint32_t lane = threadIdx.x % 64u, i = lane % 16u, g = lane / 16u, base = at.base;
     uint32_t here = 0;  // bit e: key 8 g + e is in a page of the pool, and of the piece
+    bool taken_apart;   // some key's d is not 1 (what nobody sees counts as well, and does no harm)
     {
         if (!whole) {
             const uint32_t left = p.end - min(p.end, base + 8u * g);
             here = (left >= 8u ? 0xFFu : (1u << left) - 1u) & ~tv.dead;
         }
         const uint32_t key = 8u * g + i % 8u;
+        const value_scale<Q> u(tk.scale);
         if (i < 8u) {
             scales[0][key] = tk.scale * a.scale;
         } else {
-            // a logarithm and a reciprocal of what is no denormal number.  A scale of NaN reaches its readers' weights through
-            // the logarithm; the reciprocal is finite, so that a weight of zero takes it out.
-            const float u = tk.scale < 0x1p-120f ? 0x1p-120f : tk.scale;
-            scales[1][key] = __builtin_amdgcn_logf(u);
-            scales[2][key] = __builtin_amdgcn_rcpf(u == u ? u : 1.0f);
+            scales[1][key] = u.log2_c();
+            scales[2][key] = u.over_c();
+            scales[3][key] = u.d;
         }
+        taken_apart = __any(i >= 8u && u.d != 1.0f);
     }
     // scores: the product's rows are keys (8 g + 4 t + j in lane (i, g)), its columns queries (i)
     dl_f32x4 s[NT][2];
@@ -320,6 +348,12 @@ __device__ __forceinline__ void attend_tile(const att_args &a, const piece_args 
             w[e] = __builtin_amdgcn_exp2f(x[e] - acc.low[n]);
             acc.l[n] = fmaf(w[e], iu[e], acc.l[n]);
         }
+        if (taken_apart) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = Q::in_range(w[e] * scales[3][8u * g + e]);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
         pf[n] = dl_u32x4{Q::pack(w[0], w[1]), Q::pack(w[2], w[3]), Q::pack(w[4], w[5]), Q::pack(w[6], w[7])};
     }
     if (!whole) {
@@ -353,7 +387,7 @@ __device__ __forceinline__ void attend_tile(const att_args &a, const piece_args 
 
 template <int DP, int NT>
 struct narrow_lds {
-    float scales[ATT_WAVES][3][TILE];
+    float scales[ATT_WAVES][4][TILE];
     float joined[2][NT * DP / 16 * 4 + 2 * NT][64];
 };
 
@@ -529,10 +563,11 @@ __device__ __forceinline__ void narrow_piece(const att_args &a, uint32_t block, 
 constexpr uint32_t WIDE_KEYS = 64;
 
 template <int DP>
-struct wide_tile {
+struct alignas(16) wide_tile {  // (reads of 16 bytes that lie at fours take twice as long)
     uint32_t k[WIDE_KEYS * DP / 2];  // key, dim
     uint32_t v[WIDE_KEYS * DP / 2];  // dim, key: of each 16 keys 0 - 3, 8 - 11, 4 - 7, 12 - 15
-    float ks[WIDE_KEYS], lu[WIDE_KEYS], iu[WIDE_KEYS];
+    float ks[WIDE_KEYS], lu[WIDE_KEYS], iu[WIDE_KEYS], d[WIDE_KEYS];
+    uint32_t taken_apart;  // (as in attend_tile)
 };
 template <int DP>
 struct wide_lds {
@@ -650,10 +685,29 @@ __device__ __forceinline__ void wide_piece(const att_args &a, uint32_t block, wi
         if (wave == 0) {
             to.ks[lane] = alive ? scale * a.scale : 0.0f;
         } else if (wave == 1) {
-            const float u = scale < 0x1p-120f ? 0x1p-120f : scale;  // (as in attend_tile)
-            to.lu[lane] = alive ? __builtin_amdgcn_logf(u) : -INFINITY;
-            to.iu[lane] = alive ? __builtin_amdgcn_rcpf(u == u ? u : 1.0f) : 0.0f;
+            const value_scale<Q> u(scale);
+            to.lu[lane] = alive ? u.log2_c() : -INFINITY;
+            to.iu[lane] = alive ? u.over_c() : 0.0f;
+            to.d[lane] = u.d;
+            const bool some = __any(u.d != 1.0f);
+            if (lane == 0) to.taken_apart = some;
         }
+    };
+
+    // Values times what their scales left out, in LDS, by all threads, before anybody works on the tile.  (At the weights instead, by a branch
+    // between them and the products: 256 sequences on 32768 402 us, this 393, neither 387.)
+    auto apart = [&](wide_tile<DP> &t) {
+#pragma unroll 1
+        for (uint32_t at = threadIdx.x; at < DP * 8u; at += ATT_THREADS) {
+            const uint32_t r = at / 8u, part = at % 8u, key = part / 2u * 16u + part % 2u * 4u;
+            uint32_t *const to = &t.v[(r * 8u + (part ^ ((r & 7u) ^ (r >> 3 & 3u)))) * 4u];
+#pragma unroll
+            for (uint32_t x = 0; x < 4; ++x) {
+                const float *const d = &t.d[key + x / 2u * 8u + x % 2u * 2u];
+                to[x] = Q::pack(Q::in_range(Q::lo(to[x]) * d[0]), Q::in_range(Q::hi(to[x]) * d[1]));
+            }
+        }
+        __syncthreads();
     };
 
     dl_f32x16 o[DP / 32];
@@ -674,6 +728,7 @@ __device__ __forceinline__ void wide_piece(const att_args &a, uint32_t block, wi
     uint32_t now = 0;
     for (uint32_t base = first; base < end; base += WIDE_KEYS, now ^= 1u) {
         const bool more = base + WIDE_KEYS < end;
+        if (__builtin_amdgcn_readfirstlane((int)tiles[now].taken_apart)) apart(tiles[now]);
         if (more) {
             load(now ^ 1u);
             look_up(base + 2 * WIDE_KEYS);

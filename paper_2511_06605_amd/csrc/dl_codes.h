@@ -68,6 +68,10 @@ struct dl_bf16 {
     // Weights relative to a reference, at most 2^8, are held as 2^lift times as much.  Floats of 16 bits lose bits below 2^-14,
     // so there they use the range above as well: what is 2^-21 of the reference still has all of its bits.
     static constexpr float lift = 0.0f;
+    // Scales of values from twice this one on are taken apart (value_scale in dl_attention.hip), and a product with what that leaves over
+    // is brought into the type's range.
+    static constexpr float scale_most = 0x1p40f;
+    static __device__ __forceinline__ float in_range(float w) { return w; }
     static __device__ __forceinline__ float lo(uint32_t w) { return dl_bits<float>(w << 16); }
     static __device__ __forceinline__ float hi(uint32_t w) { return dl_bits<float>(w & 0xFFFF0000u); }
     static __device__ __forceinline__ uint32_t pack(float a, float b) { return dl_bits<uint32_t>(dl_bf16x2{(__bf16)a, (__bf16)b}); }
@@ -84,6 +88,10 @@ struct dl_bf16 {
 struct dl_f16 {
     static constexpr int size = 2;
     static constexpr float lift = 7.0f;
+    // (Such products may saturate, in rows with values above 448 x 2^50 = 5e17; an output of this type is finite only where such a row's
+    // weight is less than 2^-40 of the others'.)
+    static constexpr float scale_most = 0x1p50f;
+    static __device__ __forceinline__ float in_range(float w) { return fminf(fmaxf(w, -65504.0f), 65504.0f); }
     static __device__ __forceinline__ float lo(uint32_t w) { return (float)dl_bits<dl_f16x2>(w)[0]; }
     static __device__ __forceinline__ float hi(uint32_t w) { return (float)dl_bits<dl_f16x2>(w)[1]; }
     static __device__ __forceinline__ uint32_t pack(float a, float b) { return dl_bits<uint32_t>(dl_f16x2{(_Float16)a, (_Float16)b}); }
