@@ -831,7 +831,7 @@ __global__ void __launch_bounds__(ATT_THREADS) dl_attention_join_kernel(const at
 {
     constexpr uint32_t LANES = DP / 4, SIDE = 64 / LANES, AHEAD = 4;
     const uint32_t lane = threadIdx.x % 64u, wave = threadIdx.x / 64u, part = lane / LANES + (WAVES > 1 ? wave * SIDE : 0u);
-    const uint32_t row = WAVES > 1 ? blockIdx.x : blockIdx.x * ATT_WAVES + wave;
+    const uint32_t block = blockIdx.y * gridDim.x + blockIdx.x, row = WAVES > 1 ? block : block * ATT_WAVES + wave;
     if (row >= a.rows) return;
     const uint32_t h = row % a.q_heads, bj = row / a.q_heads, b = bj / a.q_tokens, j = bj - b * a.q_tokens, D = a.c.head_dim;
     uint32_t pieces = 0;
@@ -957,7 +957,7 @@ int att_setup(const dl_kv_cache *cache, const dl_prefix_attention_args *args, dl
         args->max_pages * cache->page_tokens > 1 << 30)
         return DL_ERR_INVALID;
     const unsigned __int128 rows = (unsigned __int128)args->batch * (uint32_t)args->q_tokens * (uint32_t)args->q_heads;
-    if (rows > DL_MAX_ROWS / 2) return DL_ERR_INVALID;  // (a wavefront of the join each, and a grid has less than 2^32 threads)
+    if (rows > DL_MAX_ROWS / 2) return DL_ERR_INVALID;
     *sh = att_shape{};
     sh->rows = (uint64_t)rows;
     if (!rows) return DL_OK;
@@ -1065,6 +1065,9 @@ extern "C" int dl_prefix_attention(const dl_kv_cache *cache, const dl_prefix_att
     const bool aligned = cache->page_tokens % 8 == 0;
     // a row's pieces: a wavefront's work while the rows alone fill the chip or the pieces are few
     const bool shared_out = sh.prefix_splits + sh.own_units / a.batch > 16u && sh.rows < 4096u;
+    // (the most rows there may be are 2^24 workgroups of the join, 2^32 threads: one more than a grid is wide)
+    const uint32_t blocks = ceil_div(sh.rows, ATT_WAVES), high = ceil_div(blocks, 1u << 23);
+    const dim3 join(ceil_div(blocks, high), high);
     dl_with_16bit(args->type, [&](auto q) {
         auto with_dim = [&](auto dp) {
             constexpr int DP = decltype(dp)::value;
@@ -1083,7 +1086,7 @@ extern "C" int dl_prefix_attention(const dl_kv_cache *cache, const dl_prefix_att
             if (shared_out)
                 hipLaunchKernelGGL((dl_attention_join_kernel<decltype(q), DP, 4>), dim3((uint32_t)sh.rows), dim3(ATT_THREADS), 0, hs, a);
             else
-                hipLaunchKernelGGL((dl_attention_join_kernel<decltype(q), DP, 1>), dim3(ceil_div(sh.rows, ATT_WAVES)), dim3(ATT_THREADS), 0, hs, a);
+                hipLaunchKernelGGL((dl_attention_join_kernel<decltype(q), DP, 1>), join, dim3(ATT_THREADS), 0, hs, a);
         };
         if (a.c.head_dim <= 64)
             with_dim(std::integral_constant<int, 64>{});
