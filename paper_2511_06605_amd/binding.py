@@ -489,6 +489,11 @@ def _expect(t, what, dtype, shape, packed=False):
     return _addr(t)
 
 
+def _strides(t):
+    """Strides of a tensor, 0 where a dimension has nothing to step to (torch puts anything there)."""
+    return tuple(s if n > 1 else 0 for n, s in zip(t.shape, t.stride()))
+
+
 class _Request:
     """A descriptor of the C boundary, the tensors it names, and its address for the calls."""
 
@@ -520,10 +525,10 @@ class KvCache(_Request):
             if _dtype(s) != "float32" or tuple(s.shape) != shape[:3] or getattr(s, "is_cuda", True) is False:
                 raise ValueError(f"{name}: float32 of shape {shape[:3]} in device memory")
             setattr(d, name, _addr(s))
-        if tuple(k.stride()) != tuple(v.stride()) or tuple(k_scale.stride()) != tuple(v_scale.stride()):
+        if _strides(k) != _strides(v) or _strides(k_scale) != _strides(v_scale):
             raise ValueError("keys and values have different strides")
-        d.page_stride, d.token_stride, d.head_stride = k.stride()[:3]
-        d.scale_page_stride, d.scale_token_stride, d.scale_head_stride = k_scale.stride()
+        d.page_stride, d.token_stride, d.head_stride = _strides(k)[:3]
+        d.scale_page_stride, d.scale_token_stride, d.scale_head_stride = _strides(k_scale)
         self._hold(d, k, v, k_scale, v_scale)
 
 
