@@ -531,7 +531,8 @@ int dl_token_dispatch_device(const void *const *in, void *const *out, int W, con
  *  - they always execute as in DL_MODE_ONESHOT, on `stream` (other modes have no effect on them), allocate nothing, use no
  *    memory of the library's, and may be captured into a HIP graph.  Lengths and tables are read when the kernels run, so a
  *    captured step can be replayed as they grow;
- *  - results do not depend on the order in which workgroups run: the same inputs give the same bits;
+ *  - results do not depend on the order in which workgroups run: the same inputs give the same bits (but see dl_kv_write for
+ *    tokens that share a slot);
  *  - addresses need the alignment of one element (codes: none).
  */
 typedef enum dl_type { DL_TYPE_F32 = 0, DL_TYPE_BF16 = 1, DL_TYPE_F16 = 2 } dl_type;
@@ -582,7 +583,9 @@ typedef struct dl_kv_rows {
 
 /*
  * Quantise rows into the cache / read them back.  A slot that is negative or behind the last page is no slot: that token is not
- * written, or reads back as zeros.  Two tokens with one slot in a call of dl_kv_write leave either row there.
+ * written, or reads back as zeros.  The slots of a call of dl_kv_write differ from each other (those that are none aside): of tokens
+ * that share one, each code and the scale there may be any one's, so that what it holds stands for none of them; other slots are not
+ * affected.  In dl_kv_read slots may repeat.
  * tokens == 0: DL_OK, no work.
  */
 int dl_kv_write(const dl_kv_cache *cache, const dl_kv_rows *rows, void *stream);

@@ -617,7 +617,7 @@ def _rows_fit(cache, rows):
 
 
 def dl_kv_write(cache: KvCache, rows: KvRows, stream=None) -> None:
-    """Quantise rows into their slots of the cache."""
+    """Quantise rows into their slots of the cache, which differ from each other (but for those that are none)."""
     _rows_fit(cache, rows)
     _check(lib().dl_kv_write(cache.at, rows.at, _stream(stream)), "dl_kv_write")
 
