@@ -47,7 +47,7 @@ struct att_args {
     uint32_t batch, q_tokens, q_heads, group;
     uint32_t rows;                     // batch * q_tokens * q_heads
     uint32_t prefix_tiles, prefix_splits, prefix_piece;
-    uint32_t own_tiles, own_target;  // own_target: see own_unit
+    uint32_t own_tiles, own_target;  // own_target: see own_unit; 0: a piece a sequence
     uint32_t narrow_shared, wide_shared;  // workgroups with a piece of the prefix, of either kind
     float scale;                       // times log2 e
 };
@@ -76,7 +76,9 @@ __device__ __forceinline__ uint32_t sum_up_to(uint32_t x)
 // The sequences' own tokens are cut by their lengths, which only the device knows: into pieces of as many steps (of STEP keys)
 // as share the steps of all sequences out over own_target pieces.  Sequences are then of one or more pieces, own_target + batch
 // in all at most, and unit n is the n-th of them.  Every wavefront works this out from the lengths for itself.
-// (Batches of more than OWN_EVEN_MAX sequences have workgroups enough without: a piece a sequence.)
+// Not so batches of more than OWN_EVEN_MAX sequences, whose lengths are not added up, and tables with room for 2^31 steps and more,
+// where 32 bits may not hold the sum: a piece a sequence, whatever its length.  A long one among many short ones is then a single
+// workgroup's work in each head.
 constexpr uint32_t OWN_EVEN_MAX = 1024;
 constexpr uint32_t OWN_LEAST_STEPS = 2;
 
@@ -87,7 +89,7 @@ struct own_place {
 __device__ __forceinline__ bool own_unit(const att_args &a, uint32_t unit, own_place *at)
 {
     auto steps_of = [&](uint32_t b) { return (own_len(a, b) + STEP - 1u) / STEP; };
-    if (a.batch > OWN_EVEN_MAX) {
+    if (!a.own_target) {
         if (unit >= a.batch || !own_len(a, unit)) return false;
         *at = {unit, 0, 1, 1u << 31};
         return true;
@@ -982,9 +984,10 @@ int att_setup(const dl_kv_cache *cache, const dl_prefix_attention_args *args, dl
         // Own tokens: pieces for two rounds of workgroups; where the sequences alone are a round, of a quarter of a round's share,
         // which even out what the lengths do not.
         const uint32_t batch = (uint32_t)args->batch, round = slots / (uint32_t)cache->heads / sh->own_tiles;
-        sh->own_target = round > batch ? 2u * round - batch : round ? 4u * round : 1u;
+        const bool even = batch <= OWN_EVEN_MAX && (uint64_t)batch * ceil_div(own, STEP) < 1ull << 31;
+        sh->own_target = !even ? 0u : round > batch ? 2u * round - batch : round ? 4u * round : 1u;
         const uint64_t most = (uint64_t)batch * ceil_div(own, STEP * OWN_LEAST_STEPS);  // no piece is smaller, but a sequence's last
-        sh->own_units = batch > OWN_EVEN_MAX ? batch : (uint32_t)((uint64_t)sh->own_target + batch < most ? sh->own_target + batch : most);
+        sh->own_units = !even ? batch : (uint32_t)((uint64_t)sh->own_target + batch < most ? sh->own_target + batch : most);
     }
     return DL_OK;
 }
