@@ -16,10 +16,11 @@
 // both kinds are one launch; a second one joins each row's pieces.  (Joined in the launch that makes them, by the last workgroup of a row: slower
 // everywhere, 32 sequences on a prefix of 2048 17 : 104 us, one with 5000 tokens 12.0 : 13.2; pieces then have to be seen across dies.)
 //
-// Measured (8 heads of 128, 64 query heads, bfloat16 on fp8, unless said otherwise): 256 sequences, one query each, on a prefix of 32768 390 us,
-// 277 GFLOP, 0.71 PFLOP/s where a large matrix product reaches 1.3; 48 sequences with 5 queries on 16400 (4 heads, 28 query heads, float16 on
-// int8) 107 us; 4 sequences with up to 131072 tokens of their own (554 MB) 130 us, 4.3 TB/s; one with 5000 (32 query heads) 11.3 us, two
-// launches and the chain of length, table, codes, join.
+// Measured (8 heads of 128, 64 query heads, bfloat16 on fp8, unless said otherwise): 256 sequences, one query each, on a prefix of 32768 393 us,
+// 277 GFLOP, 0.70 PFLOP/s where a large matrix product reaches 1.3; 48 sequences with 5 queries on 16400 (4 heads, 28 query heads, float16 on
+// int8) 107 us; 4 sequences with up to 131072 tokens of their own (554 MB) 133 us, 4.2 TB/s; one with 5000 (32 query heads) 11.4 us, two
+// launches and the chain of length, table, codes, join.  Heads of 256: 256 sequences on 16384 564 us, 0.50 PFLOP/s, on one wavefront a SIMD and
+// with 50 registers spilled.
 #include "dl_codes.h"
 #include "dl_internal.h"
 
@@ -554,8 +555,9 @@ __device__ __forceinline__ void narrow_piece(const att_args &a, uint32_t block, 
 // 32 x 32 x 16 products is one 16-byte read.  While a tile is worked on, the next one's codes are on their way to registers and the
 // pages of the one after it are looked up; a barrier a tile.
 //
-// What bounds it is the sum of the pipes: of its cycles, vector instructions (scales, exponentials, sums of weights, turning codes) are issued in
-// 48 %, the matrix units work in 33 %, LDS in 49 %, and no order of the parts overlapped them better.  256 sequences on a prefix of 32768 (see
+// What bounds it is the sum of the pipes: of the call's cycles, vector instructions (scales, exponentials, sums of weights, turning codes) are issued in
+// 49 %, the matrix units work in 29 %, LDS in 44 %, and no order of the parts overlapped them better.  The largest part that could go is
+// turning codes, which each of 16 tiles of rows does again: without it (and with wrong results) 291 us of 375.  256 sequences on a prefix of 32768 (see
 // the top), this : 64 rows a wavefront (one a SIMD) 393 : 486 us, workgroups of 256 rows 416 : 430, two groups of wavefronts that take
 // turns 393 : 409, keys in the lanes of the scores 393 : 427; scores beside the next tile's conversion and operands read a group
 // ahead 393 : 380, which short prefixes lose again (32 sequences on 2048 17.8 : 18.7).
@@ -974,7 +976,10 @@ int att_setup(const dl_kv_cache *cache, const dl_prefix_attention_args *args, dl
     sh->prefix_tiles = ceil_div(all_rows, sh->wide ? 32u * ATT_WAVES : 16u * sh->nt);
     sh->own_tiles = ceil_div(seq_rows, 16u * sh->nt);
     const uint32_t step = sh->wide ? WIDE_KEYS : STEP;
-    const uint32_t slots = cache->head_dim > 128 ? 256u : sh->wide || sh->nt == 2u ? 512u : 768u;  // what registers and LDS leave room for
+    // Workgroups at once, by the registers: at head_dim 65 .. 128 three a compute unit with one narrow tile (152 - 159 registers), two with two
+    // (223 - 240) or with wide pieces (256, for the own ones of that launch too), one above.  Up to 64 there would be room for four with one tile (108 - 118) and
+    // three with two (158 - 167), which the cut does not count on.
+    const uint32_t slots = cache->head_dim > 128 ? 256u : sh->wide || sh->nt == 2u ? 512u : 768u;
     sh->prefix_splits = cut((uint64_t)cache->heads * sh->prefix_tiles, ceil_div(prefix, step), slots);
     if (sh->prefix_splits) {
         sh->prefix_piece = ceil_div(ceil_div(prefix, sh->prefix_splits), step) * step;
