@@ -670,6 +670,141 @@ typedef struct dl_verify_draft_args {
 int64_t dl_verify_draft_workspace(const dl_verify_draft_args *args);
 int dl_verify_draft(const dl_verify_draft_args *args, void *stream);
 
+/* ------------------------------------------- a prompt on its way into a bounded cache */
+
+/*
+ * The operations below bring a prompt into a paged cache and keep the cache within bounds.  What is said above of buffers, modes,
+ * graphs, results and alignment holds for them as well.  Used together, chunk by chunk: dl_norm_rotate on the new tokens' queries and
+ * keys, dl_kv_write of their keys and values, dl_chunk_attention; then dl_kv_weigh with the last queries, dl_kv_evict, and decoding
+ * (dl_prefix_attention, or dl_chunk_attention again) on the pages that hold what was kept.
+ */
+
+/*
+ * Norms of queries and keys for each head, and the rotation by their tokens' positions, in one pass.  A row x (head_dim elements of one
+ * token and head) becomes
+ *   y = x * (1 / sqrt(mean of x^2 + eps)) * weight      (weight == null: y = x, no norm)
+ * and then, in its first `rotary` elements, y_a, y_b = y_a cos - y_b sin, y_b cos + y_a sin for each i < rotary / 2, with
+ * a, b = i, i + rotary / 2, or (neighbours) 2 i, 2 i + 1, and cos, sin = table[position][i], table[position][rotary / 2 + i].
+ * 32-bit until the result is rounded to its type.
+ * rotary == 0: no rotation; table and positions are not looked at.  A token whose position is negative or not below table_rows is
+ * left out: its rows of q_out and k_out stay as they are.
+ * q or k null: that side is left out.  An output may be its input, with the same strides; it overlaps nothing else that is read or
+ * written.
+ */
+typedef struct dl_norm_rotate_args {
+    const void *q, *k;            /* [tokens][q_heads or k_heads][head_dim], strides in elements, head_dim contiguous */
+    void *q_out, *k_out;          /* the same, with strides of their own */
+    const float *q_weight, *k_weight;  /* [head_dim], or null */
+    const float *table;           /* [table_rows][rotary], table_stride apart */
+    const int64_t *positions;     /* [tokens] */
+    int64_t tokens;               /* tokens * (q_heads + k_heads) <= DL_MAX_ROWS */
+    int64_t table_rows;           /* 0 .. 2^31 - 1 */
+    int64_t table_stride;
+    int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride;
+    int64_t q_out_token_stride, q_out_head_stride, k_out_token_stride, k_out_head_stride;
+    int32_t type;                 /* dl_type of q, k, q_out and k_out */
+    int32_t q_heads, k_heads;     /* 0 .. 65535 */
+    int32_t head_dim;             /* a multiple of 16, 16 .. 256 */
+    int32_t rotary;               /* a multiple of 16, 0 .. head_dim */
+    int32_t neighbours;           /* 0 or 1 */
+    float eps;                    /* >= 0 */
+    int32_t reserved;             /* 0 */
+} dl_norm_rotate_args;
+
+int dl_norm_rotate(const dl_norm_rotate_args *args, void *stream);
+
+/*
+ * Attention of chunks of new tokens over a paged cache.  The queries of all sequences lie packed in q: sequence b has the n rows
+ * q_starts[b] .. q_starts[b + 1] - 1 of it, and they are the last n of its lens[b] tokens, whose keys and values have been written
+ * before.  Query j in head h attends, in head h / (q_heads / cache heads) of the cache, to token i if i <= lens[b] - n + j; scores, out,
+ * lse and their types are those of dl_prefix_attention (with prefix_tokens == 0), and so is what it says of queries with nothing to attend
+ * to, lengths, pages that are none, scales of NaN and what lies behind the lengths.
+ * q_starts does not decrease, and entries count as 0 .. tokens; rows of out and lse that belong to no sequence stay as they are.
+ * Work is cut for chunks of many tokens; any number gives the result, for batches of thousands with little speed.
+ */
+typedef struct dl_chunk_attention_args {
+    const void *q;                /* [tokens][q_heads][head_dim], strides in elements, head_dim contiguous */
+    void *out;                    /* the same, with strides of its own */
+    float *lse;                   /* [tokens][q_heads], contiguous; or null */
+    const int32_t *q_starts;      /* [batch + 1] */
+    const int32_t *pages;         /* [batch][max_pages], pages_stride apart */
+    const int32_t *lens;          /* [batch] */
+    void *workspace;              /* dl_chunk_attention_workspace() bytes, 16-byte aligned; see dl_prefix_attention_workspace */
+    size_t workspace_bytes;
+    int64_t tokens;               /* tokens * q_heads <= DL_MAX_ROWS / 2 */
+    int64_t max_pages;            /* max_pages * page_tokens <= 2^30 */
+    int64_t pages_stride;
+    int64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride;
+    int32_t type;                 /* of q and out: DL_TYPE_BF16 or DL_TYPE_F16 */
+    int32_t batch;                /* 0 .. 65536 */
+    int32_t q_heads;              /* a multiple of the cache's heads */
+    float scale;                  /* what the scores are multiplied with */
+} dl_chunk_attention_args;
+
+int64_t dl_chunk_attention_workspace(const dl_kv_cache *cache, const dl_chunk_attention_args *args);
+int dl_chunk_attention(const dl_kv_cache *cache, const dl_chunk_attention_args *args, void *stream);
+
+/*
+ * What cached tokens have been given: with queries, sequences and scores as in dl_chunk_attention and the queries' lse,
+ *   weights[b][i] = before[b][i] + sum over the queries j and heads h of sequence b that attend to token i of e^(s_i - lse[j][h]),
+ * for all max_pages * page_tokens entries of a row (those behind lens[b] and those that nobody attends to become before[b][i]).
+ * before == null: zeros; before may be weights itself, with the same stride.  A query whose lse is no finite number gives nothing.  A
+ * token whose page is no page of the pool gets nothing; one whose scale is NaN gets NaN from those that attend to it.  Values play no
+ * part.  Sums are 32-bit.
+ */
+typedef struct dl_kv_weigh_args {
+    const void *q;                /* [tokens][q_heads][head_dim], strides in elements, head_dim contiguous */
+    const float *lse;             /* [tokens][q_heads], contiguous */
+    const int32_t *q_starts;      /* [batch + 1] */
+    const int32_t *pages;         /* [batch][max_pages], pages_stride apart */
+    const int32_t *lens;          /* [batch] */
+    const float *before;          /* [batch][max_pages * page_tokens], before_stride apart; or null */
+    float *weights;               /* the same, weights_stride apart */
+    void *workspace;              /* dl_kv_weigh_workspace() bytes, 16-byte aligned; see dl_prefix_attention_workspace */
+    size_t workspace_bytes;
+    int64_t tokens;               /* tokens * q_heads <= DL_MAX_ROWS / 2 */
+    int64_t max_pages;            /* max_pages * page_tokens <= 2^30, and times batch <= 2^31 - 1 */
+    int64_t pages_stride;
+    int64_t before_stride, weights_stride;
+    int64_t q_token_stride, q_head_stride;
+    int32_t type;                 /* of q: DL_TYPE_BF16 or DL_TYPE_F16 */
+    int32_t batch;                /* 0 .. 65536 */
+    int32_t q_heads;              /* a multiple of the cache's heads */
+    float scale;                  /* what the scores are multiplied with */
+} dl_kv_weigh_args;
+
+int64_t dl_kv_weigh_workspace(const dl_kv_cache *cache, const dl_kv_weigh_args *args);
+int dl_kv_weigh(const dl_kv_cache *cache, const dl_kv_weigh_args *args, void *stream);
+
+/*
+ * Eviction by weight.  Sequence b, of n = lens[b] tokens, is cut to m = min(n, keep): if n > keep, its first `first` tokens stay, its last
+ * `recent`, and those with the largest weights of the others (of equal ones the lowest; NaN counts as lighter than all numbers).
+ * In their order, they become tokens 0 .. m - 1 of the pages to_pages[b]: kept[b][j] is the token that the j-th was, and the codes and
+ * scales of its keys and values, all heads, are copied to place j % page_tokens of page to_pages[b][j / page_tokens].
+ * kept_lens[b] = m, kept_weights[b][j] = weights[b][kept[b][j]]; entries from m to keep - 1 become -1 and 0.
+ * The pages that are written differ from each other and from all that are read.  A token whose page is none of the pool, in either
+ * table, is not copied.  lens[b] counts as at least 0 and at most max_pages * page_tokens.
+ */
+typedef struct dl_kv_evict_args {
+    const float *weights;         /* [batch][max_pages * page_tokens], weights_stride apart */
+    const int32_t *pages;         /* [batch][max_pages], pages_stride apart */
+    const int32_t *lens;          /* [batch]; not kept_lens */
+    const int32_t *to_pages;      /* [batch][keep / page_tokens, rounded up], to_pages_stride apart */
+    int32_t *kept;                /* [batch][keep], contiguous */
+    int32_t *kept_lens;           /* [batch] */
+    float *kept_weights;          /* [batch][keep], kept_weights_stride apart; or null; overlaps nothing that is read */
+    void *workspace;              /* dl_kv_evict_workspace() bytes, 16-byte aligned; see dl_prefix_attention_workspace */
+    size_t workspace_bytes;
+    int64_t max_pages;            /* max_pages * page_tokens <= 2^30 */
+    int64_t pages_stride, to_pages_stride, weights_stride, kept_weights_stride;
+    int32_t batch;                /* 0 .. 65536 */
+    int32_t keep;                 /* batch * keep * cache heads <= DL_MAX_ROWS */
+    int32_t first, recent;        /* first + recent <= keep */
+} dl_kv_evict_args;
+
+int64_t dl_kv_evict_workspace(const dl_kv_cache *cache, const dl_kv_evict_args *args);
+int dl_kv_evict(const dl_kv_cache *cache, const dl_kv_evict_args *args, void *stream);
+
 /*
  * Host-only: lower a collective to the list of copies the device executes
  * (the analogue of building the command list, paper Sec. III-B2 "control").

@@ -19,4 +19,6 @@ from .binding import (  # noqa: F401
     dl_last_device_error, dl_debug_lose_next_table, dl_batch_copy_static, dl_plan_mode, dl_last_mode,
     dl_complete, dl_parse_config, dl_token_dispatch_device, DL_TYPE_F32, DL_TYPE_BF16, DL_TYPE_F16, DL_KV_FP8,
     DL_KV_INT8, DL_MAX_DRAFTS, DL_MAX_ROWS, KvCache, KvRows, PrefixAttention, DraftVerify, dl_kv_write, dl_kv_read, dl_prefix_attention,
-    dl_prefix_attention_workspace, dl_verify_draft, dl_verify_draft_workspace)
+    dl_prefix_attention_workspace, dl_verify_draft, dl_verify_draft_workspace, NormRotate, ChunkAttention, KvWeigh, KvEvict,
+    dl_norm_rotate, dl_chunk_attention, dl_chunk_attention_workspace, dl_kv_weigh, dl_kv_weigh_workspace, dl_kv_evict,
+    dl_kv_evict_workspace)

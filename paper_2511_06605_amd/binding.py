@@ -60,6 +60,8 @@ EXPORTS = [
     "dl_plan_mode", "dl_last_mode", "dl_complete", "dl_parse_config", "dl_token_dispatch_device",
     "dl_kv_write", "dl_kv_read", "dl_prefix_attention", "dl_prefix_attention_workspace", "dl_verify_draft",
     "dl_verify_draft_workspace",
+    "dl_norm_rotate", "dl_chunk_attention", "dl_chunk_attention_workspace", "dl_kv_weigh", "dl_kv_weigh_workspace", "dl_kv_evict",
+    "dl_kv_evict_workspace",
 ]
 
 
@@ -158,6 +160,58 @@ class VerifyDraftDesc(ctypes.Structure):
     ]
 
 
+class NormRotateDesc(ctypes.Structure):
+    """dl_norm_rotate_args"""
+    _fields_ = [
+        ("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("q_out", ctypes.c_void_p), ("k_out", ctypes.c_void_p),
+        ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("table", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+        ("tokens", ctypes.c_int64), ("table_rows", ctypes.c_int64), ("table_stride", ctypes.c_int64),
+        ("q_token_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64),
+        ("k_token_stride", ctypes.c_int64), ("k_head_stride", ctypes.c_int64),
+        ("q_out_token_stride", ctypes.c_int64), ("q_out_head_stride", ctypes.c_int64),
+        ("k_out_token_stride", ctypes.c_int64), ("k_out_head_stride", ctypes.c_int64),
+        ("type", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("k_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+        ("rotary", ctypes.c_int32), ("neighbours", ctypes.c_int32), ("eps", ctypes.c_float), ("reserved", ctypes.c_int32),
+    ]
+
+
+class ChunkAttentionDesc(ctypes.Structure):
+    """dl_chunk_attention_args"""
+    _fields_ = [
+        ("q", ctypes.c_void_p), ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p), ("q_starts", ctypes.c_void_p),
+        ("pages", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+        ("tokens", ctypes.c_int64), ("max_pages", ctypes.c_int64), ("pages_stride", ctypes.c_int64),
+        ("q_token_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64),
+        ("out_token_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64),
+        ("type", ctypes.c_int32), ("batch", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("scale", ctypes.c_float),
+    ]
+
+
+class KvWeighDesc(ctypes.Structure):
+    """dl_kv_weigh_args"""
+    _fields_ = [
+        ("q", ctypes.c_void_p), ("lse", ctypes.c_void_p), ("q_starts", ctypes.c_void_p), ("pages", ctypes.c_void_p),
+        ("lens", ctypes.c_void_p), ("before", ctypes.c_void_p), ("weights", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+        ("tokens", ctypes.c_int64), ("max_pages", ctypes.c_int64), ("pages_stride", ctypes.c_int64),
+        ("before_stride", ctypes.c_int64), ("weights_stride", ctypes.c_int64),
+        ("q_token_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64),
+        ("type", ctypes.c_int32), ("batch", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("scale", ctypes.c_float),
+    ]
+
+
+class KvEvictDesc(ctypes.Structure):
+    """dl_kv_evict_args"""
+    _fields_ = [
+        ("weights", ctypes.c_void_p), ("pages", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("to_pages", ctypes.c_void_p),
+        ("kept", ctypes.c_void_p), ("kept_lens", ctypes.c_void_p), ("kept_weights", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+        ("max_pages", ctypes.c_int64), ("pages_stride", ctypes.c_int64), ("to_pages_stride", ctypes.c_int64),
+        ("weights_stride", ctypes.c_int64), ("kept_weights_stride", ctypes.c_int64),
+        ("batch", ctypes.c_int32), ("keep", ctypes.c_int32), ("first", ctypes.c_int32), ("recent", ctypes.c_int32),
+    ]
+
+
 _lib = None
 _marshal = None
 
@@ -241,6 +295,13 @@ def lib() -> ctypes.CDLL:
         "dl_prefix_attention_workspace": (ctypes.c_int64, [vp, vp]),
         "dl_verify_draft": (ctypes.c_int, [vp, vp]),
         "dl_verify_draft_workspace": (ctypes.c_int64, [vp]),
+        "dl_norm_rotate": (ctypes.c_int, [vp, vp]),
+        "dl_chunk_attention": (ctypes.c_int, [vp, vp, vp]),
+        "dl_chunk_attention_workspace": (ctypes.c_int64, [vp, vp]),
+        "dl_kv_weigh": (ctypes.c_int, [vp, vp, vp]),
+        "dl_kv_weigh_workspace": (ctypes.c_int64, [vp, vp]),
+        "dl_kv_evict": (ctypes.c_int, [vp, vp, vp]),
+        "dl_kv_evict_workspace": (ctypes.c_int64, [vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -484,7 +545,7 @@ def _expect(t, what, dtype, shape, packed=False):
         raise ValueError(f"{what}: not in device memory")
     if packed and not t.is_contiguous():
         raise ValueError(f"{what}: must be contiguous")
-    if not packed and t.shape[-1] > 1 and t.stride()[-1] != 1:
+    if not packed and t.numel() and t.shape[-1] > 1 and t.stride()[-1] != 1:
         raise ValueError(f"{what}: its last dimension must be contiguous")
     return _addr(t)
 
@@ -650,6 +711,161 @@ def dl_verify_draft_workspace(request: DraftVerify) -> int:
 
 def dl_verify_draft(request: DraftVerify, stream=None) -> None:
     _check(lib().dl_verify_draft(request.at, _stream(stream)), "dl_verify_draft")
+
+
+# ------------------------------------------- a prompt on its way into a bounded cache
+
+class NormRotate(_Request):
+    """A call of dl_norm_rotate: q [tokens, q_heads, head_dim] and k [tokens, k_heads, head_dim] of float32, bfloat16 or float16 (either may
+    be None), q_out and k_out like them (they themselves if None), weights [head_dim] of float32 (None: no norm on that side), table
+    [positions, rotary] of float32 (cosines, then sines; None: no rotation), positions [tokens] of int64."""
+
+    def __init__(self, q, k, q_out=None, k_out=None, q_weight=None, k_weight=None, eps=1e-6, table=None, positions=None, neighbours=False):
+        some = q if q is not None else k
+        if some is None:
+            raise ValueError("neither queries nor keys")
+        if len(some.shape) != 3:
+            raise ValueError("rows have three dimensions: tokens, heads, head_dim")
+        T, D = int(some.shape[0]), int(some.shape[2])
+        d = NormRotateDesc(tokens=T, type=_TYPES.get(_dtype(some), -1), head_dim=D, neighbours=1 if neighbours else 0, eps=float(eps))
+        for name, x, y, w in (("q", q, q_out, q_weight), ("k", k, k_out, k_weight)):
+            if x is None:
+                if y is not None or w is not None:
+                    raise ValueError(f"{name}_out or {name}_weight, but no {name}")
+                continue
+            setattr(d, name, _expect(x, name, _TYPES if x is some else _dtype(some), (T, None, D)))
+            y = x if y is None else y
+            setattr(d, name + "_out", _expect(y, name + "_out", _dtype(some), (T, x.shape[1], D)))
+            setattr(d, name + "_heads", int(x.shape[1]))
+            for side, t in (("", x), ("_out", y)):
+                step = _strides(t)
+                setattr(d, f"{name}{side}_token_stride", step[0])
+                setattr(d, f"{name}{side}_head_stride", step[1])
+            if w is not None:
+                setattr(d, name + "_weight", _expect(w, name + "_weight", "float32", (D,), packed=True))
+        if table is not None:
+            if positions is None:
+                raise ValueError("a table, but no positions")
+            d.table = _expect(table, "table", "float32", (None, None))
+            d.table_rows, d.rotary = int(table.shape[0]), int(table.shape[1])
+            d.table_stride = _strides(table)[0]
+            d.positions = _expect(positions, "positions", "int64", (T,), packed=True)
+        self._hold(d, q, k, q_out, k_out, q_weight, k_weight, table, positions)
+
+
+def _packed_queries(d, cache, q, q_starts, pages, lens, scale):
+    """What dl_chunk_attention and dl_kv_weigh have in common."""
+    shape = tuple(int(n) for n in q.shape)
+    if len(shape) != 3:
+        raise ValueError("q has three dimensions: tokens, q_heads, head_dim")
+    T, H, D = shape
+    if D != cache.desc.head_dim:
+        raise ValueError(f"q: head_dim {D}, the cache has {cache.desc.head_dim}")
+    B = int(lens.shape[0])
+    d.q, d.type = _expect(q, "q", ("bfloat16", "float16"), shape), _TYPES[_dtype(q)]
+    d.q_starts = _expect(q_starts, "q_starts", "int32", (B + 1,), packed=True)
+    d.pages = _expect(pages, "pages", "int32", (B, None))
+    d.lens = _expect(lens, "lens", "int32", (B,), packed=True)
+    d.tokens, d.q_heads, d.batch = T, H, B
+    d.max_pages, d.pages_stride = int(pages.shape[1]), _strides(pages)[0]
+    d.q_token_stride, d.q_head_stride = _strides(q)[:2]
+    d.scale = D ** -0.5 if scale is None else float(scale)
+    return shape
+
+
+class ChunkAttention(_Request):
+    """A call of dl_chunk_attention: q and out [tokens, q_heads, head_dim] of bfloat16 or float16, q_starts [batch + 1], pages [batch, max_pages]
+    and lens [batch] of int32, lse [tokens, q_heads] of float32.  scale: 1 / sqrt(head_dim) if None."""
+
+    def __init__(self, cache, q, out, q_starts, pages, lens, lse=None, scale=None):
+        d = ChunkAttentionDesc()
+        shape = _packed_queries(d, cache, q, q_starts, pages, lens, scale)
+        d.out = _expect(out, "out", _dtype(q), shape)
+        d.out_token_stride, d.out_head_stride = _strides(out)[:2]
+        if lse is not None:
+            d.lse = _expect(lse, "lse", "float32", shape[:2], packed=True)
+        self.cache = cache
+        self._hold(d, q, out, q_starts, pages, lens, lse)
+
+
+class KvWeigh(_Request):
+    """A call of dl_kv_weigh: q [tokens, q_heads, head_dim] of bfloat16 or float16, lse [tokens, q_heads] of float32, q_starts [batch + 1], pages
+    [batch, max_pages] and lens [batch] of int32, weights and before [batch, max_pages * page_tokens] of float32 (before may be weights; None:
+    zeros).  scale: 1 / sqrt(head_dim) if None."""
+
+    def __init__(self, cache, q, lse, q_starts, pages, lens, weights, before=None, scale=None):
+        d = KvWeighDesc()
+        shape = _packed_queries(d, cache, q, q_starts, pages, lens, scale)
+        d.lse = _expect(lse, "lse", "float32", shape[:2], packed=True)
+        row = (d.batch, d.max_pages * cache.desc.page_tokens)
+        d.weights = _expect(weights, "weights", "float32", row)
+        d.weights_stride = _strides(weights)[0]
+        if before is not None:
+            d.before = _expect(before, "before", "float32", row)
+            d.before_stride = _strides(before)[0]
+        self.cache = cache
+        self._hold(d, q, lse, q_starts, pages, lens, weights, before)
+
+
+class KvEvict(_Request):
+    """A call of dl_kv_evict: weights [batch, max_pages * page_tokens] of float32, pages [batch, max_pages], lens [batch] and to_pages
+    [batch, keep / page_tokens rounded up (or more)] of int32; kept [batch, keep] and kept_lens [batch] of int32 and kept_weights [batch, keep]
+    of float32 (or None) are written."""
+
+    def __init__(self, cache, weights, pages, lens, to_pages, kept, kept_lens, kept_weights=None, first=0, recent=0):
+        if len(kept.shape) != 2:
+            raise ValueError("kept has two dimensions: batch, keep")
+        B, keep, page = int(lens.shape[0]), int(kept.shape[1]), cache.desc.page_tokens
+        d = KvEvictDesc(batch=B, keep=keep, first=int(first), recent=int(recent), max_pages=int(pages.shape[1]))
+        d.pages = _expect(pages, "pages", "int32", (B, None))
+        d.lens = _expect(lens, "lens", "int32", (B,), packed=True)
+        d.weights = _expect(weights, "weights", "float32", (B, d.max_pages * page))
+        d.to_pages = _expect(to_pages, "to_pages", "int32", (B, None))
+        if int(to_pages.shape[1]) < -(-keep // page):
+            raise ValueError(f"to_pages: {int(to_pages.shape[1])} pages of {page}, {keep} tokens are kept")
+        d.kept = _expect(kept, "kept", "int32", (B, keep), packed=True)
+        d.kept_lens = _expect(kept_lens, "kept_lens", "int32", (B,), packed=True)
+        d.pages_stride, d.to_pages_stride, d.weights_stride = _strides(pages)[0], _strides(to_pages)[0], _strides(weights)[0]
+        if kept_weights is not None:
+            d.kept_weights = _expect(kept_weights, "kept_weights", "float32", (B, keep))
+            d.kept_weights_stride = _strides(kept_weights)[0]
+        self.cache = cache
+        self._hold(d, weights, pages, lens, to_pages, kept, kept_lens, kept_weights)
+
+
+def dl_norm_rotate(request: NormRotate, stream=None) -> None:
+    """Norms of queries and keys for each head, and the rotation by position, in one pass."""
+    _check(lib().dl_norm_rotate(request.at, _stream(stream)), "dl_norm_rotate")
+
+
+def dl_chunk_attention_workspace(request: ChunkAttention) -> int:
+    """Bytes of workspace a call needs."""
+    return _size(lib().dl_chunk_attention_workspace(request.cache.at, request.at), "dl_chunk_attention_workspace")
+
+
+def dl_chunk_attention(request: ChunkAttention, stream=None) -> None:
+    """Attention of chunks of new tokens, packed sequence behind sequence, over the cache."""
+    _check(lib().dl_chunk_attention(request.cache.at, request.at, _stream(stream)), "dl_chunk_attention")
+
+
+def dl_kv_weigh_workspace(request: KvWeigh) -> int:
+    """Bytes of workspace a call needs."""
+    return _size(lib().dl_kv_weigh_workspace(request.cache.at, request.at), "dl_kv_weigh_workspace")
+
+
+def dl_kv_weigh(request: KvWeigh, stream=None) -> None:
+    """Adds what the queries give to every cached token to what it has been given before."""
+    _check(lib().dl_kv_weigh(request.cache.at, request.at, _stream(stream)), "dl_kv_weigh")
+
+
+def dl_kv_evict_workspace(request: KvEvict) -> int:
+    """Bytes of workspace a call needs."""
+    return _size(lib().dl_kv_evict_workspace(request.cache.at, request.at), "dl_kv_evict_workspace")
+
+
+def dl_kv_evict(request: KvEvict, stream=None) -> None:
+    """Cuts sequences to the tokens that have been given most, which move to other pages."""
+    _check(lib().dl_kv_evict(request.cache.at, request.at, _stream(stream)), "dl_kv_evict")
 
 
 # -------------------------------------------------------------------- prelaunch

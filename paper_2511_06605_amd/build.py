@@ -13,7 +13,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdmalatte.so")
 # (with the tag of the Python it is built for: no other one loads it)
 MARSHAL = os.path.join(HERE, "_marshal" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
-SOURCES = ["dl_api.hip", "dl_exec.hip", "dl_prelaunch.hip", "dl_dispatch.hip", "dl_static.hip", "dl_kv.hip", "dl_attention.hip", "dl_verify.hip"]
+SOURCES = ["dl_api.hip", "dl_exec.hip", "dl_prelaunch.hip", "dl_dispatch.hip", "dl_static.hip", "dl_kv.hip", "dl_attention.hip", "dl_verify.hip",
+           "dl_norm.hip", "dl_chunk.hip", "dl_weigh.hip", "dl_evict.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-fno-gpu-rdc",

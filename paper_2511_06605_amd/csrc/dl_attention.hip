@@ -2,7 +2,7 @@
 //
 // With s the scores in units of ln 2 and u the scales of the values, a query's output is sum of 2^s u V / sum of 2^s over the codes V
 // of what it sees.  A scale is taken apart, u = c d, with c within 2^-40 .. 2^40 (2^50 for float16) and d = 1 for all but rows
-// of zeros and values of very unusual sizes (see value_scale).  The sums are taken piece by piece with a running reference r, within 2^8 of
+// of zeros and values of very unusual sizes (see dl_value_scale).  The sums are taken piece by piece with a running reference r, within 2^8 of
 // the largest s + log2 c so far:
 //   w = 2^(s + log2 c - r) <= 2^8,   O += w d V,   l += w / c,
 // both multiplied by 2^(r before - r) when r grows.  So the weights that go to the matrix units in 16 bits are at most 2^8 (times 2^lift,
@@ -62,18 +62,6 @@ __device__ __forceinline__ uint32_t queries(const att_args &a, uint32_t b)
     return a.q_lens ? min((uint32_t)max(a.q_lens[b], 0), a.q_tokens) : a.q_tokens;
 }
 
-// x + the lanes before it; lane 63 ends with the sum of all.
-__device__ __forceinline__ uint32_t sum_up_to(uint32_t x)
-{
-    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xF, 0xF, false);  // row_shr:1, 2, 4, 8
-    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xF, 0xF, false);
-    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xF, 0xF, false);
-    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xF, 0xF, false);
-    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xA, 0xF, false);  // row_bcast:15, 31
-    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xC, 0xF, false);
-    return x;
-}
-
 // The sequences' own tokens are cut by their lengths, which only the device knows: into pieces of as many steps (of STEP keys)
 // as share the steps of all sequences out over own_target pieces.  Sequences are then of one or more pieces, own_target + batch
 // in all at most, and unit n is the n-th of them.  Every wavefront works this out from the lengths for itself.
@@ -99,13 +87,13 @@ __device__ __forceinline__ bool own_unit(const att_args &a, uint32_t unit, own_p
     uint32_t all = 0, here = 0;
     for (uint32_t b0 = 0; b0 < a.batch; b0 += 64u) {
         here = b0 + lane < a.batch ? steps_of(b0 + lane) : 0u;
-        all += (uint32_t)__builtin_amdgcn_readlane((int)sum_up_to(here), 63);
+        all += (uint32_t)__builtin_amdgcn_readlane((int)dl_sum_up_to(here), 63);
     }
     const uint32_t size = max((all + a.own_target - 1u) / a.own_target, OWN_LEAST_STEPS);
     uint32_t before = 0;
     for (uint32_t b0 = 0; b0 < a.batch; b0 += 64u) {
         if (a.batch > 64u) here = b0 + lane < a.batch ? steps_of(b0 + lane) : 0u;
-        const uint32_t pieces = (here + size - 1u) / size, up_to = before + sum_up_to(pieces);
+        const uint32_t pieces = (here + size - 1u) / size, up_to = before + dl_sum_up_to(pieces);
         const unsigned long long where = __ballot(up_to > unit);
         if (where) {
             const int l = __ffsll((long long)where) - 1;
@@ -120,16 +108,6 @@ __device__ __forceinline__ bool own_unit(const att_args &a, uint32_t unit, own_p
     return false;
 }
 
-// A vector of N bytes, N = 4, 8, 16, as words
-template <int N>
-struct words {
-    uint32_t w[N / 4];
-};
-template <int N>
-__device__ __forceinline__ words<N> load_words(const char *p)
-{
-    return dl_load_at<words<N>>(p);
-}
 // The largest over the lanes that hold the same query (16 and 32 apart), in all of them: halves and quarters change places.
 __device__ __forceinline__ float largest_of_quarters(float x)
 {
@@ -138,29 +116,6 @@ __device__ __forceinline__ float largest_of_quarters(float x)
     const auto b = __builtin_amdgcn_permlane16_swap(dl_bits<uint32_t>(y), dl_bits<uint32_t>(y), false, false);
     return fmaxf(dl_bits<float>((uint32_t)b[0]), dl_bits<float>((uint32_t)b[1]));
 }
-
-// A value's scale u = c d for the sums, d a power of two.  c: what log2 u and 1 / u are taken of, so that neither they nor a product with
-// 2^(log2 u) or 1 / u leave the range of 32 bits, however far apart the scales of the rows are that a query sees.  d: 1, or what that
-// leaves out; it goes to the product with the values alone (never to l), and is finite, so that a weight of zero takes it out.
-// Scales below 2^-126 (dl_kv_write gives 2^-100 / 448 and more) count as zero, and so do negative ones.  A NaN stays in c.
-template <class Q>
-struct value_scale {
-    float c, d;
-    __device__ __forceinline__ explicit value_scale(float u)
-    {
-        constexpr float LOW = 0x1p-40f, HIGH = Q::scale_most;
-        // u's power of two (none for what is no positive number, infinite for infinities), and what it is more than the limit's
-        const float power = dl_bits<float>(dl_bits<uint32_t>(fmaxf(u, 0.0f)) & 0x7F800000u);
-        const bool low = u < LOW, high = u >= 2.0f * HIGH;
-        d = low ? power * (1.0f / LOW) : high ? fminf(power, 0x1p127f) * (1.0f / HIGH) : 1.0f;
-        // (the mantissa of u with the limit's power)
-        const float c_limit = dl_bits<float>((dl_bits<uint32_t>(u) & 0x007FFFFFu) | dl_bits<uint32_t>(low ? LOW : HIGH));
-        c = low || high ? c_limit : u;
-    }
-    __device__ __forceinline__ float log2_c() const { return __builtin_amdgcn_logf(c); }
-    // (finite for a NaN as well: its readers' weights have it from the logarithm)
-    __device__ __forceinline__ float over_c() const { return __builtin_amdgcn_rcpf(c == c ? c : 1.0f); }
-};
 
 // What is the same for a workgroup's whole piece: NT tiles of 16 rows against the keys first .. end - 1 of one head.
 struct piece_args {
@@ -206,12 +161,12 @@ struct place {
 // nobody stores.)
 template <int DP>
 struct tile_keys {
-    words<16> k[2][DP / 64];  // dims 64 s + 16 g ..
+    dl_words<16> k[2][DP / 64];  // dims 64 s + 16 g ..
     float scale;
 };
 template <int DP>
 struct tile_values {
-    words<DP / 16> v[8];  // dims DP / 16 * i ..
+    dl_words<DP / 16> v[8];  // dims DP / 16 * i ..
     uint32_t dead;        // bit e: the page of key 8 g + e
 };
 
@@ -229,7 +184,7 @@ __device__ __forceinline__ void load_keys(const att_args &a, const piece_args &p
         else
             kp += 4ull * a.c.token_stride;
 #pragma unroll
-        for (int s = 0; s < DP / 64; ++s) td.k[t][s] = load_words<16>((const char *)kp + min(16u * g + 64u * s, D - 16u));
+        for (int s = 0; s < DP / 64; ++s) td.k[t][s] = dl_load_words<16>((const char *)kp + min(16u * g + 64u * s, D - 16u));
     }
     const uint64_t scales = (uint64_t)(i < 8u ? a.c.k_scale : a.c.v_scale) + (uint64_t)p.head * a.c.scale_head_stride;
     td.scale = *(const float *)at.offset(a, p, g, i % 8u, at.value_page, a.c.scale_page_stride, a.c.scale_token_stride, scales, &alive);
@@ -252,7 +207,7 @@ __device__ __forceinline__ void load_values(const att_args &a, const piece_args 
         } else {
             vp += a.c.token_stride;
         }
-        td.v[e] = load_words<VB>((const char *)vp);
+        td.v[e] = dl_load_words<VB>((const char *)vp);
     }
 }
 
@@ -285,7 +240,7 @@ __device__ __forceinline__ void attend_tile(const att_args &a, const piece_args 
             here = (left >= 8u ? 0xFFu : (1u << left) - 1u) & ~tv.dead;
         }
         const uint32_t key = 8u * g + i % 8u;
-        const value_scale<Q> u(tk.scale);
+        const dl_value_scale<Q> u(tk.scale);
         if (i < 8u) {
             scales[0][key] = tk.scale * a.scale;
         } else {
@@ -362,7 +317,7 @@ __device__ __forceinline__ void attend_tile(const att_args &a, const piece_args 
     if (!whole) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            if (!(here >> e & 1u)) tv.v[e] = words<VB>{};
+            if (!(here >> e & 1u)) tv.v[e] = dl_words<VB>{};
     }
 #pragma unroll
     for (int q4 = 0; q4 < VB / 4; ++q4) {
@@ -625,13 +580,13 @@ __device__ __forceinline__ void wide_piece(const att_args &a, uint32_t block, wi
                                      page * a.c.scale_page_stride + (uint64_t)in * a.c.scale_token_stride);
         }
     };
-    words<8> kw[K_LOADS];
+    dl_words<8> kw[K_LOADS];
     uint32_t vw[V_LOADS][8];
     auto load = [&](uint32_t from) {
 #pragma unroll
         for (uint32_t x = 0; x < K_LOADS; ++x) {
             const uint32_t at = threadIdx.x + x * ATT_THREADS, key = at / PIECES, d = at % PIECES * 8u;
-            kw[x] = load_words<8>(k_from + rows_at[from][key] + min(d, D - 8u));
+            kw[x] = dl_load_words<8>(k_from + rows_at[from][key] + min(d, D - 8u));
         }
 #pragma unroll
         for (uint32_t x = 0; x < V_LOADS; ++x) {
@@ -650,7 +605,7 @@ __device__ __forceinline__ void wide_piece(const att_args &a, uint32_t block, wi
         if (all != ~0ull) {  // what is none counts as zero
 #pragma unroll
             for (uint32_t x = 0; x < K_LOADS; ++x)
-                if (!(all >> ((threadIdx.x + x * ATT_THREADS) / PIECES) & 1u)) kw[x] = words<8>{};
+                if (!(all >> ((threadIdx.x + x * ATT_THREADS) / PIECES) & 1u)) kw[x] = dl_words<8>{};
 #pragma unroll
             for (uint32_t x = 0; x < V_LOADS; ++x) {
                 const uint32_t part = (threadIdx.x + x * ATT_THREADS) / (DP / 4) % 8u, key = part / 2u * 16u + part % 2u * 4u;
@@ -689,7 +644,7 @@ __device__ __forceinline__ void wide_piece(const att_args &a, uint32_t block, wi
         if (wave == 0) {
             to.ks[lane] = alive ? scale * a.scale : 0.0f;
         } else if (wave == 1) {
-            const value_scale<Q> u(scale);
+            const dl_value_scale<Q> u(scale);
             to.lu[lane] = alive ? u.log2_c() : -INFINITY;
             to.iu[lane] = alive ? u.over_c() : 0.0f;
             to.d[lane] = u.d;

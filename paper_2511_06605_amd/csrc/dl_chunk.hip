@@ -1,0 +1,541 @@
+// Attention of chunks of new tokens over a paged cache in 8 bits (dl_chunk_attention).
+//
+// The sums are those of dl_attention.hip: with s the scores in units of ln 2 and u = c d a value's scale taken apart (dl_value_scale),
+// w = 2^(s + log2 c - r) <= 2^(8 + lift), O += w d V, l += w / c, with a reference r that follows the largest s + log2 c.
+//
+// The queries that share a head of the cache are the rows of a sequence: row j * group + g is query j in the g-th of those heads.  A
+// workgroup has a tile of 128 rows (32 a wavefront) and walks the keys that its last row sees in steps of 64, which its wavefronts share:
+// codes are turned into elements of Q once, on their way into LDS, keys as rows and values transposed, so that every operand of the
+// 32 x 32 x 16 products is one 16-byte read.  While a step is worked on, the next one's codes are on their way to registers and the pages
+// of the one after it are looked up.  Masks cost something only where a wavefront's rows end.
+#include "dl_codes.h"
+#include "dl_internal.h"
+#include "dl_packed.h"
+
+namespace {
+
+constexpr uint32_t CH_THREADS = 256, CH_WAVES = CH_THREADS / 64;
+constexpr uint32_t CH_ROWS = 32 * CH_WAVES;
+constexpr uint32_t CH_KEYS = 64;
+
+struct chunk_args {
+    dl_cache_view c;
+    dl_packed p;
+    const char *q;
+    char *out;
+    float *lse;
+    // What pieces leave behind for the join, by slot, head and row of the tile
+    dl_f32x2 *rl;    // r and l
+    float *partial;  // head_dim sums
+    int64_t q_token, q_head, out_token, out_head;  // bytes
+    uint32_t q_heads, group;
+    uint32_t target;  // see chunk_plan; 0: a piece a tile
+    float scale;      // times log2 e
+};
+
+// The key axis of a sequence is cut into pieces where there are few tiles, by the lengths, which only the device knows: into pieces of as
+// many steps as share the steps of all tiles out over `target` pieces.  All tiles of a sequence are cut alike, at multiples of `keys`; a
+// tile whose rows end before a piece begins has nothing of it.  With T steps in all a piece has T / target or more, so tiles that are
+// cut have no more than 2 target pieces between them: as many slots there are, and no more than target such tiles.
+// Every wavefront works this out from the lengths for itself.
+constexpr uint32_t LEAST_STEPS = 4;
+
+struct chunk_place {
+    uint32_t b, tile, piece, pieces, keys;
+    uint32_t slot;  // of this piece; the others of the tile lie next to it
+};
+__device__ __forceinline__ uint32_t tiles_of(const chunk_args &a, uint32_t b)
+{
+    const uint32_t first = a.p.start(b);
+    return (a.p.queries(b, first) * a.group + CH_ROWS - 1u) / CH_ROWS;
+}
+__device__ __forceinline__ uint32_t steps_of(const chunk_args &a, uint32_t b) { return (a.p.len(b) + CH_KEYS - 1u) / CH_KEYS; }
+
+// The unit-th piece of all (CUT: the unit-th tile of those that are cut, its first piece); false: there is none.
+template <bool CUT>
+__device__ __forceinline__ bool chunk_unit(const chunk_args &a, uint32_t unit, chunk_place *at)
+{
+    const uint32_t lane = threadIdx.x % 64u;
+    uint32_t size = 1u << 26, tiles = 0, steps = 0;
+    if (a.target) {
+        uint64_t all = 0;
+        for (uint32_t b0 = 0; b0 < a.p.batch; b0 += 64u) {
+            const bool there = b0 + lane < a.p.batch;
+            tiles = there ? tiles_of(a, b0 + lane) : 0u;
+            steps = there ? steps_of(a, b0 + lane) : 0u;
+            uint64_t x = (uint64_t)tiles * steps;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) x += (uint64_t)__shfl_xor((unsigned long long)x, d);
+            all += x;
+        }
+        size = max((uint32_t)((all + a.target - 1u) / a.target), LEAST_STEPS);
+    }
+    uint32_t before = 0, slots = 0;
+    for (uint32_t b0 = 0; b0 < a.p.batch; b0 += 64u) {
+        if (a.p.batch > 64u || !a.target) {
+            const bool there = b0 + lane < a.p.batch;
+            tiles = there ? tiles_of(a, b0 + lane) : 0u;
+            steps = there ? steps_of(a, b0 + lane) : 0u;
+        }
+        const uint32_t pieces = max((steps + size - 1u) / size, 1u), cut = pieces > 1u ? tiles * pieces : 0u;
+        const uint32_t counted = CUT ? (pieces > 1u ? tiles : 0u) : tiles * pieces;
+        const uint32_t up_to = before + dl_sum_up_to(counted), slots_up_to = slots + dl_sum_up_to(cut);
+        const unsigned long long where = __ballot(up_to > unit);
+        if (where) {
+            const int l = __ffsll((long long)where) - 1;
+            auto of = [&](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, l); };
+            const uint32_t n = unit - (of(up_to) - of(counted)), its = of(pieces), its_steps = of(steps);
+            if (n >= of(counted)) return false;  // (starts that decrease may count more tiles than 32 bits hold)
+            at->b = b0 + (uint32_t)l;
+            at->pieces = its;
+            // even shares of the steps: no piece is longer than `size`
+            at->keys = (its_steps + its - 1u) / its * CH_KEYS;
+            // (the last tile first: it sees the most)
+            at->tile = of(tiles) - 1u - (CUT ? n : n / its);
+            at->piece = CUT ? 0u : n % its;
+            at->slot = of(slots_up_to) - of(cut) + (CUT ? n * its : n);
+            return true;
+        }
+        before = (uint32_t)__builtin_amdgcn_readlane((int)up_to, 63);
+        slots = (uint32_t)__builtin_amdgcn_readlane((int)slots_up_to, 63);
+    }
+    return false;
+}
+
+// A tile's rows: where they are, and what they see.
+struct chunk_rows {
+    uint32_t first, row0, rows;  // first row of q, the tile's first row, rows of the sequence
+    int32_t ahead;               // row r sees the keys up to ahead + r / group
+    uint32_t end;                // keys that some row of the tile sees
+
+    __device__ __forceinline__ chunk_rows(const chunk_args &a, const chunk_place &at)
+    {
+        first = a.p.start(at.b);
+        const uint32_t n = a.p.queries(at.b, first), len = a.p.len(at.b);
+        rows = n * a.group;
+        row0 = at.tile * CH_ROWS;
+        ahead = (int32_t)len - (int32_t)n;
+        end = seen_by(a, min(row0 + CH_ROWS, rows) - 1u);
+    }
+    __device__ __forceinline__ uint32_t seen_by(const chunk_args &a, uint32_t row) const { return (uint32_t)max(ahead + (int32_t)(row / a.group) + 1, 0); }
+};
+
+template <int DP>
+struct alignas(16) chunk_tile {  // (reads of 16 bytes that lie at fours take twice as long)
+    uint32_t k[CH_KEYS * DP / 2];  // key, dim
+    uint32_t v[CH_KEYS * DP / 2];  // dim, key: of each 16 keys 0 - 3, 8 - 11, 4 - 7, 12 - 15
+    float ks[CH_KEYS], lu[CH_KEYS], iu[CH_KEYS], d[CH_KEYS];
+    uint32_t taken_apart;  // some value's d is not 1
+};
+template <int DP>
+struct chunk_lds {
+    chunk_tile<DP> tiles[2];
+    uint64_t rows_at[2][CH_KEYS];  // offsets of the codes' rows
+    uint64_t alive_at[2];          // bit k: key k is one of the piece, in a page of the pool
+};
+
+// Operands lie in rows of 16-byte pieces, whose places are exchanged (by an exclusive or with the row's number) so that eight
+// neighbouring lanes use all banks, in reads and in writes.
+template <class Q, class C, int DP>
+__global__ void __launch_bounds__(CH_THREADS, DP <= 128 ? 2 : 1) dl_chunk_kernel(const chunk_args a)
+{
+    constexpr uint32_t PIECES = DP / 8;                          // 16-byte pieces of a key's row
+    constexpr uint32_t K_LOADS = CH_KEYS * PIECES / CH_THREADS;  // of 8 codes
+    constexpr uint32_t V_ITEMS = 8 * (DP / 4);                   // 8 keys (half of 16) x 4 dims
+    constexpr uint32_t V_LOADS = (V_ITEMS + CH_THREADS - 1) / CH_THREADS;
+    __shared__ chunk_lds<DP> lds;
+    auto &tiles = lds.tiles;
+    auto &rows_at = lds.rows_at;
+    auto &alive_at = lds.alive_at;
+    const uint32_t lane = threadIdx.x % 64u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
+    const uint32_t i = lane % 32u, half = lane / 32u, D = a.c.head_dim, head = blockIdx.x % a.c.heads;
+    chunk_place at;
+    if (!chunk_unit<false>(a, blockIdx.x / a.c.heads, &at)) return;
+    const chunk_rows t(a, at);
+    const uint32_t first = at.piece * at.keys, end = min(first + at.keys, t.end);
+    if (at.piece && first >= end) return;
+    const int32_t *const table = a.p.pages + at.b * a.p.pages_stride;
+    const char *const k_from = a.c.k + (int64_t)head * a.c.head_stride, *const v_from = a.c.v + (int64_t)head * a.c.head_stride;
+
+    const uint32_t wave_row = t.row0 + wave * 32u, my = wave_row + i, row = min(my, t.rows - 1u);
+    const uint32_t j = row / a.group, h = head * a.group + row - j * a.group;
+    const int32_t last = t.ahead + (int32_t)j;
+    // keys before whole_end are seen by all rows of the wavefront, those from wave_end on by none
+    const uint32_t wave_end = wave_row < t.rows ? min(t.seen_by(a, min(wave_row + 32u, t.rows) - 1u), end) : 0u;
+    const uint32_t whole_end = wave_row < t.rows ? t.seen_by(a, wave_row) : 0u;
+    const char *const q = a.q + (uint64_t)(t.first + j) * a.q_token + h * a.q_head;
+    dl_u32x4 qf[DP / 16];
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) qf[s] = 16u * s < D ? dl_load_at<dl_u32x4>(q + 2u * (16u * s + 8u * half)) : dl_u32x4{0, 0, 0, 0};
+
+    // a key's page: looked up by the first two wavefronts, for the keys' and the values' scales; the first hands the rows on
+    uint32_t looked_up = 0;
+    auto look_up = [&](uint32_t base) {
+        if (wave < 2) looked_up = (uint32_t)table[dl_divide(min(base + lane, end - 1u), a.c.page)];
+    };
+    float scale = 0.0f;
+    bool alive = false;
+    auto hand_on = [&](uint32_t base, uint32_t to) {  // what was looked up for the step at base
+        if (wave < 2) {
+            const uint32_t key = min(base + lane, end - 1u), in = key - dl_divide(key, a.c.page) * a.c.page.d;
+            alive = base + lane < end && looked_up < a.c.pages;
+            const uint64_t page = looked_up < a.c.pages ? looked_up : 0u;
+            if (wave == 0) {
+                rows_at[to][lane] = page * a.c.page_stride + (uint64_t)in * a.c.token_stride;
+                const unsigned long long all = __ballot(alive);
+                if (lane == 0) alive_at[to] = all;
+            }
+            scale = *(const float *)((const char *)(wave == 0 ? a.c.k_scale : a.c.v_scale) + (int64_t)head * a.c.scale_head_stride +
+                                     page * a.c.scale_page_stride + (uint64_t)in * a.c.scale_token_stride);
+        }
+    };
+    dl_words<8> kw[K_LOADS];
+    uint32_t vw[V_LOADS][8];
+    auto load = [&](uint32_t from) {
+#pragma unroll
+        for (uint32_t x = 0; x < K_LOADS; ++x) {
+            const uint32_t n = threadIdx.x + x * CH_THREADS, key = n / PIECES, d = n % PIECES * 8u;
+            kw[x] = dl_load_words<8>(k_from + rows_at[from][key] + min(d, D - 8u));
+        }
+#pragma unroll
+        for (uint32_t x = 0; x < V_LOADS; ++x) {
+            const uint32_t n = threadIdx.x + x * CH_THREADS, d = n % (DP / 4) * 4u, part = n / (DP / 4) % 8u;
+            const uint32_t key = part / 2u * 16u + part % 2u * 4u;
+#pragma unroll
+            for (uint32_t e = 0; e < 8; ++e)
+                vw[x][e] = dl_load_at<uint32_t>(v_from + rows_at[from][key + (e & 3u) + (e >> 2) * 8u] + min(d, D - 4u));
+        }
+    };
+    auto put = [&](uint32_t from) {  // what has been loaded, into the tile
+        chunk_tile<DP> &to = tiles[from];
+        const uint32_t all_lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)alive_at[from]);
+        const uint32_t all_hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(alive_at[from] >> 32));
+        const uint64_t all = (uint64_t)all_hi << 32 | all_lo;
+        if (all != ~0ull) {  // what is none counts as zero
+#pragma unroll
+            for (uint32_t x = 0; x < K_LOADS; ++x)
+                if (!(all >> ((threadIdx.x + x * CH_THREADS) / PIECES) & 1u)) kw[x] = dl_words<8>{};
+#pragma unroll
+            for (uint32_t x = 0; x < V_LOADS; ++x) {
+                const uint32_t part = (threadIdx.x + x * CH_THREADS) / (DP / 4) % 8u, key = part / 2u * 16u + part % 2u * 4u;
+#pragma unroll
+                for (uint32_t e = 0; e < 8; ++e)
+                    if (!(all >> (key + (e & 3u) + (e >> 2) * 8u) & 1u)) vw[x][e] = 0;
+            }
+        }
+#pragma unroll
+        for (uint32_t x = 0; x < K_LOADS; ++x) {
+            const uint32_t n = threadIdx.x + x * CH_THREADS, key = n / PIECES, c = n % PIECES;
+            const dl_u32x2 p = C::template spread<Q>(kw[x].w[0]), r = C::template spread<Q>(kw[x].w[1]);
+            *(dl_u32x4 *)&to.k[(key * PIECES + (c ^ (key & 7u))) * 4u] = dl_u32x4{p[0], p[1], r[0], r[1]};
+        }
+#pragma unroll
+        for (uint32_t x = 0; x < V_LOADS; ++x) {
+            const uint32_t n = threadIdx.x + x * CH_THREADS, d = n % (DP / 4) * 4u, part = n / (DP / 4) % 8u;
+            if (V_ITEMS % CH_THREADS && n >= V_ITEMS) continue;
+            dl_u32x2 four[2][4];
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                const uint32_t w0 = vw[x][4 * g], w1 = vw[x][4 * g + 1], w2 = vw[x][4 * g + 2], w3 = vw[x][4 * g + 3];
+                const uint32_t a01 = __builtin_amdgcn_perm(w1, w0, 0x05010400u), a23 = __builtin_amdgcn_perm(w3, w2, 0x05010400u);
+                const uint32_t b01 = __builtin_amdgcn_perm(w1, w0, 0x07030602u), b23 = __builtin_amdgcn_perm(w3, w2, 0x07030602u);
+                four[g][0] = C::template spread<Q>(__builtin_amdgcn_perm(a23, a01, 0x05040100u));
+                four[g][1] = C::template spread<Q>(__builtin_amdgcn_perm(a23, a01, 0x07060302u));
+                four[g][2] = C::template spread<Q>(__builtin_amdgcn_perm(b23, b01, 0x05040100u));
+                four[g][3] = C::template spread<Q>(__builtin_amdgcn_perm(b23, b01, 0x07060302u));
+            }
+#pragma unroll
+            for (uint32_t f = 0; f < 4; ++f) {
+                const uint32_t r = d + f, c = part ^ ((r & 7u) ^ (r >> 3 & 3u));
+                *(dl_u32x4 *)&to.v[(r * 8u + c) * 4u] = dl_u32x4{four[0][f][0], four[0][f][1], four[1][f][0], four[1][f][1]};
+            }
+        }
+        if (wave == 0) {
+            to.ks[lane] = alive ? scale * a.scale : 0.0f;
+        } else if (wave == 1) {
+            const dl_value_scale<Q> u(scale);
+            to.lu[lane] = alive ? u.log2_c() : -INFINITY;
+            to.iu[lane] = alive ? u.over_c() : 0.0f;
+            to.d[lane] = u.d;
+            const bool some = __any(u.d != 1.0f);
+            if (lane == 0) to.taken_apart = some;
+        }
+    };
+    // Values times what their scales left out, in LDS, by all threads, before anybody works on the step.
+    auto apart = [&](chunk_tile<DP> &to) {
+#pragma unroll 1
+        for (uint32_t n = threadIdx.x; n < DP * 8u; n += CH_THREADS) {
+            const uint32_t r = n / 8u, part = n % 8u, key = part / 2u * 16u + part % 2u * 4u;
+            uint32_t *const v = &to.v[(r * 8u + (part ^ ((r & 7u) ^ (r >> 3 & 3u)))) * 4u];
+#pragma unroll
+            for (uint32_t x = 0; x < 4; ++x) {
+                const float *const d = &to.d[key + x / 2u * 8u + x % 2u * 2u];
+                v[x] = Q::pack(Q::in_range(Q::lo(v[x]) * d[0]), Q::in_range(Q::hi(v[x]) * d[1]));
+            }
+        }
+        __syncthreads();
+    };
+
+    dl_f32x16 o[DP / 32];
+    float r = -INFINITY, low = -Q::lift, l = 0.0f;
+#pragma unroll
+    for (int x = 0; x < DP / 32; ++x)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[x][e] = 0.0f;
+
+    if (first < end) {
+        look_up(first);
+        hand_on(first, 0);
+        __syncthreads();
+        load(0);
+        look_up(first + CH_KEYS);
+        put(0);
+        hand_on(first + CH_KEYS, 1);
+        __syncthreads();
+    }
+    uint32_t now = 0;
+    for (uint32_t base = first; base < end; base += CH_KEYS, now ^= 1u) {
+        const bool more = base + CH_KEYS < end;
+        if (__builtin_amdgcn_readfirstlane((int)tiles[now].taken_apart)) apart(tiles[now]);
+        if (more) {
+            load(now ^ 1u);
+            look_up(base + 2 * CH_KEYS);
+        }
+        const chunk_tile<DP> &in = tiles[now];
+#pragma unroll 1
+        for (uint32_t kb = 0; kb < 2; ++kb) {
+            const uint32_t key0 = base + 32u * kb;
+            if (key0 >= wave_end) break;
+            // scores: rows of the product are keys (8 (e / 4) + 4 half + e % 4), its columns queries (i)
+            dl_f32x16 s;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = 0.0f;
+            const uint32_t key = 32u * kb + i;
+#pragma unroll
+            for (uint32_t st = 0; st < DP / 16; ++st) {
+                const dl_u32x4 kf = *(const dl_u32x4 *)&in.k[(key * PIECES + ((2u * st + half) ^ (key & 7u))) * 4u];
+                s = Q::mfma32(kf, qf[st], s);
+            }
+            float ks[16], lu[16], iu[16];
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                const uint32_t k4 = 32u * kb + 2u * e + 4u * half;
+                const dl_f32x4 x = *(const dl_f32x4 *)&in.ks[k4], y = *(const dl_f32x4 *)&in.lu[k4], z = *(const dl_f32x4 *)&in.iu[k4];
+#pragma unroll
+                for (int f = 0; f < 4; ++f) ks[e + f] = x[f], lu[e + f] = y[f], iu[e + f] = z[f];
+            }
+            float top = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = fmaf(s[e], ks[e], lu[e]);
+            if (key0 + 32u > whole_end) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if ((int32_t)(key0 + 2u * (e & ~3) + 4u * half + (e & 3)) > last) s[e] = -INFINITY;
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) top = fmaxf(top, s[e]);
+            // (the reference follows the largest only where that is 2^8 times above it)
+            if (__any(top > r + 8.0f)) {
+                const auto swapped = __builtin_amdgcn_permlane32_swap(dl_bits<uint32_t>(top), dl_bits<uint32_t>(top), false, false);
+                top = fmaxf(dl_bits<float>((uint32_t)swapped[0]), dl_bits<float>((uint32_t)swapped[1]));
+                const float most = fmaxf(r, top), ref = most == -INFINITY ? 0.0f : most, fade = __builtin_amdgcn_exp2f(r - ref);
+                r = most;
+                low = ref - Q::lift;
+                l *= fade;
+#pragma unroll
+                for (int x = 0; x < DP / 32; ++x) o[x] *= fade;
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                s[e] = __builtin_amdgcn_exp2f(s[e] - low);
+                l = fmaf(s[e], iu[e], l);
+            }
+            dl_u32x4 pf[2];
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) pf[x][e] = Q::pack(s[8 * x + 2 * e], s[8 * x + 2 * e + 1]);
+            // sums: rows of the product are dims, its columns queries
+#pragma unroll
+            for (uint32_t x = 0; x < 2; ++x)
+#pragma unroll
+                for (uint32_t dt = 0; dt < DP / 32; ++dt) {
+                    const uint32_t d = 32u * dt + i, c = (4u * kb + 2u * x + half) ^ ((d & 7u) ^ (d >> 3 & 3u));
+                    const dl_u32x4 vf = *(const dl_u32x4 *)&in.v[(d * 8u + c) * 4u];
+                    o[dt] = Q::mfma32(vf, pf[x], o[dt]);
+                }
+        }
+        if (more) {
+            put(now ^ 1u);
+            hand_on(base + 2 * CH_KEYS, now);
+        }
+        __syncthreads();
+    }
+    l += __shfl_xor(l, 32);
+    if (my >= t.rows) return;
+    if (at.pieces > 1u) {
+        const uint64_t to = ((uint64_t)at.slot * a.c.heads + head) * CH_ROWS + (my - t.row0);
+        if (half == 0) a.rl[to] = dl_f32x2{r, l};
+#pragma unroll
+        for (int x = 0; x < DP / 32; ++x)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                const uint32_t d = 32u * x + 2u * e + 4u * half;
+                if (d < D) *(dl_f32x4 *)(a.partial + to * D + d) = dl_f32x4{o[x][e], o[x][e + 1], o[x][e + 2], o[x][e + 3]};
+            }
+        return;
+    }
+    const bool none = l == 0.0f;
+    const float f = none ? 0.0f : 1.0f / l;
+    char *const to = a.out + (uint64_t)(t.first + j) * a.out_token + h * a.out_head;
+#pragma unroll
+    for (int x = 0; x < DP / 32; ++x)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+            const uint32_t d = 32u * x + 2u * e + 4u * half;
+            if (d < D)
+                dl_store_at(to + 2u * d, none ? dl_u32x2{0, 0} : dl_u32x2{Q::pack(o[x][e] * f, o[x][e + 1] * f), Q::pack(o[x][e + 2] * f, o[x][e + 3] * f)});
+        }
+    if (a.lse && half == 0)
+        a.lse[(uint64_t)(t.first + j) * a.q_heads + h] = none ? -INFINITY : ((r == -INFINITY ? 0.0f : r) - Q::lift + log2f(l)) * DL_LN2;
+}
+
+// Joins the pieces of tiles that are cut.  A workgroup has 32 rows of one; DP / 4 lanes hold a row's sums, four each.
+constexpr uint32_t JOIN_ROWS = 32;
+template <class Q, int DP>
+__global__ void __launch_bounds__(CH_THREADS) dl_chunk_join_kernel(const chunk_args a)
+{
+    constexpr uint32_t LANES = DP / 4, AT_ONCE = CH_THREADS / LANES, AHEAD = 4;
+    const uint32_t D = a.c.head_dim, d0 = threadIdx.x % LANES * 4u;
+    const uint32_t part = blockIdx.x % (CH_ROWS / JOIN_ROWS), head = blockIdx.x / (CH_ROWS / JOIN_ROWS) % a.c.heads;
+    chunk_place at;
+    if (!chunk_unit<true>(a, blockIdx.x / (CH_ROWS / JOIN_ROWS) / a.c.heads, &at)) return;
+    const chunk_rows t(a, at);
+    const uint32_t pieces = max((t.end + at.keys - 1u) / at.keys, 1u);
+    for (uint32_t in = part * JOIN_ROWS + threadIdx.x / LANES; in < (part + 1u) * JOIN_ROWS; in += AT_ONCE) {
+        const uint32_t row = t.row0 + in;
+        if (row >= t.rows) return;
+        float r = -INFINITY, l = 0.0f;
+        dl_f32x4 o = {0, 0, 0, 0};
+        for (uint32_t p0 = 0; p0 < pieces; p0 += AHEAD) {
+            dl_f32x2 rl[AHEAD];
+            dl_f32x4 x[AHEAD];
+#pragma unroll
+            for (uint32_t k = 0; k < AHEAD; ++k) {
+                const uint64_t from = ((uint64_t)(at.slot + min(p0 + k, pieces - 1u)) * a.c.heads + head) * CH_ROWS + in;
+                rl[k] = a.rl[from];
+                x[k] = d0 < D ? *(const dl_f32x4 *)(a.partial + from * D + d0) : dl_f32x4{0, 0, 0, 0};
+                if (p0 + k >= pieces) rl[k] = dl_f32x2{-INFINITY, 0.0f}, x[k] = dl_f32x4{0, 0, 0, 0};
+            }
+            float now = r;
+#pragma unroll
+            for (uint32_t k = 0; k < AHEAD; ++k) now = fmaxf(now, rl[k][0]);
+            const float ref = now == -INFINITY ? 0.0f : now, fade = __builtin_amdgcn_exp2f(r - ref);
+            r = now;
+            l *= fade;
+            o *= fade;
+#pragma unroll
+            for (uint32_t k = 0; k < AHEAD; ++k) {
+                const float f = __builtin_amdgcn_exp2f(rl[k][0] - ref);
+                l = fmaf(rl[k][1], f, l);
+                o += x[k] * f;
+            }
+        }
+        const bool none = l == 0.0f;
+        const uint32_t j = row / a.group, h = head * a.group + row - j * a.group;
+        const float f = none ? 0.0f : 1.0f / l;
+        if (d0 < D)
+            dl_store_at(a.out + (uint64_t)(t.first + j) * a.out_token + h * a.out_head + 2u * d0,
+                        none ? dl_u32x2{0, 0} : dl_u32x2{Q::pack(o[0] * f, o[1] * f), Q::pack(o[2] * f, o[3] * f)});
+        if (a.lse && d0 == 0)
+            a.lse[(uint64_t)(t.first + j) * a.q_heads + h] = none ? -INFINITY : ((r == -INFINITY ? 0.0f : r) - Q::lift + log2f(l)) * DL_LN2;
+    }
+}
+
+struct chunk_shape {
+    uint64_t units;   // at most so many pieces a head, over all sequences
+    uint32_t target;  // 0: nothing is cut
+};
+
+int chunk_sizes(const dl_kv_cache *cache, const dl_chunk_attention_args *args, dl_cache_view *view, chunk_shape *sh)
+{
+    const int rc = dl_packed_sizes(cache, args, view);
+    if (rc != DL_OK) return rc;
+    *sh = chunk_shape{0, 0};
+    if (!args->tokens || !args->q_heads || !args->batch) return DL_OK;
+    const uint64_t rows = (uint64_t)args->tokens * (uint32_t)(args->q_heads / cache->heads);
+    // every sequence begins a tile of its own
+    uint64_t tiles = rows / CH_ROWS + (uint64_t)args->batch;
+    if (tiles > rows) tiles = rows;
+    const uint64_t most = (uint64_t)args->max_pages * (uint32_t)cache->page_tokens;
+    // Workgroups at once, by the registers and LDS: two a compute unit up to head_dim 128, one above.
+    const uint32_t slots = cache->head_dim > 128 ? 256u : 512u, round = slots / (uint32_t)cache->heads;
+    if (most > LEAST_STEPS * CH_KEYS && round > 1u) sh->target = round;
+    sh->units = tiles + sh->target;
+    return DL_OK;
+}
+
+size_t chunk_slots(const chunk_shape &sh, uint32_t heads) { return (size_t)2 * sh.target * heads * CH_ROWS; }
+
+}  // namespace
+
+extern "C" int64_t dl_chunk_attention_workspace(const dl_kv_cache *cache, const dl_chunk_attention_args *args)
+{
+    dl_cache_view view;
+    chunk_shape sh;
+    const int rc = chunk_sizes(cache, args, &view, &sh);
+    if (rc != DL_OK) return rc;
+    return (int64_t)(DL_CONTROL_BYTES + chunk_slots(sh, view.heads) * (sizeof(dl_f32x2) + view.head_dim * sizeof(float)));
+}
+
+extern "C" int dl_chunk_attention(const dl_kv_cache *cache, const dl_chunk_attention_args *args, void *stream)
+{
+    DL_LOCKED;
+    if (!g_dl.inited) return DL_ERR_STATE;
+    if (dl_device_error_pending()) return DL_ERR_LOST;
+    chunk_args a;
+    chunk_shape sh;
+    int rc = chunk_sizes(cache, args, &a.c, &sh);
+    if (rc != DL_OK) return rc;
+    if (!sh.units) return DL_OK;
+    rc = dl_cache_check(cache, 3, &a.c);
+    if (rc != DL_OK) return rc;
+    rc = dl_packed_setup(cache, args, (size_t)dl_chunk_attention_workspace(cache, args), &a.p);
+    if (rc != DL_OK) return rc;
+    if (!args->q || !args->out || (uint64_t)args->out % 2u) return DL_ERR_INVALID;
+    a.q = (const char *)args->q;
+    a.out = (char *)args->out;
+    a.lse = args->lse;
+    a.rl = (dl_f32x2 *)((char *)args->workspace + DL_CONTROL_BYTES);
+    a.partial = (float *)(a.rl + chunk_slots(sh, a.c.heads));
+    a.q_token = 2 * args->q_token_stride;
+    a.q_head = 2 * args->q_head_stride;
+    a.out_token = 2 * args->out_token_stride;
+    a.out_head = 2 * args->out_head_stride;
+    a.q_heads = (uint32_t)args->q_heads;
+    a.group = a.q_heads / a.c.heads;
+    a.target = sh.target;
+    a.scale = args->scale * DL_LOG2E;
+    const uint64_t grid = sh.units * a.c.heads;
+    if (grid >= (1ull << 32) / CH_THREADS) return DL_ERR_INVALID;
+    hipStream_t hs = (hipStream_t)stream;
+    dl_with_16bit(args->type, [&](auto q) {
+        auto go = [&](auto dp) {
+            constexpr int DP = decltype(dp)::value;
+            dl_with_format(cache->format, [&](auto c) {
+                hipLaunchKernelGGL((dl_chunk_kernel<decltype(q), decltype(c), DP>), dim3((uint32_t)grid), dim3(CH_THREADS), 0, hs, a);
+            });
+            if (sh.target)
+                hipLaunchKernelGGL((dl_chunk_join_kernel<decltype(q), DP>), dim3(sh.target * a.c.heads * (CH_ROWS / JOIN_ROWS)), dim3(CH_THREADS), 0, hs, a);
+        };
+        if (a.c.head_dim <= 64)
+            go(std::integral_constant<int, 64>{});
+        else if (a.c.head_dim <= 128)
+            go(std::integral_constant<int, 128>{});
+        else
+            go(std::integral_constant<int, 256>{});
+    });
+    DL_HIP(hipGetLastError());
+    t_dl_last.mode = DL_MODE_ONESHOT;
+    return DL_OK;
+}

@@ -1,4 +1,4 @@
-// Element types and 8-bit codes of the operators over a quantised cache (dl_kv.hip, dl_attention.hip, dl_verify.hip).
+// Element types and 8-bit codes of the operators over a quantised cache, and what their kernels share.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -68,7 +68,7 @@ struct dl_bf16 {
     // Weights relative to a reference, at most 2^8, are held as 2^lift times as much.  Floats of 16 bits lose bits below 2^-14,
     // so there they use the range above as well: what is 2^-21 of the reference still has all of its bits.
     static constexpr float lift = 0.0f;
-    // Scales of values from twice this one on are taken apart (value_scale in dl_attention.hip), and a product with what that leaves over
+    // Scales of values from twice this one on are taken apart (dl_value_scale below), and a product with what that leaves over
     // is brought into the type's range.
     static constexpr float scale_most = 0x1p40f;
     static __device__ __forceinline__ float in_range(float w) { return w; }
@@ -166,6 +166,102 @@ struct dl_int8 {
     }
 };
 
+// ------------------------------------------------------------------ what the kernels share
+
+// x + the lanes before it; lane 63 ends with the sum of all.
+__device__ __forceinline__ uint32_t dl_sum_up_to(uint32_t x)
+{
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xF, 0xF, false);  // row_shr:1, 2, 4, 8
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xF, 0xF, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xF, 0xF, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xF, 0xF, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xA, 0xF, false);  // row_bcast:15, 31
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xC, 0xF, false);
+    return x;
+}
+
+// N elements of a row as floats
+template <class T, int N>
+__device__ __forceinline__ void dl_load_row(const char *p, float (&x)[N])
+{
+    if constexpr (T::size == 4) {
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) {
+            const dl_f32x4 w = dl_load_at<dl_f32x4>(p + 16 * i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[4 * i + j] = w[j];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N / 8; ++i) {
+            const dl_u32x4 w = dl_load_at<dl_u32x4>(p + 16 * i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[8 * i + 2 * j] = T::lo(w[j]), x[8 * i + 2 * j + 1] = T::hi(w[j]);
+        }
+    }
+}
+
+// STREAM: past the caches
+template <bool STREAM, class V>
+__device__ __forceinline__ void dl_put(char *p, V v)
+{
+    typedef V anywhere __attribute__((aligned(1)));
+    if constexpr (STREAM)
+        __builtin_nontemporal_store(v, (anywhere *)p);
+    else
+        dl_store_at(p, v);
+}
+
+template <class T, bool STREAM, int N>
+__device__ __forceinline__ void dl_store_row(char *p, const float (&x)[N])
+{
+    if constexpr (T::size == 4) {
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) dl_put<STREAM>(p + 16 * i, dl_f32x4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]});
+    } else {
+#pragma unroll
+        for (int i = 0; i < N / 8; ++i) {
+            dl_u32x4 w;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = T::pack(x[8 * i + 2 * j], x[8 * i + 2 * j + 1]);
+            dl_put<STREAM>(p + 16 * i, w);
+        }
+    }
+}
+
+// A vector of N bytes, N = 4, 8, 16, as words
+template <int N>
+struct dl_words {
+    uint32_t w[N / 4];
+};
+template <int N>
+__device__ __forceinline__ dl_words<N> dl_load_words(const char *p)
+{
+    return dl_load_at<dl_words<N>>(p);
+}
+// A value's scale u = c d for the sums, d a power of two.  c: what log2 u and 1 / u are taken of, so that neither they nor a product with
+// 2^(log2 u) or 1 / u leave the range of 32 bits, however far apart the scales of the rows are that a query sees.  d: 1, or what that
+// leaves out; it goes to the product with the values alone (never to l), and is finite, so that a weight of zero takes it out.
+// Scales below 2^-126 (dl_kv_write gives 2^-100 / 448 and more) count as zero, and so do negative ones.  A NaN stays in c.
+template <class Q>
+struct dl_value_scale {
+    float c, d;
+    __device__ __forceinline__ explicit dl_value_scale(float u)
+    {
+        constexpr float LOW = 0x1p-40f, HIGH = Q::scale_most;
+        // u's power of two (none for what is no positive number, infinite for infinities), and what it is more than the limit's
+        const float power = dl_bits<float>(dl_bits<uint32_t>(fmaxf(u, 0.0f)) & 0x7F800000u);
+        const bool low = u < LOW, high = u >= 2.0f * HIGH;
+        d = low ? power * (1.0f / LOW) : high ? fminf(power, 0x1p127f) * (1.0f / HIGH) : 1.0f;
+        // (the mantissa of u with the limit's power)
+        const float c_limit = dl_bits<float>((dl_bits<uint32_t>(u) & 0x007FFFFFu) | dl_bits<uint32_t>(low ? LOW : HIGH));
+        c = low || high ? c_limit : u;
+    }
+    __device__ __forceinline__ float log2_c() const { return __builtin_amdgcn_logf(c); }
+    // (finite for a NaN as well: its readers' weights have it from the logarithm)
+    __device__ __forceinline__ float over_c() const { return __builtin_amdgcn_rcpf(c == c ? c : 1.0f); }
+};
+
 // Calls f with the types that belong to a dl_kv_format / to a 16-bit dl_type.
 template <class F>
 static inline void dl_with_format(int32_t format, F f)
@@ -190,6 +286,22 @@ static inline void dl_with_type(int32_t type, F f)
         f(dl_f32{});
     else
         dl_with_16bit(type, f);
+}
+
+// The lanes that a row takes, a power of two.
+template <int N, class F>
+static inline void dl_with_lanes(uint32_t head_dim, F f)
+{
+    if (head_dim <= 16)
+        f(std::integral_constant<int, 16 / N>{});
+    else if (head_dim <= 32)
+        f(std::integral_constant<int, 32 / N>{});
+    else if (head_dim <= 64)
+        f(std::integral_constant<int, 64 / N>{});
+    else if (head_dim <= 128)
+        f(std::integral_constant<int, 128 / N>{});
+    else
+        f(std::integral_constant<int, 256 / N>{});
 }
 
 // The cache as the kernels get it.

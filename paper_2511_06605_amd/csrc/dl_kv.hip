@@ -23,55 +23,6 @@ struct kv_args {
     int32_t shift;  // log2 of the tokens of a page, or -1
 };
 
-// N elements of a row as floats
-template <class T, int N>
-__device__ __forceinline__ void load_row(const char *p, float (&x)[N])
-{
-    if constexpr (T::size == 4) {
-#pragma unroll
-        for (int i = 0; i < N / 4; ++i) {
-            const dl_f32x4 w = dl_load_at<dl_f32x4>(p + 16 * i);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[4 * i + j] = w[j];
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < N / 8; ++i) {
-            const dl_u32x4 w = dl_load_at<dl_u32x4>(p + 16 * i);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[8 * i + 2 * j] = T::lo(w[j]), x[8 * i + 2 * j + 1] = T::hi(w[j]);
-        }
-    }
-}
-
-// STREAM: past the caches
-template <bool STREAM, class V>
-__device__ __forceinline__ void put(char *p, V v)
-{
-    typedef V anywhere __attribute__((aligned(1)));
-    if constexpr (STREAM)
-        __builtin_nontemporal_store(v, (anywhere *)p);
-    else
-        dl_store_at(p, v);
-}
-
-template <class T, bool STREAM, int N>
-__device__ __forceinline__ void store_row(char *p, const float (&x)[N])
-{
-    if constexpr (T::size == 4) {
-#pragma unroll
-        for (int i = 0; i < N / 4; ++i) put<STREAM>(p + 16 * i, dl_f32x4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]});
-    } else {
-#pragma unroll
-        for (int i = 0; i < N / 8; ++i) {
-            dl_u32x4 w;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = T::pack(x[8 * i + 2 * j], x[8 * i + 2 * j + 1]);
-            put<STREAM>(p + 16 * i, w);
-        }
-    }
-}
-
 // Where a row of a slot lies: false if the slot is none.
 __device__ __forceinline__ bool place(const kv_args &a, int64_t slot, uint32_t head, int64_t *codes, int64_t *scale)
 {
@@ -119,7 +70,7 @@ __global__ void __launch_bounds__(KV_THREADS) dl_kv_write_kernel(const kv_args a
         slot[r] = a.slots[token];
 #pragma unroll
         for (int i = 0; i < N; ++i) x[r][i] = 0.0f;
-        if (mine) load_row<T>(from + (size_t)lane * N * T::size, x[r]);
+        if (mine) dl_load_row<T>(from + (size_t)lane * N * T::size, x[r]);
     }
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
@@ -141,7 +92,7 @@ __global__ void __launch_bounds__(KV_THREADS) dl_kv_write_kernel(const kv_args a
             w[i] = C::code4(x[r][4 * i] * factor, x[r][4 * i + 1] * factor, x[r][4 * i + 2] * factor, x[r][4 * i + 3] * factor);
             if (!finite) w[i] = 0;
         }
-        if (mine) put<MANY>((values ? a.c.v : a.c.k) + at + lane * (uint32_t)N, w);
+        if (mine) dl_put<MANY>((values ? a.c.v : a.c.k) + at + lane * (uint32_t)N, w);
         if (lane == 0) *(float *)((char *)(values ? a.c.v_scale : a.c.k_scale) + scale_at) = finite ? most * (1.0f / C::limit) : __builtin_nanf("");
     }
 }
@@ -186,24 +137,8 @@ __global__ void __launch_bounds__(KV_THREADS) dl_kv_read_kernel(const kv_args a)
 #pragma unroll
             for (int j = 0; j < 4; ++j) x[4 * i + j] = y[j] * scale[r];
         }
-        store_row<T, MANY>(to + (size_t)lane * N * T::size, x);
+        dl_store_row<T, MANY>(to + (size_t)lane * N * T::size, x);
     }
-}
-
-// The lanes that a row takes, a power of two.
-template <int N, class F>
-void with_lanes(uint32_t head_dim, F f)
-{
-    if (head_dim <= 16)
-        f(std::integral_constant<int, 16 / N>{});
-    else if (head_dim <= 32)
-        f(std::integral_constant<int, 32 / N>{});
-    else if (head_dim <= 64)
-        f(std::integral_constant<int, 64 / N>{});
-    else if (head_dim <= 128)
-        f(std::integral_constant<int, 128 / N>{});
-    else
-        f(std::integral_constant<int, 256 / N>{});
 }
 
 int kv_setup(const dl_kv_cache *cache, const dl_kv_rows *rows, kv_args *a, bool *nothing)
@@ -246,7 +181,7 @@ int kv_run(const dl_kv_cache *cache, const dl_kv_rows *rows, void *stream)
     if (rc != DL_OK || nothing) return rc;
     dl_with_type(rows->type, [&](auto t) {
         dl_with_format(cache->format, [&](auto c) {
-            with_lanes<WRITE ? WRITE_ELEMENTS : READ_ELEMENTS>(a.c.head_dim, [&](auto lanes) {
+            dl_with_lanes<WRITE ? WRITE_ELEMENTS : READ_ELEMENTS>(a.c.head_dim, [&](auto lanes) {
                 constexpr int L = decltype(lanes)::value;
                 auto go = [&](auto many) {
                     constexpr bool MANY = decltype(many)::value;

@@ -1,0 +1,179 @@
+// Norms of queries and keys for each head, and the rotation by position, in one pass (dl_norm_rotate).
+//
+// A row is held in registers from its load to its store, eight elements a lane, as many lanes as it takes (the next power of two) side
+// by side: the sum of squares goes round by swaps among them, and the other half of a pair is either in the lane itself (neighbours) or
+// comes from the lane rotary / 16 further.  So every lane stores what it has loaded and nothing else, and an output may be its input.
+// Memory is what bounds it: each row once in and once out; the table's rows come from the caches, since the heads of a token share one.
+#include "dl_codes.h"
+#include "dl_internal.h"
+
+namespace {
+
+struct norm_side {
+    const char *x;
+    char *y;
+    const float *weight;
+    int64_t token, head, out_token, out_head;  // bytes
+};
+struct norm_args {
+    norm_side q, k;
+    const float *table;
+    const int64_t *positions;
+    int64_t table_rows, table_stride;  // floats
+    uint32_t rows, q_heads, head_dim, rotary;
+    dl_divider heads;  // q_heads + k_heads
+    float over_dim, eps;
+    int32_t neighbours;
+};
+
+constexpr uint32_t NORM_THREADS = 256;
+constexpr int NORM_ELEMENTS = 8;
+// From so many threads on two rows of a thread are on their way at once and stores go past the caches.
+constexpr uint64_t NORM_MANY_THREADS = 1ull << 20;
+
+template <class T, int LANES, bool MANY>
+__global__ void __launch_bounds__(NORM_THREADS) dl_norm_rotate_kernel(const norm_args a)
+{
+    constexpr int ROWS = MANY ? 2 : 1, N = NORM_ELEMENTS;
+    const uint32_t lane = threadIdx.x % LANES, row0 = blockIdx.x * (NORM_THREADS / LANES * ROWS) + threadIdx.x / LANES;
+    const uint32_t at = lane * (uint32_t)N, half = a.rotary / 2u;
+    const bool mine = at < a.head_dim, turned = at < a.rotary;
+    // which pairs: of the lane's elements as first or second of theirs, or its own neighbours
+    const bool second = !a.neighbours && at >= half;
+    const uint32_t angle = a.neighbours ? at / 2u : second ? at - half : at;
+    float x[ROWS][N], w[ROWS][N], c[ROWS][N], z[ROWS][N];
+    bool live[ROWS], normed[ROWS];
+    char *to[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        const uint32_t row = row0 + r * (NORM_THREADS / LANES), from = min(row, a.rows - 1u), token = dl_divide(from, a.heads);
+        uint32_t h = from - token * a.heads.d;
+        const bool is_q = h < a.q_heads;
+        const norm_side &s = is_q ? a.q : a.k;
+        if (!is_q) h -= a.q_heads;
+        live[r] = row < a.rows && mine;
+        to[r] = s.y + token * s.out_token + h * s.out_head + (size_t)at * T::size;
+        normed[r] = s.weight != nullptr;
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[r][i] = 0.0f, w[r][i] = 1.0f, c[r][i] = 1.0f, z[r][i] = 0.0f;
+        if (mine) {
+            dl_load_row<T>(s.x + token * s.token + h * s.head + (size_t)at * T::size, x[r]);
+            if (normed[r]) dl_load_row<dl_f32>((const char *)(s.weight + at), w[r]);
+        }
+        if (a.rotary) {
+            const int64_t position = a.positions[token];
+            const bool known = position >= 0 && position < a.table_rows;
+            live[r] &= known;
+            if (turned && known) {
+                const char *const p = (const char *)(a.table + position * a.table_stride + angle);
+                if (a.neighbours) {
+                    const dl_f32x4 u = dl_load_at<dl_f32x4>(p), v = dl_load_at<dl_f32x4>(p + 4u * half);
+#pragma unroll
+                    for (int i = 0; i < N; ++i) c[r][i] = u[i / 2], z[r][i] = v[i / 2];
+                } else {
+                    dl_load_row<dl_f32>(p, c[r]);
+                    dl_load_row<dl_f32>(p + 4u * half, z[r]);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum = fmaf(x[r][i], x[r][i], sum);
+#pragma unroll
+        for (int d = 1; d < LANES; d *= 2) sum += __shfl_xor(sum, d);
+        if (normed[r]) {
+            const float f = rsqrtf(fmaf(sum, a.over_dim, a.eps));
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[r][i] = x[r][i] * f * w[r][i];
+        }
+        if (a.rotary) {
+            float y[N];
+            if (a.neighbours) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) y[i] = x[r][i ^ 1] * (i % 2 ? 1.0f : -1.0f);
+            } else {
+                // (all lanes take part; those behind the rotated elements get something, which z = 0 would let infinities into)
+                const uint32_t self = threadIdx.x % 64u, other = turned ? second ? self - half / N : self + half / N : self;
+#pragma unroll
+                for (int i = 0; i < N; ++i) y[i] = __shfl(x[r][i], (int)other) * (second ? 1.0f : -1.0f);
+            }
+            if (turned) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) x[r][i] = fmaf(x[r][i], c[r][i], y[i] * z[r][i]);
+            }
+        }
+        if (live[r]) dl_store_row<T, MANY>(to[r], x[r]);
+    }
+}
+
+int norm_setup(const dl_norm_rotate_args *args, norm_args *a, bool *nothing)
+{
+    if (!args) return DL_ERR_INVALID;
+    if (args->type < DL_TYPE_F32 || args->type > DL_TYPE_F16 || args->reserved != 0) return DL_ERR_INVALID;
+    if (args->head_dim < 16 || args->head_dim > 256 || args->head_dim % 16 || args->rotary < 0 || args->rotary > args->head_dim || args->rotary % 16)
+        return DL_ERR_INVALID;
+    if (args->neighbours < 0 || args->neighbours > 1 || !(args->eps >= 0.0f)) return DL_ERR_INVALID;
+    if (args->q_heads < 0 || args->k_heads < 0 || args->q_heads > 65535 || args->k_heads > 65535) return DL_ERR_INVALID;
+    if (args->table_rows < 0 || args->table_rows > INT32_MAX) return DL_ERR_INVALID;
+    const int64_t q_heads = args->q ? args->q_heads : 0, heads = q_heads + (args->k ? args->k_heads : 0);
+    if (heads > 65536 || args->tokens < 0 || args->tokens > DL_MAX_ROWS || args->tokens * heads > DL_MAX_ROWS) return DL_ERR_INVALID;
+    *nothing = args->tokens * heads == 0;
+    if (*nothing) return DL_OK;
+    if ((args->q && !args->q_out) || (args->k && !args->k_out)) return DL_ERR_INVALID;
+    if (args->rotary && (!args->positions || (args->table_rows && !args->table))) return DL_ERR_INVALID;
+    const int size = args->type == DL_TYPE_F32 ? 4 : 2;
+    if (((uint64_t)args->q | (uint64_t)args->k | (uint64_t)args->q_out | (uint64_t)args->k_out) % size ||
+        ((uint64_t)args->q_weight | (uint64_t)args->k_weight | (uint64_t)args->table) % 4u || (uint64_t)args->positions % 8u)
+        return DL_ERR_INVALID;
+    a->q = {(const char *)args->q, (char *)args->q_out, args->q_weight, args->q_token_stride * size, args->q_head_stride * size,
+            args->q_out_token_stride * size, args->q_out_head_stride * size};
+    a->k = {(const char *)args->k, (char *)args->k_out, args->k_weight, args->k_token_stride * size, args->k_head_stride * size,
+            args->k_out_token_stride * size, args->k_out_head_stride * size};
+    a->table = args->table;
+    a->positions = args->positions;
+    a->table_rows = args->table_rows;
+    a->table_stride = args->table_stride;
+    a->rows = (uint32_t)(args->tokens * heads);
+    a->q_heads = (uint32_t)q_heads;
+    a->head_dim = (uint32_t)args->head_dim;
+    a->rotary = (uint32_t)args->rotary;
+    a->heads = dl_make_divider((uint32_t)heads);
+    a->over_dim = 1.0f / (float)args->head_dim;
+    a->eps = args->eps;
+    a->neighbours = args->neighbours;
+    return DL_OK;
+}
+
+}  // namespace
+
+extern "C" int dl_norm_rotate(const dl_norm_rotate_args *args, void *stream)
+{
+    DL_LOCKED;
+    if (!g_dl.inited) return DL_ERR_STATE;
+    if (dl_device_error_pending()) return DL_ERR_LOST;
+    norm_args a;
+    bool nothing;
+    const int rc = norm_setup(args, &a, &nothing);
+    if (rc != DL_OK || nothing) return rc;
+    dl_with_type(args->type, [&](auto t) {
+        dl_with_lanes<NORM_ELEMENTS>(a.head_dim, [&](auto lanes) {
+            constexpr int L = decltype(lanes)::value;
+            auto go = [&](auto many) {
+                constexpr bool MANY = decltype(many)::value;
+                constexpr uint32_t ROWS = NORM_THREADS / L * (MANY ? 2 : 1);
+                hipLaunchKernelGGL((dl_norm_rotate_kernel<decltype(t), L, MANY>), dim3((a.rows + ROWS - 1u) / ROWS), dim3(NORM_THREADS), 0,
+                                   (hipStream_t)stream, a);
+            };
+            if ((uint64_t)a.rows * L >= NORM_MANY_THREADS)
+                go(std::true_type{});
+            else
+                go(std::false_type{});
+        });
+    });
+    DL_HIP(hipGetLastError());
+    t_dl_last.mode = DL_MODE_ONESHOT;
+    return DL_OK;
+}

@@ -1,0 +1,156 @@
+"""Eviction by weight (dl_kv_evict): which tokens stay, and that they and nothing else have moved."""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2511_06605_amd as dl
+
+import prompt_ref
+from prompt_ref import Packed
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def library():
+    torch.cuda.set_device(0)
+    dl.dl_init(0)
+    yield
+    dl.dl_shutdown()
+
+
+@pytest.fixture(scope="module")
+def workspace():
+    w = torch.full((1 << 26,), 0xFF, dtype=torch.uint8, device="cuda")
+    w[:65536] = 0
+    return w
+
+
+def bits(t):
+    return t.contiguous().view(torch.uint8).cpu().numpy().reshape(*t.shape, -1)
+
+
+def check(workspace, lens, keep, first=0, recent=0, weights=None, spoil=None, with_weights=True, **more):
+    page = more.get("page", 16)
+    to_wide = -(-keep // page)
+    p = Packed([(0, n) for n in lens], more_pages=len(lens) * to_wide, **more)
+    B, width = p.table.shape[0], p.table.shape[1] * page
+    if weights is None:
+        weights = p.rng.standard_normal((B, width)).astype(np.float32)
+    weights = np.asarray(weights, dtype=np.float32)
+    to_pages = p.free[:B * to_wide].reshape(B, to_wide).copy()
+    if spoil:
+        spoil(p, to_pages)
+    room = torch.full((B + 2, width + 3), float("nan"), device="cuda")
+    w = room[1:-1, 1:width + 1]
+    w.copy_(torch.from_numpy(weights))
+    kept = torch.full((B + 2, keep), 7, dtype=torch.int32, device="cuda")
+    kept_lens = torch.full((B + 2,), 7, dtype=torch.int32, device="cuda")
+    kept_weights = torch.full((B + 2, keep + 4), 7.0, device="cuda")
+    before = [bits(t) for t in (p.k, p.k_scale, p.v, p.v_scale)]
+    r = dl.KvEvict(p.cache(), w, p.put(p.table), p.put(np.array(lens, dtype=np.int32)), p.put(to_pages), kept[1:-1], kept_lens[1:-1],
+                   kept_weights=kept_weights[1:-1, 2:keep + 2] if with_weights else None, first=first, recent=recent)
+    assert dl.dl_kv_evict_workspace(r) <= workspace.numel()
+    r.use_workspace(workspace)
+    dl.dl_kv_evict(r, torch.cuda.current_stream())
+    want = [x.copy() for x in before]
+    pages = before[0].shape[0]
+    want_kept, want_weights = np.full((B, keep), -1), np.zeros((B, keep), dtype=np.float32)
+    for b, n in enumerate(lens):
+        stay = prompt_ref.evicted(weights[b], n, keep, first, recent)
+        want_kept[b, :len(stay)], want_weights[b, :len(stay)] = stay, weights[b][stay]
+        for j, i in enumerate(stay):
+            source, to = p.table[b, i // page], to_pages[b, j // page]
+            if 0 <= source < pages and 0 <= to < pages:
+                for x, y in zip(want, before):
+                    x[to, j % page] = y[source, i % page]
+    k = kept.cpu().numpy()
+    assert (k[1:-1] == want_kept).all() and (k[[0, -1]] == 7).all()
+    assert kept_lens.tolist() == [7] + [min(n, keep) for n in lens] + [7]
+    got = kept_weights.cpu().numpy()
+    if with_weights:
+        assert np.array_equal(got[1:-1, 2:keep + 2], want_weights, equal_nan=True)
+        got[1:-1, 2:keep + 2] = 7
+    assert (got == 7).all()
+    for x, t in zip(want, (p.k, p.k_scale, p.v, p.v_scale)):
+        assert (bits(t) == x).all()
+    return want_kept
+
+
+@pytest.mark.parametrize("kind", ["fp8", "int8"])
+@pytest.mark.parametrize("dim,heads", [(16, 3), (32, 2), (64, 2), (80, 1), (128, 8), (208, 1), (256, 2)])
+def test_heads(workspace, kind, dim, heads):
+    check(workspace, [50, 7, 40], 20, first=2, recent=5, kind=kind, dim=dim, heads=heads)
+
+
+@pytest.mark.parametrize("page", [1, 5, 16, 24, 128])
+def test_pages(workspace, page):
+    check(workspace, [100, 31, 1], 37, first=1, recent=3, page=page)
+
+
+@pytest.mark.parametrize("lens,keep,first,recent", [
+    ([0], 5, 1, 1), ([5], 5, 2, 2), ([6], 5, 2, 2), ([6], 5, 0, 0), ([6], 5, 5, 0), ([6], 5, 0, 5), ([6], 5, 2, 3), ([40], 1, 0, 0), ([40], 1, 1, 0),
+    ([40], 1, 0, 1), ([10, 0, 300, 20], 20, 4, 8), ([1023, 1024, 1025], 1000, 3, 10), ([2100, 4096, 5000], 2049, 0, 1), ([30], 0, 0, 0)])
+def test_lengths(workspace, lens, keep, first, recent):
+    check(workspace, lens, keep, first, recent, heads=1, dim=16)
+
+
+@pytest.mark.parametrize("n,keep", [(5000, 1000), (20001, 700), (70001, 20000)])
+def test_long_sequences(workspace, n, keep):
+    check(workspace, [n, n // 3], keep, first=4, recent=64, heads=1, dim=16)
+
+
+def test_equal_weights(workspace):
+    rng = np.random.default_rng(0)
+    for values in ([1.0], [0.0, -0.0], [0.0, 1.0], [2.0, 2.0 + 2.0 ** -22], [1e-40, 0.0, -1e-40]):
+        check(workspace, [3000, 500], 400, first=3, recent=7, weights=rng.choice(np.array(values, dtype=np.float32), (2, 3008)), heads=1, dim=16)
+    # equal to the last one that stays, and nothing else: the lowest
+    kept = check(workspace, [2500], 1200, weights=np.ones((1, 2512)), heads=1, dim=16)
+    assert (kept[0] == np.arange(1200)).all()
+
+
+def test_weights_that_are_no_numbers(workspace):
+    rng = np.random.default_rng(1)
+    w = rng.standard_normal((2, 2000)).astype(np.float32)
+    w[:, rng.integers(0, 2000, 300)] = np.inf
+    w[:, rng.integers(0, 2000, 300)] = -np.inf
+    w[0, rng.integers(0, 2000, 1500)] = np.nan
+    w[1, ::3] = -np.float32(np.nan)
+    for keep in (150, 700, 1900):
+        check(workspace, [2000, 1999], keep, first=2, recent=9, weights=w, heads=1, dim=16)
+    check(workspace, [300], 40, weights=np.full((1, 304), np.nan), heads=1, dim=16)
+
+
+def test_weights_that_differ_in_their_last_bits(workspace):
+    rng = np.random.default_rng(2)
+    base = np.float32(1.5).view(np.uint32)
+    w = (base + rng.integers(0, 4000, (1, 4000)).astype(np.uint32)).view(np.float32)
+    check(workspace, [3999], 1777, weights=w, heads=1, dim=16)
+
+
+def test_pages_that_are_none(workspace):
+    def spoil(p, to_pages):
+        p.table[0, 1], p.table[0, 3], to_pages[0, 1] = -1, 1 << 30, -5
+
+    check(workspace, [100, 30], 50, spoil=spoil)
+
+
+@pytest.mark.parametrize("order", [(0, 2, 1), (2, 0, 1), (1, 0, 2)])
+def test_orders_of_a_cache(workspace, order):
+    check(workspace, [50, 30], 20, first=1, recent=2, order=order)
+
+
+def test_without_weights_of_what_stays(workspace):
+    check(workspace, [50, 10], 20, with_weights=False)
+
+
+def test_lengths_beyond_the_table(workspace):
+    p = Packed([(0, 48), (0, 40)], more_pages=4)
+    weights = torch.rand((2, 48), device="cuda")
+    kept, lens = torch.zeros((2, 10), dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    r = dl.KvEvict(p.cache(), weights, p.put(p.table), torch.tensor([1 << 30, -4], dtype=torch.int32, device="cuda"), p.put(p.free[:2].reshape(2, 1)), kept, lens)
+    r.use_workspace(workspace)
+    dl.dl_kv_evict(r, torch.cuda.current_stream())
+    assert lens.tolist() == [10, 0] and kept[1].tolist() == [-1] * 10
+    assert kept[0].tolist() == prompt_ref.evicted(weights[0].cpu().numpy(), 48, 10, 0, 0)

@@ -1,0 +1,155 @@
+"""What cached tokens have been given (dl_kv_weigh) against a plain implementation in 64 bits."""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2511_06605_amd as dl
+
+from prompt_ref import Packed
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def library():
+    torch.cuda.set_device(0)
+    dl.dl_init(0)
+    yield
+    dl.dl_shutdown()
+
+
+@pytest.fixture(scope="module")
+def workspace():
+    w = torch.full((1 << 28,), 0xFF, dtype=torch.uint8, device="cuda")
+    w[:65536] = 0
+    return w
+
+
+def check(p, workspace, with_before=True, dead=(), lse=None, q=None, in_place=False):
+    lse = p.put(p.exact_lse(dead) if lse is None else lse).float()
+    B, width = p.table.shape[0], p.table.shape[1] * p.page
+    before = torch.from_numpy(p.rng.random((B, width + 5))).float().cuda()[:, 2:width + 2] if with_before else None
+    weights = before if in_place else torch.full((B + 2, width + 3), 7.0, device="cuda")[1:-1, 1:width + 1]
+    old = None if before is None else before.double().cpu().numpy()
+    r = dl.KvWeigh(p.cache(), p.q if q is None else q, lse, *p.plan(), weights, before=before, scale=p.scale)
+    assert dl.dl_kv_weigh_workspace(r) <= workspace.numel()
+    r.use_workspace(workspace)
+    dl.dl_kv_weigh(r, torch.cuda.current_stream())
+    want, bound = p.weighed(lse.double().cpu().numpy(), old, dead)
+    got = weights.double().cpu().numpy()
+    assert (np.isnan(got) == np.isnan(want)).all()
+    fine = ~np.isnan(want)
+    off = np.abs(got - want)[fine]
+    assert (off <= bound[fine]).all(), float((off / np.maximum(bound[fine], 1e-300)).max())
+    if not in_place:
+        room = weights._base
+        assert (room[0] == 7).all() and (room[-1] == 7).all() and (room[:, 0] == 7).all() and (room[:, width + 1:] == 7).all()
+    return weights, want
+
+
+TYPES = [(torch.bfloat16, "fp8"), (torch.float16, "int8"), (torch.bfloat16, "int8"), (torch.float16, "fp8")]
+
+
+@pytest.mark.parametrize("dtype,kind", TYPES)
+@pytest.mark.parametrize("dim,heads,group", [(64, 2, 1), (128, 1, 7), (256, 1, 3), (80, 2, 4), (16, 3, 2), (96, 1, 20), (208, 12, 1), (64, 9, 2)])
+def test_types_and_heads(workspace, dtype, kind, dim, heads, group):
+    check(Packed([(5, 5), (3, 70), (20, 90)], heads=heads, group=group, dim=dim, dtype=dtype, kind=kind, seed=dim + group, gaps=2), workspace)
+
+
+@pytest.mark.parametrize("page", [1, 5, 16, 24, 128])
+def test_pages_that_end_anywhere(workspace, page):
+    check(Packed([(1, 1), (31, 64), (2, 33), (33, 100)], page=page, group=2, heads=1, seed=page, spare=2), workspace)
+
+
+@pytest.mark.parametrize("sizes", [
+    [(1, 1)], [(1, 0)], [(0, 5)], [(0, 0)], [(3, 1)], [(5, 0), (2, 7), (0, 3), (4, 4)], [(31, 33)], [(64, 64)], [(130, 131)], [(1, 600)],
+    [(40, 20), (20, 40)], [(1, 9)] * 70])
+def test_lengths(workspace, sizes):
+    for dtype, kind in TYPES[:2]:
+        for with_before in (True, False):
+            check(Packed(sizes, heads=1, group=3, dtype=dtype, kind=kind, seed=len(sizes)), workspace, with_before)
+
+
+@pytest.mark.parametrize("heads,group,sizes", [(1, 1, [(300, 300)]), (8, 2, [(65, 200)]), (2, 16, [(33, 100), (2, 900)]), (4, 4, [(128, 260), (1, 9)])])
+def test_many_queries(workspace, heads, group, sizes):
+    for dtype, kind in TYPES[:2]:
+        check(Packed(sizes, heads=heads, group=group, dim=64, dtype=dtype, kind=kind, seed=heads), workspace)
+
+
+def test_the_weights_of_a_query_add_up(workspace):
+    """Every query and head gives one in all."""
+    p = Packed([(7, 300), (40, 40)], heads=2, group=3)
+    weights, _ = check(p, workspace, with_before=False)
+    for b, (m, n) in enumerate(p.sizes):
+        assert abs(float(weights[b].double().sum()) - m * 6) <= 1e-4 * m * 6
+
+
+def test_in_place_and_step_after_step(workspace):
+    check(Packed([(5, 40), (3, 3)], group=2), workspace, in_place=True)
+
+
+def test_strides_of_queries(workspace):
+    p = Packed([(6, 40), (11, 11)], heads=2, group=3, dim=80)
+    q = torch.empty((6, p.tokens, 83), dtype=p.dtype, device="cuda").permute(1, 0, 2)[..., 1:81]
+    q.copy_(p.q)
+    check(p, workspace, q=q)
+
+
+@pytest.mark.parametrize("order", [(0, 2, 1), (2, 0, 1), (1, 0, 2)])
+def test_orders_of_a_cache(workspace, order):
+    check(Packed([(3, 50), (9, 20)], order=order, group=2), workspace)
+
+
+def test_pages_that_are_none(workspace):
+    p = Packed([(20, 100)], heads=1, group=2)
+    p.table[0, 1], p.table[0, 3] = -1, 1 << 30
+    weights, _ = check(p, workspace, with_before=False, dead=[(0, 1), (0, 3)])
+    assert not weights[0, 16:32].any() and not weights[0, 48:64].any()
+
+
+def test_queries_without_a_number_give_nothing(workspace):
+    p = Packed([(6, 50)], heads=1, group=2)
+    lse = p.exact_lse()
+    lse[1, 0], lse[2, 1], lse[3, 0] = np.nan, -np.inf, np.inf
+    check(p, workspace, lse=lse)
+
+
+def test_a_scale_of_nan(workspace):
+    p = Packed([(20, 60)], heads=2, group=2)
+    lse = p.exact_lse()
+    p.k_scale[int(p.table[0, 3]), 2, 1] = float("nan")  # token 50: the first ten queries do not see it
+    weights, want = check(p, workspace, lse=lse)
+    assert np.isnan(want).sum() == 1
+
+
+def test_starts_that_decrease_or_leave_the_rows(workspace):
+    p = Packed([(20, 60), (20, 60), (20, 60)], heads=1, group=2)
+    _, pages, lens = p.plan()
+    for starts in ([0, 1 << 30, -5, 60], [50, 10, 70, 2], [-(1 << 31), (1 << 31) - 1, 0, (1 << 31) - 1]):
+        weights = torch.full((5, 64), 7.0, device="cuda")
+        r = dl.KvWeigh(p.cache(), p.q, torch.zeros((60, 2), device="cuda"), torch.tensor(starts, dtype=torch.int32, device="cuda"), pages, lens, weights[1:4])
+        r.use_workspace(workspace)
+        dl.dl_kv_weigh(r, torch.cuda.current_stream())
+        assert (weights[0] == 7).all() and (weights[4] == 7).all() and torch.isfinite(weights).all()
+
+
+def test_no_queries(workspace):
+    """What was there before, or zeros."""
+    p = Packed([(0, 20), (0, 3)])
+    weights, _ = check(p, workspace)
+    weights, _ = check(p, workspace, with_before=False)
+    assert not weights.any()
+
+
+def test_the_same_bits_again(workspace):
+    p = Packed([(70, 400), (3, 900)], heads=4, group=2)
+    lse = p.put(p.exact_lse()).float()
+    said = []
+    for _ in range(4):
+        weights = torch.empty((2, p.table.shape[1] * 16), device="cuda")
+        r = dl.KvWeigh(p.cache(), p.q, lse, *p.plan(), weights)
+        r.use_workspace(workspace)
+        dl.dl_kv_weigh(r, torch.cuda.current_stream())
+        said.append(weights)
+    assert all(torch.equal(said[0], w) for w in said)
