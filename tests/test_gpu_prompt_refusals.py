@@ -82,7 +82,7 @@ def test_weigh(field, value):
     r = weigh()
     setattr(r.desc, field, value)
     refused(dl.dl_kv_weigh, r)
-    assert not r._tensors[6].any()
+    assert not r._tensors[5].any()
 
 
 @pytest.mark.parametrize("field,value", [
