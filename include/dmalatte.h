@@ -736,8 +736,8 @@ typedef struct dl_chunk_attention_args {
     int64_t pages_stride;
     int64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride;
     int32_t type;                 /* of q and out: DL_TYPE_BF16 or DL_TYPE_F16 */
-    int32_t batch;                /* 0 .. 65536 */
-    int32_t q_heads;              /* a multiple of the cache's heads */
+    int32_t batch;                /* 0 .. 65535 */
+    int32_t q_heads;              /* a multiple of the cache's heads, at most 65536 */
     float scale;                  /* what the scores are multiplied with */
 } dl_chunk_attention_args;
 
@@ -768,8 +768,8 @@ typedef struct dl_kv_weigh_args {
     int64_t before_stride, weights_stride;
     int64_t q_token_stride, q_head_stride;
     int32_t type;                 /* of q: DL_TYPE_BF16 or DL_TYPE_F16 */
-    int32_t batch;                /* 0 .. 65536 */
-    int32_t q_heads;              /* a multiple of the cache's heads */
+    int32_t batch;                /* 0 .. 65535 */
+    int32_t q_heads;              /* a multiple of the cache's heads, at most 65536 */
     float scale;                  /* what the scores are multiplied with */
 } dl_kv_weigh_args;
 
@@ -797,7 +797,7 @@ typedef struct dl_kv_evict_args {
     size_t workspace_bytes;
     int64_t max_pages;            /* max_pages * page_tokens <= 2^30 */
     int64_t pages_stride, to_pages_stride, weights_stride, kept_weights_stride;
-    int32_t batch;                /* 0 .. 65536 */
+    int32_t batch;                /* 0 .. 65535 */
     int32_t keep;                 /* batch * keep * cache heads <= DL_MAX_ROWS */
     int32_t first, recent;        /* first + recent <= keep */
 } dl_kv_evict_args;

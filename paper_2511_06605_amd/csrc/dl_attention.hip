@@ -871,15 +871,6 @@ __global__ void __launch_bounds__(ATT_THREADS) dl_attention_join_kernel(const at
 
 uint32_t ceil_div(uint64_t a, uint64_t b) { return (uint32_t)((a + b - 1) / b); }
 
-template <class F>
-void with_bool(bool b, F f)
-{
-    if (b)
-        f(std::true_type{});
-    else
-        f(std::false_type{});
-}
-
 struct att_shape {
     uint32_t nt;
     bool wide;  // pieces of the prefix are wide ones
@@ -1036,9 +1027,9 @@ extern "C" int dl_prefix_attention(const dl_kv_cache *cache, const dl_prefix_att
             constexpr int DP = decltype(dp)::value;
             if (grid)
                 dl_with_format(cache->format, [&](auto c) {
-                    with_bool(aligned, [&](auto al) {
-                        with_bool(sh.wide, [&](auto wd) {
-                            with_bool(sh.nt == 2, [&](auto two) {
+                    dl_with_bool(aligned, [&](auto al) {
+                        dl_with_bool(sh.wide, [&](auto wd) {
+                            dl_with_bool(sh.nt == 2, [&](auto two) {
                                 hipLaunchKernelGGL((dl_attention_kernel<decltype(q), decltype(c), DP, decltype(two)::value ? 2 : 1, decltype(al)::value,
                                                                         decltype(wd)::value>),
                                                    dim3((uint32_t)grid), dim3(ATT_THREADS), 0, hs, a);

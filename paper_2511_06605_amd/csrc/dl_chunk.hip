@@ -29,6 +29,7 @@ struct chunk_args {
     float *partial;  // head_dim sums
     int64_t q_token, q_head, out_token, out_head;  // bytes
     uint32_t q_heads, group;
+    dl_divider groups;  // by group
     uint32_t target;  // see chunk_plan; 0: a piece a tile
     float scale;      // times log2 e
 };
@@ -117,7 +118,7 @@ struct chunk_rows {
         ahead = (int32_t)len - (int32_t)n;
         end = seen_by(a, min(row0 + CH_ROWS, rows) - 1u);
     }
-    __device__ __forceinline__ uint32_t seen_by(const chunk_args &a, uint32_t row) const { return (uint32_t)max(ahead + (int32_t)(row / a.group) + 1, 0); }
+    __device__ __forceinline__ uint32_t seen_by(const chunk_args &a, uint32_t row) const { return (uint32_t)max(ahead + (int32_t)(dl_divide(row, a.groups)) + 1, 0); }
 };
 
 template <int DP>
@@ -158,7 +159,7 @@ __global__ void __launch_bounds__(CH_THREADS, DP <= 128 ? 2 : 1) dl_chunk_kernel
     const char *const k_from = a.c.k + (int64_t)head * a.c.head_stride, *const v_from = a.c.v + (int64_t)head * a.c.head_stride;
 
     const uint32_t wave_row = t.row0 + wave * 32u, my = wave_row + i, row = min(my, t.rows - 1u);
-    const uint32_t j = row / a.group, h = head * a.group + row - j * a.group;
+    const uint32_t j = dl_divide(row, a.groups), h = head * a.group + row - j * a.group;
     const int32_t last = t.ahead + (int32_t)j;
     // keys before whole_end are seen by all rows of the wavefront, those from wave_end on by none
     const uint32_t wave_end = wave_row < t.rows ? min(t.seen_by(a, min(wave_row + 32u, t.rows) - 1u), end) : 0u;
@@ -330,7 +331,7 @@ __global__ void __launch_bounds__(CH_THREADS, DP <= 128 ? 2 : 1) dl_chunk_kernel
             if (key0 + 32u > whole_end) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    if ((int32_t)(key0 + 2u * (e & ~3) + 4u * half + (e & 3)) > last) s[e] = -INFINITY;
+                    if (2 * (e & ~3) + (e & 3) > last - (int32_t)(key0 + 4u * half)) s[e] = -INFINITY;
             }
 #pragma unroll
             for (int e = 0; e < 16; ++e) top = fmaxf(top, s[e]);
@@ -442,7 +443,7 @@ __global__ void __launch_bounds__(CH_THREADS) dl_chunk_join_kernel(const chunk_a
             }
         }
         const bool none = l == 0.0f;
-        const uint32_t j = row / a.group, h = head * a.group + row - j * a.group;
+        const uint32_t j = dl_divide(row, a.groups), h = head * a.group + row - j * a.group;
         const float f = none ? 0.0f : 1.0f / l;
         if (d0 < D)
             dl_store_at(a.out + (uint64_t)(t.first + j) * a.out_token + h * a.out_head + 2u * d0,
@@ -514,6 +515,7 @@ extern "C" int dl_chunk_attention(const dl_kv_cache *cache, const dl_chunk_atten
     a.out_head = 2 * args->out_head_stride;
     a.q_heads = (uint32_t)args->q_heads;
     a.group = a.q_heads / a.c.heads;
+    a.groups = dl_make_divider(a.group ? a.group : 1u);
     a.target = sh.target;
     a.scale = args->scale * DL_LOG2E;
     const uint64_t grid = sh.units * a.c.heads;

@@ -262,6 +262,14 @@ struct dl_value_scale {
     __device__ __forceinline__ float over_c() const { return __builtin_amdgcn_rcpf(c == c ? c : 1.0f); }
 };
 
+template <class F>
+static inline void dl_with_bool(bool b, F f)
+{
+    if (b)
+        f(std::true_type{});
+    else
+        f(std::false_type{});
+}
 // Calls f with the types that belong to a dl_kv_format / to a 16-bit dl_type.
 template <class F>
 static inline void dl_with_format(int32_t format, F f)

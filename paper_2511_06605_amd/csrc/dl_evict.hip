@@ -12,6 +12,8 @@ namespace {
 
 constexpr uint32_t PICK_THREADS = 1024, PICK_WAVES = PICK_THREADS / 64;
 constexpr uint32_t DIGIT_BITS = 8, DIGITS = 1u << DIGIT_BITS;
+// Counts of a digit that lanes take in turn: weights share their upper bits, and counts at one address wait for each other.
+constexpr uint32_t COPIES = 16;
 constexpr uint32_t MOVE_THREADS = 256;
 
 struct evict_args {
@@ -27,98 +29,166 @@ struct evict_args {
     uint32_t lanes;  // a row of the move takes, a power of two
 };
 
-// Whole numbers in the order of weights: 0 for NaN, both zeros alike.
+// Whole numbers in the order of weights, both zeros alike: 1 for NaN, above it 2^23 - 1 (-infinity) to 0xFF800000.  0 is what is no token, and the
+// largest number what stays in any case: so the tokens that stay are the `keep` with the largest numbers.
+constexpr uint32_t FIXED = ~0u;
 __device__ __forceinline__ uint32_t order_of(float w)
 {
     const uint32_t u = dl_bits<uint32_t>(w + 0.0f);  // (-0 + 0 = 0)
-    return w != w ? 0u : u >> 31 ? ~u : u | 0x80000000u;
+    return w != w ? 1u : u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+
+// Numbers of so many tokens fit LDS.
+constexpr uint32_t PICK_HELD = 32768;
+
+struct pick_lds {
+    __align__(16) uint32_t held[PICK_HELD];
+    uint32_t count[DIGITS * COPIES];
+    uint32_t totals[PICK_WAVES], above[PICK_WAVES], equal[PICK_WAVES];
+    uint32_t digit, left, here;
+};
+
+// Which tokens of a sequence of n > keep stay.  A wavefront has `share` tokens in a row (a multiple of 256).  HELD: from the first look on their
+// numbers come from LDS, else they are made from memory each time.
+template <bool HELD>
+__device__ __forceinline__ void pick(const evict_args &a, const float *weights, int32_t *kept, uint32_t n, pick_lds &lds)
+{
+    const uint32_t thread = threadIdx.x, lane = thread % 64u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(thread / 64u));
+    const uint32_t share = (n + 4u * PICK_THREADS - 1u) / (4u * PICK_THREADS) * 256u, from = wave * share, to = from + share;
+    const uint32_t end = n - a.recent;
+    auto number = [&](uint32_t i, float w) { return i >= n ? 0u : i < a.first || i >= end ? FIXED : order_of(w); };
+    // f(token of the first lane, four numbers a lane, one behind the other): 256 tokens at a time; tokens from n on are none
+    auto from_memory = [&](auto f) {
+        constexpr uint32_t AHEAD = 8;  // loads on their way at once
+        for (uint32_t i0 = from; i0 < to; i0 += 256u * AHEAD) {
+            dl_f32x4 w[AHEAD];
+#pragma unroll
+            for (uint32_t x = 0; x < AHEAD; ++x) {
+                const uint32_t i = i0 + 256u * x + 4u * lane;
+                if (i + 4u <= n) {
+                    w[x] = dl_load_at<dl_f32x4>(weights + i);
+                } else {
+#pragma unroll
+                    for (uint32_t c = 0; c < 4u; ++c) w[x][c] = weights[min(i + c, n - 1u)];
+                }
+            }
+#pragma unroll
+            for (uint32_t x = 0; x < AHEAD; ++x) {
+                const uint32_t i = i0 + 256u * x + 4u * lane;
+                if (i0 + 256u * x < to) f(i0 + 256u * x, dl_u32x4{number(i, w[x][0]), number(i + 1u, w[x][1]), number(i + 2u, w[x][2]), number(i + 3u, w[x][3])});
+            }
+        }
+    };
+    auto each = [&](auto f) {
+        if constexpr (HELD) {
+            constexpr uint32_t AHEAD = 2;
+            for (uint32_t i0 = from; i0 < to; i0 += 256u * AHEAD) {
+                dl_u32x4 k[AHEAD];
+#pragma unroll
+                for (uint32_t x = 0; x < AHEAD; ++x) k[x] = *(const dl_u32x4 *)&lds.held[min(i0 + 256u * x, to - 256u) + 4u * lane];
+#pragma unroll
+                for (uint32_t x = 0; x < AHEAD; ++x)
+                    if (i0 + 256u * x < to) f(i0 + 256u * x, k[x]);
+            }
+        } else {
+            from_memory(f);
+        }
+    };
+    // The number of the last that stays, and how many of those equal to it do (fewer stay than there are, since n > keep).
+    uint32_t left = a.keep, known = 0, mask = 0;
+    for (int shift = 32 - (int)DIGIT_BITS; left && shift >= 0; shift -= (int)DIGIT_BITS) {
+        for (uint32_t x = thread; x < DIGITS * COPIES; x += PICK_THREADS) lds.count[x] = 0;
+        __syncthreads();
+        auto count = [&](dl_u32x4 k) {
+#pragma unroll
+            for (uint32_t c = 0; c < 4u; ++c)
+                if ((k[c] & mask) == known) atomicAdd(&lds.count[(k[c] >> shift & (DIGITS - 1u)) * COPIES + lane % COPIES], 1u);
+        };
+        if (HELD && !mask)
+            from_memory([&](uint32_t i0, dl_u32x4 k) {
+                *(dl_u32x4 *)&lds.held[i0 + 4u * lane] = k;
+                count(k);
+            });
+        else
+            each([&](uint32_t, dl_u32x4 k) { count(k); });
+        __syncthreads();
+        // a digit a thread, from the top; the one at which the count reaches what is left
+        uint32_t own = 0;
+        if (thread < DIGITS) {
+#pragma unroll
+            for (uint32_t c = 0; c < COPIES; ++c) own += lds.count[(DIGITS - 1u - thread) * COPIES + (c + thread) % COPIES];
+        }
+        const uint32_t up_to = dl_sum_up_to(own);
+        if (lane == 63u) lds.totals[wave] = up_to;
+        __syncthreads();
+        uint32_t before = up_to - own;
+        for (uint32_t v = 0; v < wave && v < DIGITS / 64u; ++v) before += lds.totals[v];
+        if (before < left && before + own >= left) lds.digit = DIGITS - 1u - thread, lds.left = left - before, lds.here = own;
+        __syncthreads();
+        known |= lds.digit << shift;
+        mask |= (DIGITS - 1u) << shift;
+        left = lds.left;
+        if (lds.here == left) {  // all that share what is known stay: those above the lowest that there could be, and all equal to it
+            left = n;
+            break;
+        }
+    }
+    if (!left) known = FIXED;  // (none stays)
+    uint32_t over_here = 0, same_here = 0;
+    auto walk = [&](auto f) {
+        if (HELD && !a.keep) return;  // (nothing is held)
+        each(f);
+    };
+    walk([&](uint32_t, dl_u32x4 k) {
+#pragma unroll
+        for (uint32_t c = 0; c < 4u; ++c) {
+            over_here += (uint32_t)__popcll(__ballot(k[c] > known));
+            same_here += (uint32_t)__popcll(__ballot(k[c] == known));
+        }
+    });
+    if (lane == 0) lds.above[wave] = over_here, lds.equal[wave] = same_here;
+    __syncthreads();
+    uint32_t placed = 0, ties = 0;
+    for (uint32_t v = 0; v < wave; ++v) placed += lds.above[v], ties += lds.equal[v];
+    walk([&](uint32_t i0, dl_u32x4 k) {
+        // of the lanes before this one
+        uint32_t at_over = placed, at_same = ties;
+#pragma unroll
+        for (uint32_t c = 0; c < 4u; ++c) {
+            const unsigned long long over = __ballot(k[c] > known), same = __ballot(k[c] == known);
+            at_over = __builtin_amdgcn_mbcnt_hi((uint32_t)(over >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)over, at_over));
+            at_same = __builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, at_same));
+            placed += (uint32_t)__popcll(over);
+            ties += (uint32_t)__popcll(same);
+        }
+#pragma unroll
+        for (uint32_t c = 0; c < 4u; ++c) {
+            // (of those before it, the ones above and as many of the equal ones as stay)
+            if (k[c] > known || (k[c] == known && at_same < left)) kept[at_over + min(at_same, left)] = (int32_t)(i0 + 4u * lane + c);
+            at_over += k[c] > known;
+            at_same += k[c] == known;
+        }
+    });
 }
 
 __global__ void __launch_bounds__(PICK_THREADS) dl_evict_pick_kernel(const evict_args a)
 {
-    __shared__ uint32_t count[PICK_WAVES][DIGITS];
-    __shared__ uint32_t above[PICK_WAVES], equal[PICK_WAVES];
-    __shared__ uint32_t found[2];
-    const uint32_t b = blockIdx.x, thread = threadIdx.x, lane = thread % 64u, wave = thread / 64u;
+    __shared__ pick_lds lds;
+    const uint32_t b = blockIdx.x, thread = threadIdx.x;
     const float *const weights = a.weights + b * a.weights_stride;
     int32_t *const kept = a.kept + (uint64_t)b * a.keep;
-    float *const kept_weights = a.kept_weights ? a.kept_weights + b * a.kept_weights_stride : nullptr;
-    const uint32_t n = a.most ? min((uint32_t)max(a.lens[b], 0), a.most) : 0u, m = min(n, a.keep);
-    if (thread == 0) a.kept_lens[b] = (int32_t)m;
-    for (uint32_t j = m + thread; j < a.keep; j += PICK_THREADS) {
-        kept[j] = -1;
-        if (kept_weights) kept_weights[j] = 0.0f;
-    }
+    const uint32_t n = a.most ? min((uint32_t)max(a.lens[b], 0), a.most) : 0u;
+    if (thread == 0) a.kept_lens[b] = (int32_t)min(n, a.keep);
     if (n <= a.keep) {
-        for (uint32_t j = thread; j < n; j += PICK_THREADS) {
-            kept[j] = (int32_t)j;
-            if (kept_weights) kept_weights[j] = weights[j];
-        }
-        return;
-    }
-    // The others: tokens first .. end - 1, of which `left` stay (fewer than there are, since n > keep).
-    const uint32_t end = n - a.recent;
-    uint32_t left = a.keep - a.first - a.recent, known = 0;
-    if (left) {
-        for (int shift = 32 - (int)DIGIT_BITS; shift >= 0; shift -= (int)DIGIT_BITS) {
-            for (uint32_t x = lane; x < DIGITS; x += 64u) count[wave][x] = 0;
-            __syncthreads();
-            for (uint32_t i = a.first + thread; i < end; i += PICK_THREADS) {
-                const uint32_t k = order_of(weights[i]);
-                if (shift + (int)DIGIT_BITS == 32 || k >> (shift + (int)DIGIT_BITS) == known) atomicAdd(&count[wave][k >> shift & (DIGITS - 1u)], 1u);
-            }
-            __syncthreads();
-            if (wave == 0) {
-                // four digits a lane, the highest in lane 0; the digit at which the count from the top reaches what is left
-                uint32_t own[4], sum = 0;
-#pragma unroll
-                for (uint32_t x = 0; x < 4u; ++x) {
-                    own[x] = 0;
-                    for (uint32_t v = 0; v < PICK_WAVES; ++v) own[x] += count[v][DIGITS - 1u - (4u * lane + x)];
-                    sum += own[x];
-                }
-                uint32_t before = dl_sum_up_to(sum) - sum;
-#pragma unroll
-                for (uint32_t x = 0; x < 4u; ++x) {
-                    if (before < left && before + own[x] >= left) found[0] = DIGITS - 1u - (4u * lane + x), found[1] = left - before;
-                    before += own[x];
-                }
-            }
-            __syncthreads();
-            known = known << DIGIT_BITS | found[0];
-            left = found[1];
-        }
-    }
-    // `left`: how many of those equal to `known` stay, the lowest.  (None looked for: all are lighter than what stays.)
-    const bool some = a.keep > a.first + a.recent;
-    uint32_t placed = 0, ties = 0;
-    for (uint32_t i0 = 0; i0 < n; i0 += PICK_THREADS) {
-        const uint32_t i = i0 + thread;
-        const bool there = i < n, fixed = there && (i < a.first || i >= end);
-        const float w = there ? weights[i] : 0.0f;
-        const uint32_t k = order_of(w);
-        const bool over = fixed || (some && there && k > known), same = some && there && !fixed && k == known;
-        const unsigned long long all_over = __ballot(over), all_same = __ballot(same), below = (1ull << lane) - 1u;
-        if (lane == 0) above[wave] = (uint32_t)__popcll(all_over), equal[wave] = (uint32_t)__popcll(all_same);
-        __syncthreads();
-        uint32_t at_over = placed, at_same = ties;
-        for (uint32_t v = 0; v < PICK_WAVES; ++v) {
-            if (v < wave) at_over += above[v], at_same += equal[v];
-            placed += above[v], ties += equal[v];
-        }
-        at_over += (uint32_t)__popcll(all_over & below);
-        at_same += (uint32_t)__popcll(all_same & below);
-        // (of those before it, the ones above and as many of the equal ones as stay)
-        if (over || (same && at_same < left)) {
-            const uint32_t j = at_over + min(at_same, left);
-            kept[j] = (int32_t)i;
-            if (kept_weights) kept_weights[j] = w;
-        }
-        __syncthreads();
+        for (uint32_t j = thread; j < a.keep; j += PICK_THREADS) kept[j] = j < n ? (int32_t)j : -1;
+    } else if (n <= PICK_HELD) {
+        pick<true>(a, weights, kept, n, lds);
+    } else {
+        pick<false>(a, weights, kept, n, lds);
     }
 }
 
-// blockIdx.y: 0 keys, 1 values.
+// blockIdx.y: 0 keys, 1 values.  The first head's keys take a token's weight along.
 template <int ROWS>
 __global__ void __launch_bounds__(MOVE_THREADS) dl_evict_move_kernel(const evict_args a)
 {
@@ -137,6 +207,8 @@ __global__ void __launch_bounds__(MOVE_THREADS) dl_evict_move_kernel(const evict
         seq[r] = token[r] / a.keep;
         j[r] = token[r] - seq[r] * a.keep;
         source[r] = row0 + r * per < a.rows ? a.kept[token[r]] : -1;
+        if (a.kept_weights && row0 + r * per < a.rows && head[r] == 0 && lane == 0 && blockIdx.y == 0)
+            a.kept_weights[seq[r] * a.kept_weights_stride + j[r]] = source[r] >= 0 ? a.weights[seq[r] * a.weights_stride + source[r]] : 0.0f;
     }
     uint32_t page[ROWS], to_page[ROWS], in[ROWS], to_in[ROWS];
 #pragma unroll

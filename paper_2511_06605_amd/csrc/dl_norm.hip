@@ -14,66 +14,67 @@ struct norm_side {
     char *y;
     const float *weight;
     int64_t token, head, out_token, out_head;  // bytes
+    uint32_t heads;
 };
 struct norm_args {
     norm_side q, k;
     const float *table;
     const int64_t *positions;
     int64_t table_rows, table_stride;  // floats
-    uint32_t rows, q_heads, head_dim, rotary;
-    dl_divider heads;  // q_heads + k_heads
+    uint32_t head_dim, rotary;
+    // a part is a thread's heads of one token; those of q come first
+    uint32_t tasks, q_parts;
+    dl_divider parts;  // of a token
     float over_dim, eps;
     int32_t neighbours;
 };
 
 constexpr uint32_t NORM_THREADS = 256;
 constexpr int NORM_ELEMENTS = 8;
-// From so many threads on two rows of a thread are on their way at once and stores go past the caches.
+// From so many threads on, four rows of a thread are on their way at once and stores go past the caches.
 constexpr uint64_t NORM_MANY_THREADS = 1ull << 20;
 
-template <class T, int LANES, bool MANY>
+// A thread has ROWS heads of one side of one token, which share the token's cosines and sines and the side's weights.
+template <class T, int LANES, int ROWS, bool STREAM>
 __global__ void __launch_bounds__(NORM_THREADS) dl_norm_rotate_kernel(const norm_args a)
 {
-    constexpr int ROWS = MANY ? 2 : 1, N = NORM_ELEMENTS;
-    const uint32_t lane = threadIdx.x % LANES, row0 = blockIdx.x * (NORM_THREADS / LANES * ROWS) + threadIdx.x / LANES;
+    constexpr int N = NORM_ELEMENTS;
+    const uint32_t lane = threadIdx.x % LANES, task = blockIdx.x * (NORM_THREADS / LANES) + threadIdx.x / LANES;
     const uint32_t at = lane * (uint32_t)N, half = a.rotary / 2u;
     const bool mine = at < a.head_dim, turned = at < a.rotary;
     // which pairs: of the lane's elements as first or second of theirs, or its own neighbours
     const bool second = !a.neighbours && at >= half;
     const uint32_t angle = a.neighbours ? at / 2u : second ? at - half : at;
-    float x[ROWS][N], w[ROWS][N], c[ROWS][N], z[ROWS][N];
-    bool live[ROWS], normed[ROWS];
-    char *to[ROWS];
+    const uint32_t part = min(task, a.tasks - 1u), token = dl_divide(part, a.parts);
+    uint32_t h0 = part - token * a.parts.d;
+    const bool is_q = h0 < a.q_parts;
+    const norm_side &s = is_q ? a.q : a.k;
+    h0 = (is_q ? h0 : h0 - a.q_parts) * ROWS;
+    const bool normed = s.weight != nullptr;
+    bool live = task < a.tasks && mine;
+    float x[ROWS][N], w[N], c[N], z[N];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-        const uint32_t row = row0 + r * (NORM_THREADS / LANES), from = min(row, a.rows - 1u), token = dl_divide(from, a.heads);
-        uint32_t h = from - token * a.heads.d;
-        const bool is_q = h < a.q_heads;
-        const norm_side &s = is_q ? a.q : a.k;
-        if (!is_q) h -= a.q_heads;
-        live[r] = row < a.rows && mine;
-        to[r] = s.y + token * s.out_token + h * s.out_head + (size_t)at * T::size;
-        normed[r] = s.weight != nullptr;
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[r][i] = 0.0f, w[r][i] = 1.0f, c[r][i] = 1.0f, z[r][i] = 0.0f;
-        if (mine) {
-            dl_load_row<T>(s.x + token * s.token + h * s.head + (size_t)at * T::size, x[r]);
-            if (normed[r]) dl_load_row<dl_f32>((const char *)(s.weight + at), w[r]);
-        }
-        if (a.rotary) {
-            const int64_t position = a.positions[token];
-            const bool known = position >= 0 && position < a.table_rows;
-            live[r] &= known;
-            if (turned && known) {
-                const char *const p = (const char *)(a.table + position * a.table_stride + angle);
-                if (a.neighbours) {
-                    const dl_f32x4 u = dl_load_at<dl_f32x4>(p), v = dl_load_at<dl_f32x4>(p + 4u * half);
+        for (int i = 0; i < N; ++i) x[r][i] = 0.0f;
+        if (mine) dl_load_row<T>(s.x + token * s.token + min(h0 + r, s.heads - 1u) * s.head + (size_t)at * T::size, x[r]);
+    }
 #pragma unroll
-                    for (int i = 0; i < N; ++i) c[r][i] = u[i / 2], z[r][i] = v[i / 2];
-                } else {
-                    dl_load_row<dl_f32>(p, c[r]);
-                    dl_load_row<dl_f32>(p + 4u * half, z[r]);
-                }
+    for (int i = 0; i < N; ++i) w[i] = 1.0f, c[i] = 1.0f, z[i] = 0.0f;
+    if (mine && normed) dl_load_row<dl_f32>((const char *)(s.weight + at), w);
+    if (a.rotary) {
+        const int64_t position = a.positions[token];
+        const bool known = position >= 0 && position < a.table_rows;
+        live &= known;
+        if (turned && known) {
+            const char *const p = (const char *)(a.table + position * a.table_stride + angle);
+            if (a.neighbours) {
+                const dl_f32x4 u = dl_load_at<dl_f32x4>(p), v = dl_load_at<dl_f32x4>(p + 4u * half);
+#pragma unroll
+                for (int i = 0; i < N; ++i) c[i] = u[i / 2], z[i] = v[i / 2];
+            } else {
+                dl_load_row<dl_f32>(p, c);
+                dl_load_row<dl_f32>(p + 4u * half, z);
             }
         }
     }
@@ -84,10 +85,10 @@ __global__ void __launch_bounds__(NORM_THREADS) dl_norm_rotate_kernel(const norm
         for (int i = 0; i < N; ++i) sum = fmaf(x[r][i], x[r][i], sum);
 #pragma unroll
         for (int d = 1; d < LANES; d *= 2) sum += __shfl_xor(sum, d);
-        if (normed[r]) {
+        if (normed) {
             const float f = rsqrtf(fmaf(sum, a.over_dim, a.eps));
 #pragma unroll
-            for (int i = 0; i < N; ++i) x[r][i] = x[r][i] * f * w[r][i];
+            for (int i = 0; i < N; ++i) x[r][i] = x[r][i] * f * w[i];
         }
         if (a.rotary) {
             float y[N];
@@ -95,17 +96,17 @@ __global__ void __launch_bounds__(NORM_THREADS) dl_norm_rotate_kernel(const norm
 #pragma unroll
                 for (int i = 0; i < N; ++i) y[i] = x[r][i ^ 1] * (i % 2 ? 1.0f : -1.0f);
             } else {
-                // (all lanes take part; those behind the rotated elements get something, which z = 0 would let infinities into)
+                // (all lanes take part; those behind the rotated elements stay as they are, whatever they get)
                 const uint32_t self = threadIdx.x % 64u, other = turned ? second ? self - half / N : self + half / N : self;
 #pragma unroll
                 for (int i = 0; i < N; ++i) y[i] = __shfl(x[r][i], (int)other) * (second ? 1.0f : -1.0f);
             }
             if (turned) {
 #pragma unroll
-                for (int i = 0; i < N; ++i) x[r][i] = fmaf(x[r][i], c[r][i], y[i] * z[r][i]);
+                for (int i = 0; i < N; ++i) x[r][i] = fmaf(x[r][i], c[i], y[i] * z[i]);
             }
         }
-        if (live[r]) dl_store_row<T, MANY>(to[r], x[r]);
+        if (live && h0 + r < s.heads) dl_store_row<T, STREAM>(s.y + token * s.out_token + (h0 + r) * s.out_head + (size_t)at * T::size, x[r]);
     }
 }
 
@@ -129,18 +130,15 @@ int norm_setup(const dl_norm_rotate_args *args, norm_args *a, bool *nothing)
         ((uint64_t)args->q_weight | (uint64_t)args->k_weight | (uint64_t)args->table) % 4u || (uint64_t)args->positions % 8u)
         return DL_ERR_INVALID;
     a->q = {(const char *)args->q, (char *)args->q_out, args->q_weight, args->q_token_stride * size, args->q_head_stride * size,
-            args->q_out_token_stride * size, args->q_out_head_stride * size};
+            args->q_out_token_stride * size, args->q_out_head_stride * size, (uint32_t)q_heads};
     a->k = {(const char *)args->k, (char *)args->k_out, args->k_weight, args->k_token_stride * size, args->k_head_stride * size,
-            args->k_out_token_stride * size, args->k_out_head_stride * size};
+            args->k_out_token_stride * size, args->k_out_head_stride * size, (uint32_t)(heads - q_heads)};
     a->table = args->table;
     a->positions = args->positions;
     a->table_rows = args->table_rows;
     a->table_stride = args->table_stride;
-    a->rows = (uint32_t)(args->tokens * heads);
-    a->q_heads = (uint32_t)q_heads;
     a->head_dim = (uint32_t)args->head_dim;
     a->rotary = (uint32_t)args->rotary;
-    a->heads = dl_make_divider((uint32_t)heads);
     a->over_dim = 1.0f / (float)args->head_dim;
     a->eps = args->eps;
     a->neighbours = args->neighbours;
@@ -161,16 +159,25 @@ extern "C" int dl_norm_rotate(const dl_norm_rotate_args *args, void *stream)
     dl_with_type(args->type, [&](auto t) {
         dl_with_lanes<NORM_ELEMENTS>(a.head_dim, [&](auto lanes) {
             constexpr int L = decltype(lanes)::value;
-            auto go = [&](auto many) {
-                constexpr bool MANY = decltype(many)::value;
-                constexpr uint32_t ROWS = NORM_THREADS / L * (MANY ? 2 : 1);
-                hipLaunchKernelGGL((dl_norm_rotate_kernel<decltype(t), L, MANY>), dim3((a.rows + ROWS - 1u) / ROWS), dim3(NORM_THREADS), 0,
-                                   (hipStream_t)stream, a);
+            auto go = [&](auto rows, auto stream_stores) {
+                constexpr int ROWS = decltype(rows)::value;
+                a.q_parts = (a.q.heads + ROWS - 1u) / ROWS;
+                const uint32_t parts = a.q_parts + (a.k.heads + ROWS - 1u) / ROWS;
+                a.parts = dl_make_divider(parts);
+                a.tasks = (uint32_t)args->tokens * parts;
+                hipLaunchKernelGGL((dl_norm_rotate_kernel<decltype(t), L, ROWS, decltype(stream_stores)::value>),
+                                   dim3((a.tasks + NORM_THREADS / L - 1u) / (NORM_THREADS / L)), dim3(NORM_THREADS), 0, (hipStream_t)stream, a);
             };
-            if ((uint64_t)a.rows * L >= NORM_MANY_THREADS)
-                go(std::true_type{});
+            // (heads of a side that do not fill a thread's rows cost it as much as if they were there)
+            auto filled = [&](uint32_t rows) { return 5u * (a.q.heads + a.k.heads) >= 4u * rows * ((a.q.heads + rows - 1u) / rows + (a.k.heads + rows - 1u) / rows); };
+            if ((uint64_t)args->tokens * (a.q.heads + a.k.heads) * L < NORM_MANY_THREADS)
+                go(std::integral_constant<int, 1>{}, std::false_type{});
+            else if (filled(4))
+                go(std::integral_constant<int, 4>{}, std::true_type{});
+            else if (filled(2))
+                go(std::integral_constant<int, 2>{}, std::true_type{});
             else
-                go(std::false_type{});
+                go(std::integral_constant<int, 1>{}, std::true_type{});
         });
     });
     DL_HIP(hipGetLastError());

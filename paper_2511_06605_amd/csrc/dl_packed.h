@@ -22,7 +22,7 @@ static inline int dl_packed_sizes(const dl_kv_cache *cache, const Args *args, dl
     const int rc = dl_cache_check(cache, 0, view);
     if (rc != DL_OK) return rc;
     if (args->type != DL_TYPE_BF16 && args->type != DL_TYPE_F16) return DL_ERR_INVALID;
-    if (args->batch < 0 || args->batch > 65535 || args->q_heads < 0 || args->q_heads % cache->heads) return DL_ERR_INVALID;
+    if (args->batch < 0 || args->batch > 65535 || args->q_heads < 0 || args->q_heads > 65536 || args->q_heads % cache->heads) return DL_ERR_INVALID;
     if (args->tokens < 0 || args->tokens > DL_MAX_ROWS / 2 || args->tokens * args->q_heads > DL_MAX_ROWS / 2) return DL_ERR_INVALID;
     if (args->max_pages < 0 || args->max_pages > 1 << 30 || args->max_pages * cache->page_tokens > 1 << 30) return DL_ERR_INVALID;
     return DL_OK;

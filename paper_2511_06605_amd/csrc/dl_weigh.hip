@@ -1,16 +1,15 @@
 // What cached tokens have been given by queries whose sums are known (dl_kv_weigh).
 //
 // With the scores s and lse in units of ln 2, a token is given the sum over queries and heads of 2^(s - lse).  The lse is known, so no
-// maximum is looked for and the sum is over the queries alone: a wavefront has 32 keys in its lanes, as the right operand of 32 x 32 x 16
-// products whose rows are queries, and adds up in registers over heads and queries.  The wavefronts of a workgroup share out the heads of
-// their keys and add their sums in LDS at the end, in a fixed order.
+// maximum is looked for and the sum is over the queries alone: a wavefront has 32 keys, as the left operand of 32 x 32 x 16 products whose
+// columns are queries, and adds up in registers over heads and queries, a query a lane; the lanes' sums are added at the end.  So in the
+// loop a lane needs one lse, and its keys' scales stay where they are.  All sums are taken in a fixed order.
 #include "dl_codes.h"
 #include "dl_internal.h"
 #include "dl_packed.h"
 
 namespace {
 
-constexpr uint32_t WEIGH_WAVES = 8, WEIGH_THREADS = 64 * WEIGH_WAVES;
 
 struct weigh_args {
     dl_cache_view c;
@@ -22,93 +21,308 @@ struct weigh_args {
     int64_t before_stride, weights_stride;
     uint32_t width;        // entries of a row: max_pages * page_tokens (also where the pool has no pages)
     uint32_t q_heads, group;
-    uint32_t sharing;      // wavefronts that share the heads of their keys: 1, 2, 4 or 8
-    float scale;           // times log2 e
+    dl_divider groups;  // by group
+    uint32_t sharing;      // few queries: wavefronts that share the heads of their keys: 1, 2, 4 or 8
+    // many queries: the heads are shared out over `parts` workgroups, which leave their sums in partial [part][batch][width] (one: none)
+    uint32_t parts;
+    float *partial;
+    float scale;  // times log2 e
 };
 
-template <class Q, class C, int DP>
-__global__ void __launch_bounds__(WEIGH_THREADS, DP <= 128 ? 2 : 1) dl_weigh_kernel(const weigh_args a)
+// The last step of either kernel: x[e] of lane (i, half) is a sum over some queries for key 8 (e / 4) + 4 half + e % 4; over the 32 lanes that hold
+// the same keys, halves of them swap halves of their sums, so that lane i ends with that of e = i % 16.
+__device__ __forceinline__ float over_lanes(float (&x)[16], uint32_t i)
 {
-    constexpr uint32_t PAIRS = DP >= 32 ? DP / 32 : 1;  // of pieces of 16 dims, one for each half of the wavefront
-    __shared__ float sums[WEIGH_WAVES][32];
+#pragma unroll
+    for (int d = 8; d >= 1; d /= 2)
+#pragma unroll
+        for (int e = 0; e < d; ++e) {
+            const bool up = i & (uint32_t)d;
+            const float low = x[e], high = x[e + d];
+            x[e] = (up ? high : low) + __shfl_xor(up ? low : high, d);
+        }
+    return x[0] + __shfl_xor(x[0], 16);
+}
+
+// A tile's scores s: rows are keys (8 (e / 4) + 4 half + e % 4, with the scales ks), columns queries.  lse in units of ln 2; masked: keys from
+// `seen` + 1 on are not seen by the lane's query.
+__device__ __forceinline__ void add_weights(dl_f32x16 &s, const float *ks, float lse, bool masked, int32_t seen, uint32_t half, float (&sum)[16])
+{
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) {
+        const dl_f32x4 k = *(const dl_f32x4 *)&ks[2u * e + 4u * half];
+#pragma unroll
+        for (int f = 0; f < 4; ++f) s[e + f] = fmaf(s[e + f], k[f], -lse);
+    }
+    if (masked) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            if (2 * (e & ~3) + (e & 3) > seen - 4 * (int32_t)half) s[e] = -INFINITY;
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sum[e] += __builtin_amdgcn_exp2f(s[e]);
+}
+
+// A lane's key: where its codes and its scale are, and whether it is one.
+struct weigh_key {
+    const char *codes, *scale;
+    bool alive;
+    __device__ __forceinline__ weigh_key(const weigh_args &a, uint32_t b, uint32_t key, uint32_t len)
+    {
+        const uint32_t at = min(key, len - 1u), n = dl_divide(at, a.c.page), in = at - n * a.c.page.d;
+        uint32_t page = (uint32_t)a.p.pages[b * a.p.pages_stride + n];
+        alive = page < a.c.pages && key < len;
+        page = page < a.c.pages ? page : 0u;
+        codes = a.c.k + (uint64_t)page * a.c.page_stride + (uint64_t)in * a.c.token_stride;
+        scale = (const char *)a.c.k_scale + (uint64_t)page * a.c.scale_page_stride + (uint64_t)in * a.c.scale_token_stride;
+    }
+};
+
+// Few queries: what is read is the keys.  The wavefronts of a workgroup share out the heads of their keys, and every operand comes from memory
+// straight into registers.
+// WHOLE: head_dim is DP, and the places of a row's pieces are known.
+constexpr uint32_t FEW_WAVES = 8;
+template <class Q, class C, int DP, bool WHOLE>
+__global__ void __launch_bounds__(64 * FEW_WAVES, DP <= 128 ? 4 : 2) dl_weigh_few_kernel(const weigh_args a)
+{
+    constexpr uint32_t PAIRS = DP / 32;  // of pieces of 16 dims, one for each half of the wavefront
+    __shared__ __align__(16) float sums[FEW_WAVES][32];  // (the scales of its keys, until a wavefront has its sums)
+    const uint32_t lane = threadIdx.x % 64u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
+    const uint32_t i = lane % 32u, half = lane / 32u, D = WHOLE ? DP : a.c.head_dim, b = blockIdx.y;
+    const uint32_t share = wave % a.sharing, block_keys = 32u * (FEW_WAVES / a.sharing);
+    const uint32_t first = a.p.start(b), queries = a.p.queries(b, first), rows = queries * a.group, len = a.p.len(b);
+    const int32_t ahead = (int32_t)len - (int32_t)queries;  // query j sees the keys up to ahead + j
+    const uint32_t block0 = (blockIdx.z * gridDim.x + blockIdx.x) * block_keys;
+    if (block0 >= a.width) return;
+    const uint32_t base = block0 + wave / a.sharing * 32u;
+    float sum[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sum[e] = 0.0f;
+    uint32_t dead = ~0u;  // bit key: nothing is given to it
+    if (base < len && rows) {
+        const weigh_key key(a, b, base + i, len);
+        dead = (uint32_t)__ballot(!key.alive);
+        // rows before the first that sees any of the keys are left out, from row whole on all keys are seen
+        const int64_t since = ((int64_t)base - ahead) * a.group, until = ((int64_t)base + 31 - ahead) * a.group;
+        const uint32_t row0 = (uint32_t)max(since, (int64_t)0) & ~31u, whole = (uint32_t)max(until, (int64_t)0);
+#pragma unroll 1
+        for (uint32_t head = share; head < a.c.heads; head += a.sharing) {
+            dl_u32x4 qf[2 * PAIRS];
+            float given;
+            int32_t last;
+            auto load_queries = [&](uint32_t r0) {
+                const uint32_t row = min(r0 + i, rows - 1u), j = dl_divide(row, a.groups), h = head * a.group + row - j * a.group;
+                const char *const q = a.q + (uint64_t)(first + j) * a.q_token + h * a.q_head;
+                given = a.lse[(uint64_t)(first + j) * a.q_heads + h];
+                last = ahead + (int32_t)j - (int32_t)base;
+#pragma unroll
+                for (uint32_t x = 0; x < 2 * PAIRS; ++x)  // (behind head_dim the keys are zero)
+                    qf[x] = dl_load_at<dl_u32x4>(q + 2u * min(16u * (2u * (x / 2) + half) + 8u * (x % 2), D - 8u));
+            };
+            load_queries(row0);
+            dl_words<16> codes[PAIRS];
+#pragma unroll
+            for (uint32_t x = 0; x < PAIRS; ++x) codes[x] = dl_load_words<16>(key.codes + head * a.c.head_stride + min(16u * (2u * x + half), D - 16u));
+#pragma unroll
+            for (uint32_t x = 0; x < PAIRS; ++x)
+                if (16u * (2u * x + half) >= D) codes[x] = dl_words<16>{};
+            const float scale = *(const float *)(key.scale + head * a.c.scale_head_stride);
+            // (what is none gets nothing in the end, but a number until then)
+            if (half == 0) sums[wave][i] = key.alive ? scale * a.scale : 0.0f;
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+            for (uint32_t r0 = row0; r0 < rows; r0 += 32u) {
+                // (a row that is none, or whose lse is no number: nothing is left of it)
+                const float lse = r0 + i < rows && fabsf(given) < INFINITY ? given * DL_LOG2E : INFINITY;
+                const int32_t seen = last;
+                // (elements and scales are made and read anew for each tile: kept, they would cost half the wavefronts)
+#pragma unroll
+                for (uint32_t x = 0; x < PAIRS; ++x)
+#pragma unroll
+                    for (uint32_t u = 0; u < 4; ++u) asm volatile("" : "+v"(codes[x].w[u]));
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                dl_f32x16 s;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[e] = 0.0f;
+#pragma unroll
+                for (uint32_t x = 0; x < 2 * PAIRS; ++x) {
+                    const dl_u32x2 lo = C::template spread<Q>(codes[x / 2].w[2 * (x % 2)]), hi = C::template spread<Q>(codes[x / 2].w[2 * (x % 2) + 1]);
+                    s = Q::mfma32(dl_u32x4{lo[0], lo[1], hi[0], hi[1]}, qf[x], s);
+                }
+                // the next rows are on their way while this one's weights are taken
+                if (r0 + 32u < rows) load_queries(r0 + 32u);
+                add_weights(s, sums[wave], lse, r0 < whole, seen, half, sum);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+    const float its = over_lanes(sum, i);
+    if (i < 16u) sums[wave][8u * (i / 4u) + 4u * half + i % 4u] = its;
+    __syncthreads();
+    const uint32_t key = base + i;
+    if (share == 0 && half == 0 && key < a.width) {
+        float all = sums[wave][i];
+        for (uint32_t w = 1; w < a.sharing; ++w) all += sums[wave + w][i];
+        if (dead >> i & 1u) all = 0.0f;
+        a.weights[b * a.weights_stride + key] = (a.before ? a.before[b * a.before_stride + key] : 0.0f) + all;
+    }
+}
+
+// Many queries: a workgroup's wavefronts have keys of their own and take the same rows of the same head at a time, which go through LDS once for
+// all of them: in registers a lane would load a row's pieces, and every load touch as many lines as there are rows.  Rows lie in 16-byte
+// pieces whose places are exchanged by an exclusive or with the row's number; while a tile of 32 rows is worked on, the next one is on its
+// way, and so are the keys of the next head from the first tile of this one on.
+constexpr uint32_t MANY_THREADS = 512, MANY_KEYS = 32 * MANY_THREADS / 64;
+constexpr uint32_t MANY_BLOCKS = 2048;  // heads are shared out up to so many workgroups
+template <class Q, class C, int DP>
+__global__ void __launch_bounds__(MANY_THREADS, DP <= 128 ? 4 : 2) dl_weigh_many_kernel(const weigh_args a)
+{
+    constexpr uint32_t PAIRS = DP / 32, PIECES = DP / 8, LOADS = (32 * PIECES + MANY_THREADS - 1) / MANY_THREADS;
+    __shared__ __align__(16) uint32_t tiles[2][32 * PIECES * 4];
+    __shared__ float lses[2][32];
+    __shared__ __align__(16) float scales[MANY_THREADS / 64][32];
     const uint32_t lane = threadIdx.x % 64u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
     const uint32_t i = lane % 32u, half = lane / 32u, D = a.c.head_dim, b = blockIdx.y;
-    const uint32_t share = wave % a.sharing, block_keys = 32u * (WEIGH_WAVES / a.sharing);
     const uint32_t first = a.p.start(b), queries = a.p.queries(b, first), rows = queries * a.group, len = a.p.len(b);
-    const int32_t *const table = a.p.pages + b * a.p.pages_stride;
-    for (uint32_t block0 = blockIdx.x * block_keys; block0 < a.width; block0 += gridDim.x * block_keys) {
-        const uint32_t base = block0 + wave / a.sharing * 32u, key = base + i;
-        float sum = 0.0f;
-        if (base < len && rows) {
-            // the first row that sees the lane's key: that of query key - (len - queries)
-            const int64_t since = ((int64_t)key - (int64_t)len + (int64_t)queries) * a.group;
-            uint32_t page = ~0u, in = 0;
-            if (key < len) {
-                const uint32_t n = dl_divide(key, a.c.page);
-                page = (uint32_t)table[n];
-                in = key - n * a.c.page.d;
-            }
-            const bool alive = page < a.c.pages;
-            const uint32_t from_row = alive ? (uint32_t)max(since, (int64_t)0) : ~0u;
-            page = alive ? page : 0u;
-            const char *const codes = a.c.k + (uint64_t)page * a.c.page_stride + (uint64_t)in * a.c.token_stride;
-            const char *const scales = (const char *)a.c.k_scale + (uint64_t)page * a.c.scale_page_stride + (uint64_t)in * a.c.scale_token_stride;
-            const int64_t wave_since = ((int64_t)base - (int64_t)len + (int64_t)queries) * a.group;
-            const uint32_t row0 = (uint32_t)max(wave_since, (int64_t)0) & ~31u;
-            for (uint32_t head = share; head < a.c.heads; head += a.sharing) {
-                dl_words<16> k[PAIRS];
+    const int32_t ahead = (int32_t)len - (int32_t)queries;
+    const uint32_t at = blockIdx.z * gridDim.x + blockIdx.x, part = at % a.parts, block0 = at / a.parts * MANY_KEYS, base = block0 + wave * 32u;
+    if (block0 >= a.width) return;
+    const uint32_t head0 = part * a.c.heads / a.parts, heads_end = (part + 1u) * a.c.heads / a.parts;
+    float sum[16];
 #pragma unroll
-                for (uint32_t x = 0; x < PAIRS; ++x) k[x] = dl_load_words<16>(codes + head * a.c.head_stride + min(16u * (2u * x + half), D - 16u));
-                float scale = *(const float *)(scales + head * a.c.scale_head_stride);
-                scale = alive ? scale * a.scale : 0.0f;
-                for (uint32_t r0 = row0; r0 < rows; r0 += 32u) {
-                    const uint32_t row = min(r0 + i, rows - 1u), j = row / a.group, h = head * a.group + row - j * a.group;
-                    const char *const q = a.q + (uint64_t)(first + j) * a.q_token + h * a.q_head;
-                    const float given = a.lse[(uint64_t)(first + j) * a.q_heads + h] * DL_LOG2E;
-                    // (a row that is none, or whose lse is no number: nothing is left of it)
-                    const float lse = r0 + i < rows && fabsf(given) < INFINITY ? given : INFINITY;
+    for (int e = 0; e < 16; ++e) sum[e] = 0.0f;
+    uint32_t dead = ~0u;
+    if (block0 < len && rows) {
+        const weigh_key key(a, b, base + i, len);
+        dead = (uint32_t)__ballot(!key.alive);
+        const int64_t of_block = ((int64_t)block0 - ahead) * a.group;
+        const uint32_t row0 = (uint32_t)max(of_block, (int64_t)0) & ~31u;
+        const int64_t since = ((int64_t)base - ahead) * a.group, until = ((int64_t)base + 31 - ahead) * a.group;
+        const uint32_t from = base < len ? (uint32_t)max(since, (int64_t)0) : ~0u, whole = (uint32_t)max(until, (int64_t)0);
+        dl_u32x4 staged[LOADS];
+        float staged_lse = INFINITY;
+        auto stage = [&](uint32_t head, uint32_t r0) {
+#pragma unroll
+            for (uint32_t x = 0; x < LOADS; ++x) {
+                const uint32_t n = threadIdx.x + x * MANY_THREADS, row = min(r0 + n / PIECES, rows - 1u), j = dl_divide(row, a.groups);
+                const char *const q = a.q + (uint64_t)(first + j) * a.q_token + (head * a.group + row - j * a.group) * a.q_head;
+                staged[x] = dl_load_at<dl_u32x4>(q + 2u * min(n % PIECES * 8u, D - 8u));
+            }
+            if (threadIdx.x < 32u) {
+                const uint32_t row = min(r0 + i, rows - 1u), j = dl_divide(row, a.groups);
+                const float given = a.lse[(uint64_t)(first + j) * a.q_heads + head * a.group + row - j * a.group];
+                staged_lse = r0 + i < rows && fabsf(given) < INFINITY ? given * DL_LOG2E : INFINITY;
+            }
+        };
+        auto put = [&](uint32_t to) {
+#pragma unroll
+            for (uint32_t x = 0; x < LOADS; ++x) {
+                const uint32_t n = threadIdx.x + x * MANY_THREADS, row = n / PIECES, piece = n % PIECES;
+                if (32u * PIECES % MANY_THREADS == 0 || n < 32u * PIECES) *(dl_u32x4 *)&tiles[to][(row * PIECES + (piece ^ (row & 7u))) * 4u] = staged[x];
+            }
+            if (threadIdx.x < 32u) lses[to][i] = staged_lse;
+        };
+        dl_words<16> codes[PAIRS];
+        float scale = 0.0f;
+        auto load_keys = [&](uint32_t head) {
+#pragma unroll
+            for (uint32_t x = 0; x < PAIRS; ++x) codes[x] = dl_load_words<16>(key.codes + head * a.c.head_stride + min(16u * (2u * x + half), D - 16u));
+            scale = *(const float *)(key.scale + head * a.c.scale_head_stride);
+        };
+        dl_u32x4 kf[2 * PAIRS];
+        load_keys(head0);
+        stage(head0, row0);
+        put(0);
+        __syncthreads();
+        uint32_t now = 0;
+#pragma unroll 1
+        for (uint32_t head = head0; head < heads_end; ++head) {
+#pragma unroll
+            for (uint32_t x = 0; x < 2 * PAIRS; ++x) {
+                const dl_u32x2 lo = C::template spread<Q>(codes[x / 2].w[2 * (x % 2)]), hi = C::template spread<Q>(codes[x / 2].w[2 * (x % 2) + 1]);
+                kf[x] = dl_u32x4{lo[0], lo[1], hi[0], hi[1]};
+                if (16u * (2u * (x / 2) + half) >= D) kf[x] = dl_u32x4{0, 0, 0, 0};
+            }
+            if (half == 0) scales[wave][i] = key.alive ? scale * a.scale : 0.0f;
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            if (head + 1u < heads_end) load_keys(head + 1u);
+#pragma unroll 1
+            for (uint32_t r0 = row0; r0 < rows; r0 += 32u, now ^= 1u) {
+                const bool same_head = r0 + 32u < rows, more = same_head || head + 1u < heads_end;
+                if (more) stage(same_head ? head : head + 1u, same_head ? r0 + 32u : row0);
+                if (r0 + 32u > from) {
                     dl_f32x16 s;
 #pragma unroll
                     for (int e = 0; e < 16; ++e) s[e] = 0.0f;
 #pragma unroll
-                    for (uint32_t x = 0; x < PAIRS; ++x)
-#pragma unroll
-                        for (uint32_t u = 0; u < 2; ++u) {
-                            const uint32_t d = 16u * (2u * x + half) + 8u * u;
-                            const dl_u32x4 qf = d < D ? dl_load_at<dl_u32x4>(q + 2u * d) : dl_u32x4{0, 0, 0, 0};
-                            const dl_u32x2 lo = C::template spread<Q>(k[x].w[2 * u]), hi = C::template spread<Q>(k[x].w[2 * u + 1]);
-                            s = Q::mfma32(qf, dl_u32x4{lo[0], lo[1], hi[0], hi[1]}, s);
-                        }
-                    // rows of the product are queries (8 (e / 4) + 4 half + e % 4), its columns keys (i)
-                    float four[4] = {0, 0, 0, 0};
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const uint32_t in_tile = 8u * (e / 4) + 4u * half + e % 4;
-                        const float its = __shfl(lse, (int)in_tile);
-                        const float w = __builtin_amdgcn_exp2f(fmaf(s[e], scale, -its));
-                        four[e % 4] += r0 + in_tile >= from_row ? w : 0.0f;
+                    for (uint32_t x = 0; x < 2 * PAIRS; ++x) {
+                        const uint32_t piece = 2u * (2u * (x / 2) + half) + x % 2u;
+                        s = Q::mfma32(kf[x], *(const dl_u32x4 *)&tiles[now][(i * PIECES + (piece ^ (i & 7u))) * 4u], s);
                     }
-                    sum += (four[0] + four[1]) + (four[2] + four[3]);
+                    const int32_t seen = ahead + (int32_t)(dl_divide(r0 + i, a.groups)) - (int32_t)base;
+                    add_weights(s, scales[wave], lses[now][i], r0 < whole, seen, half, sum);
                 }
+                if (more) put(now ^ 1u);
+                __syncthreads();
             }
-            sum += __shfl_xor(sum, 32);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
         }
-        if (half == 0) sums[wave][i] = sum;
-        __syncthreads();
-        if (share == 0 && half == 0 && key < a.width) {
-            float all = sum;
-            for (uint32_t w = 1; w < a.sharing; ++w) all += sums[wave + w][i];
-            a.weights[b * a.weights_stride + key] = (a.before ? a.before[b * a.before_stride + key] : 0.0f) + all;
-        }
-        __syncthreads();
     }
+    const float its = over_lanes(sum, i);
+    const uint32_t in = 8u * (i / 4u) + 4u * half + i % 4u, key = base + in;
+    if (i >= 16u || key >= a.width) return;
+    const float all = dead >> in & 1u ? 0.0f : its;
+    if (a.parts > 1u)
+        a.partial[((uint64_t)part * a.p.batch + b) * a.width + key] = all;
+    else
+        a.weights[b * a.weights_stride + key] = (a.before ? a.before[b * a.before_stride + key] : 0.0f) + all;
 }
 
-int weigh_sizes(const dl_kv_cache *cache, const dl_kv_weigh_args *args, dl_cache_view *view)
+// Adds the parts, in their order.
+constexpr uint32_t ADD_THREADS = 256;
+__global__ void __launch_bounds__(ADD_THREADS) dl_weigh_add_kernel(const weigh_args a)
+{
+    const uint32_t key = blockIdx.x * ADD_THREADS + threadIdx.x, b = blockIdx.y;
+    if (key >= a.width) return;
+    float all = 0.0f;
+    if (key < a.p.len(b))
+        for (uint32_t part = 0; part < a.parts; ++part) all += a.partial[((uint64_t)part * a.p.batch + b) * a.width + key];
+    a.weights[b * a.weights_stride + key] = (a.before ? a.before[b * a.before_stride + key] : 0.0f) + all;
+}
+
+struct weigh_shape {
+    bool many;
+    uint32_t blocks, parts;
+};
+
+int weigh_sizes(const dl_kv_cache *cache, const dl_kv_weigh_args *args, dl_cache_view *view, weigh_shape *sh)
 {
     const int rc = dl_packed_sizes(cache, args, view);
     if (rc != DL_OK) return rc;
-    return args->max_pages * cache->page_tokens * args->batch > INT32_MAX ? DL_ERR_INVALID : DL_OK;
+    const int64_t width = args->max_pages * cache->page_tokens;
+    if (width * args->batch > INT32_MAX) return DL_ERR_INVALID;
+    *sh = weigh_shape{};
+    if (!args->batch || !width) return DL_OK;
+    // By the rows that a head of a sequence has on average.
+    sh->many = (uint64_t)args->tokens * (uint32_t)(args->q_heads / cache->heads) > 32u * (uint64_t)args->batch;
+    sh->parts = 1;
+    if (sh->many) {
+        sh->blocks = (uint32_t)((width + MANY_KEYS - 1) / MANY_KEYS);
+        const uint64_t all = (uint64_t)sh->blocks * (uint32_t)args->batch;
+        sh->parts = all >= MANY_BLOCKS ? 1u : (uint32_t)((MANY_BLOCKS + all - 1u) / all);
+        if (sh->parts > (uint32_t)cache->heads) sh->parts = (uint32_t)cache->heads;
+        sh->blocks *= sh->parts;
+    }
+    return DL_OK;
+}
+
+size_t weigh_bytes(const dl_kv_cache *cache, const dl_kv_weigh_args *args, const weigh_shape &sh)
+{
+    return DL_CONTROL_BYTES + (sh.parts > 1u ? (size_t)sh.parts * (uint32_t)args->batch * (uint64_t)(args->max_pages * cache->page_tokens) * sizeof(float) : 0u);
 }
 
 }  // namespace
@@ -116,8 +330,9 @@ int weigh_sizes(const dl_kv_cache *cache, const dl_kv_weigh_args *args, dl_cache
 extern "C" int64_t dl_kv_weigh_workspace(const dl_kv_cache *cache, const dl_kv_weigh_args *args)
 {
     dl_cache_view view;
-    const int rc = weigh_sizes(cache, args, &view);
-    return rc != DL_OK ? rc : (int64_t)DL_CONTROL_BYTES;
+    weigh_shape sh;
+    const int rc = weigh_sizes(cache, args, &view, &sh);
+    return rc != DL_OK ? rc : (int64_t)weigh_bytes(cache, args, sh);
 }
 
 extern "C" int dl_kv_weigh(const dl_kv_cache *cache, const dl_kv_weigh_args *args, void *stream)
@@ -126,12 +341,13 @@ extern "C" int dl_kv_weigh(const dl_kv_cache *cache, const dl_kv_weigh_args *arg
     if (!g_dl.inited) return DL_ERR_STATE;
     if (dl_device_error_pending()) return DL_ERR_LOST;
     weigh_args a;
-    int rc = weigh_sizes(cache, args, &a.c);
+    weigh_shape sh;
+    int rc = weigh_sizes(cache, args, &a.c, &sh);
     if (rc != DL_OK) return rc;
     if (!args->batch || !args->max_pages) return DL_OK;
     rc = dl_cache_check(cache, 1, &a.c);
     if (rc != DL_OK) return rc;
-    rc = dl_packed_setup(cache, args, DL_CONTROL_BYTES, &a.p);
+    rc = dl_packed_setup(cache, args, weigh_bytes(cache, args, sh), &a.p);
     if (rc != DL_OK) return rc;
     if (!args->weights || (args->tokens && args->q_heads && (!args->q || !args->lse)) || ((uint64_t)args->weights | (uint64_t)args->before) % 4u)
         return DL_ERR_INVALID;
@@ -146,14 +362,27 @@ extern "C" int dl_kv_weigh(const dl_kv_cache *cache, const dl_kv_weigh_args *arg
     a.width = (uint32_t)(args->max_pages * cache->page_tokens);
     a.q_heads = (uint32_t)args->q_heads;
     a.group = a.q_heads / a.c.heads;
-    a.sharing = a.c.heads >= 8u ? 8u : a.c.heads >= 4u ? 4u : a.c.heads >= 2u ? 2u : 1u;
+    a.groups = dl_make_divider(a.group ? a.group : 1u);
     a.scale = args->scale * DL_LOG2E;
-    const uint32_t block_keys = 32u * (WEIGH_WAVES / a.sharing), blocks = (a.width + block_keys - 1u) / block_keys;
-    const dim3 grid(blocks < 65536u ? blocks : 65536u, a.p.batch);
+    a.parts = sh.parts;
+    a.partial = (float *)((char *)args->workspace + DL_CONTROL_BYTES);
+    a.sharing = 1;
+    while (a.sharing < FEW_WAVES && 2u * a.sharing <= a.c.heads) a.sharing *= 2u;
+    const uint32_t few_keys = 32u * (FEW_WAVES / a.sharing), blocks = sh.many ? sh.blocks : (a.width + few_keys - 1u) / few_keys;
+    // (blocks may be more than a grid of so many threads is wide)
+    const uint32_t high = (blocks + 65535u) / 65536u;
+    const dim3 grid((blocks + high - 1u) / high, a.p.batch, high);
     dl_with_16bit(args->type, [&](auto q) {
         dl_with_format(cache->format, [&](auto c) {
             auto go = [&](auto dp) {
-                hipLaunchKernelGGL((dl_weigh_kernel<decltype(q), decltype(c), decltype(dp)::value>), grid, dim3(WEIGH_THREADS), 0, (hipStream_t)stream, a);
+                constexpr int DP = decltype(dp)::value;
+                if (sh.many)
+                    hipLaunchKernelGGL((dl_weigh_many_kernel<decltype(q), decltype(c), DP>), grid, dim3(MANY_THREADS), 0, (hipStream_t)stream, a);
+                else
+                    dl_with_bool(a.c.head_dim == DP, [&](auto whole) {
+                        hipLaunchKernelGGL((dl_weigh_few_kernel<decltype(q), decltype(c), DP, decltype(whole)::value>), grid, dim3(64 * FEW_WAVES), 0,
+                                           (hipStream_t)stream, a);
+                    });
             };
             if (a.c.head_dim <= 64)
                 go(std::integral_constant<int, 64>{});
@@ -163,6 +392,8 @@ extern "C" int dl_kv_weigh(const dl_kv_cache *cache, const dl_kv_weigh_args *arg
                 go(std::integral_constant<int, 256>{});
         });
     });
+    if (a.parts > 1u)
+        hipLaunchKernelGGL(dl_weigh_add_kernel, dim3((a.width + ADD_THREADS - 1u) / ADD_THREADS, a.p.batch), dim3(ADD_THREADS), 0, (hipStream_t)stream, a);
     DL_HIP(hipGetLastError());
     t_dl_last.mode = DL_MODE_ONESHOT;
     return DL_OK;
