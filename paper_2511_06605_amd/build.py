@@ -20,6 +20,8 @@ HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-fno-gpu-rdc",
     "-parallel-jobs=8",  # sources side by side
     "-Wall", "-Wextra", "-Wno-unused-parameter",
+    # matrix products may leave their results in ordinary registers also where a wavefront has more than 256
+    "-mllvm", "-amdgpu-mfma-vgpr-form",
     # packed-fp32 instructions stay off for every device function in this library
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
 ]

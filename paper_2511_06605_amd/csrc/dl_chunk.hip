@@ -15,7 +15,6 @@
 namespace {
 
 constexpr uint32_t CH_THREADS = 256, CH_WAVES = CH_THREADS / 64;
-constexpr uint32_t CH_ROWS = 32 * CH_WAVES;
 constexpr uint32_t CH_KEYS = 64;
 
 struct chunk_args {
@@ -30,8 +29,9 @@ struct chunk_args {
     int64_t q_token, q_head, out_token, out_head;  // bytes
     uint32_t q_heads, group;
     dl_divider groups;  // by group
-    uint32_t target;  // see chunk_plan; 0: a piece a tile
-    float scale;      // times log2 e
+    uint32_t tile_rows;  // 32 or 64 a wavefront
+    uint32_t target;     // see chunk_unit; 0: a piece a tile
+    float scale;         // times log2 e
 };
 
 // The key axis of a sequence is cut into pieces where there are few tiles, by the lengths, which only the device knows: into pieces of as
@@ -48,7 +48,7 @@ struct chunk_place {
 __device__ __forceinline__ uint32_t tiles_of(const chunk_args &a, uint32_t b)
 {
     const uint32_t first = a.p.start(b);
-    return (a.p.queries(b, first) * a.group + CH_ROWS - 1u) / CH_ROWS;
+    return (a.p.queries(b, first) * a.group + a.tile_rows - 1u) / a.tile_rows;
 }
 __device__ __forceinline__ uint32_t steps_of(const chunk_args &a, uint32_t b) { return (a.p.len(b) + CH_KEYS - 1u) / CH_KEYS; }
 
@@ -114,9 +114,9 @@ struct chunk_rows {
         first = a.p.start(at.b);
         const uint32_t n = a.p.queries(at.b, first), len = a.p.len(at.b);
         rows = n * a.group;
-        row0 = at.tile * CH_ROWS;
+        row0 = at.tile * a.tile_rows;
         ahead = (int32_t)len - (int32_t)n;
-        end = seen_by(a, min(row0 + CH_ROWS, rows) - 1u);
+        end = seen_by(a, min(row0 + a.tile_rows, rows) - 1u);
     }
     __device__ __forceinline__ uint32_t seen_by(const chunk_args &a, uint32_t row) const { return (uint32_t)max(ahead + (int32_t)(dl_divide(row, a.groups)) + 1, 0); }
 };
@@ -135,19 +135,203 @@ struct chunk_lds {
     uint64_t alive_at[2];          // bit k: key k is one of the piece, in a page of the pool
 };
 
-// Operands lie in rows of 16-byte pieces, whose places are exchanged (by an exclusive or with the row's number) so that eight
-// neighbouring lanes use all banks, in reads and in writes.
+// Codes on their way into a tile.  Operands lie in rows of 16-byte pieces, whose places are exchanged (by an exclusive or with the row's
+// number) so that eight neighbouring lanes use all banks, in reads and in writes.
+template <class Q, class C, int DP>
+struct chunk_feed {
+    static constexpr uint32_t PIECES = DP / 8;                          // 16-byte pieces of a key's row
+    static constexpr uint32_t K_LOADS = CH_KEYS * PIECES / CH_THREADS;  // of 8 codes
+    static constexpr uint32_t V_ITEMS = 8 * (DP / 4);                   // 8 keys (half of 16) x 4 dims
+    static constexpr uint32_t V_LOADS = (V_ITEMS + CH_THREADS - 1) / CH_THREADS;
+    const int32_t *table;
+    const char *k_from, *v_from, *scales;
+    uint32_t end, lane, wave, looked_up = 0;
+    float scale = 0.0f;
+    bool alive = false;
+    dl_words<8> kw[K_LOADS];
+    uint32_t vw[V_LOADS][8];
+
+    __device__ __forceinline__ chunk_feed(const chunk_args &a, uint32_t b, uint32_t head, uint32_t last, uint32_t in_wave, uint32_t of_wave)
+    {
+        table = a.p.pages + b * a.p.pages_stride;
+        k_from = a.c.k + (int64_t)head * a.c.head_stride;
+        v_from = a.c.v + (int64_t)head * a.c.head_stride;
+        scales = (const char *)(of_wave == 0 ? a.c.k_scale : a.c.v_scale) + (int64_t)head * a.c.scale_head_stride;
+        end = last;
+        lane = in_wave;
+        wave = of_wave;
+    }
+    // A key's page: looked up by the first two wavefronts, for the keys' and the values' scales; the first hands the rows on.
+    __device__ __forceinline__ void look_up(const chunk_args &a, uint32_t base)
+    {
+        if (wave < 2) looked_up = (uint32_t)table[dl_divide(min(base + lane, end - 1u), a.c.page)];
+    }
+    __device__ __forceinline__ void hand_on(const chunk_args &a, uint32_t base, uint64_t (&rows_at)[CH_KEYS], uint64_t &alive_at)  // what was looked up for the step at base
+    {
+        if (wave < 2) {
+            const uint32_t key = min(base + lane, end - 1u), in = key - dl_divide(key, a.c.page) * a.c.page.d;
+            alive = base + lane < end && looked_up < a.c.pages;
+            const uint64_t page = looked_up < a.c.pages ? looked_up : 0u;
+            if (wave == 0) {
+                rows_at[lane] = page * a.c.page_stride + (uint64_t)in * a.c.token_stride;
+                const unsigned long long all = __ballot(alive);
+                if (lane == 0) alive_at = all;
+            }
+            scale = *(const float *)(scales + page * a.c.scale_page_stride + (uint64_t)in * a.c.scale_token_stride);
+        }
+    }
+    // One part of LOAD_PARTS of a step's loads: where its row begins, and the load from there.
+    static constexpr uint32_t LOAD_PARTS = K_LOADS + 8 * V_LOADS;
+    static __device__ __forceinline__ uint64_t load_from(const uint64_t (&rows_at)[CH_KEYS], uint32_t part_of)
+    {
+        if (part_of < K_LOADS) return rows_at[(threadIdx.x + part_of * CH_THREADS) / PIECES];
+        const uint32_t x = (part_of - K_LOADS) / 8u, e = (part_of - K_LOADS) % 8u, part = (threadIdx.x + x * CH_THREADS) / (DP / 4) % 8u;
+        return rows_at[part / 2u * 16u + part % 2u * 4u + (e & 3u) + (e >> 2) * 8u];
+    }
+    __device__ __forceinline__ void load_part(const chunk_args &a, uint64_t from, uint32_t part_of)
+    {
+        const uint32_t D = a.c.head_dim;
+        if (part_of < K_LOADS) {
+            kw[part_of] = dl_load_words<8>(k_from + from + min((threadIdx.x + part_of * CH_THREADS) % PIECES * 8u, D - 8u));
+        } else {
+            const uint32_t x = (part_of - K_LOADS) / 8u, e = (part_of - K_LOADS) % 8u;
+            vw[x][e] = dl_load_at<uint32_t>(v_from + from + min((threadIdx.x + x * CH_THREADS) % (DP / 4) * 4u, D - 4u));
+        }
+    }
+    __device__ __forceinline__ void load(const chunk_args &a, const uint64_t (&rows_at)[CH_KEYS])
+    {
+#pragma unroll
+        for (uint32_t n = 0; n < LOAD_PARTS; ++n) load_part(a, load_from(rows_at, n), n);
+    }
+    // What is none counts as zero.
+    __device__ __forceinline__ void clear(uint64_t alive_at)
+    {
+        const uint32_t all_lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)alive_at);
+        const uint32_t all_hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(alive_at >> 32));
+        const uint64_t all = (uint64_t)all_hi << 32 | all_lo;
+        if (all == ~0ull) return;
+#pragma unroll
+        for (uint32_t x = 0; x < K_LOADS; ++x)
+            if (!(all >> ((threadIdx.x + x * CH_THREADS) / PIECES) & 1u)) kw[x] = dl_words<8>{};
+#pragma unroll
+        for (uint32_t x = 0; x < V_LOADS; ++x) {
+            const uint32_t part = (threadIdx.x + x * CH_THREADS) / (DP / 4) % 8u, key = part / 2u * 16u + part % 2u * 4u;
+#pragma unroll
+            for (uint32_t e = 0; e < 8; ++e)
+                if (!(all >> (key + (e & 3u) + (e >> 2) * 8u) & 1u)) vw[x][e] = 0;
+        }
+    }
+    // One part of PUT_PARTS of what goes to the tile: the keys' loads, then four dims at a time of the values'.
+    static constexpr uint32_t PUT_PARTS = K_LOADS + 4 * V_LOADS;
+    __device__ __forceinline__ void put_part(chunk_tile<DP> &to, uint32_t part_of)
+    {
+        if (part_of < K_LOADS) {
+            const uint32_t x = part_of, n = threadIdx.x + x * CH_THREADS, key = n / PIECES, c = n % PIECES;
+            const dl_u32x2 p = C::template spread<Q>(kw[x].w[0]), r = C::template spread<Q>(kw[x].w[1]);
+            *(dl_u32x4 *)&to.k[(key * PIECES + (c ^ (key & 7u))) * 4u] = dl_u32x4{p[0], p[1], r[0], r[1]};
+            return;
+        }
+        const uint32_t x = (part_of - K_LOADS) / 4u, f = (part_of - K_LOADS) % 4u;
+        const uint32_t n = threadIdx.x + x * CH_THREADS, d = n % (DP / 4) * 4u, part = n / (DP / 4) % 8u;
+        if (V_ITEMS % CH_THREADS && n >= V_ITEMS) return;
+        dl_u32x2 two[2];
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const uint32_t pick = f < 2 ? 0x05010400u : 0x07030602u;
+            const uint32_t a01 = __builtin_amdgcn_perm(vw[x][4 * g + 1], vw[x][4 * g], pick), a23 = __builtin_amdgcn_perm(vw[x][4 * g + 3], vw[x][4 * g + 2], pick);
+            two[g] = C::template spread<Q>(__builtin_amdgcn_perm(a23, a01, f % 2 ? 0x07060302u : 0x05040100u));
+        }
+        const uint32_t r = d + f, c = part ^ ((r & 7u) ^ (r >> 3 & 3u));
+        *(dl_u32x4 *)&to.v[(r * 8u + c) * 4u] = dl_u32x4{two[0][0], two[0][1], two[1][0], two[1][1]};
+    }
+    __device__ __forceinline__ void put_codes(chunk_tile<DP> &to)
+    {
+#pragma unroll
+        for (uint32_t n = 0; n < PUT_PARTS; ++n) put_part(to, n);
+    }
+    __device__ __forceinline__ void put_scales(const chunk_args &a, chunk_tile<DP> &to)
+    {
+        if (wave == 0) {
+            to.ks[lane] = alive ? scale * a.scale : 0.0f;
+        } else if (wave == 1) {
+            const dl_value_scale<Q> u(scale);
+            to.lu[lane] = alive ? u.log2_c() : -INFINITY;
+            to.iu[lane] = alive ? u.over_c() : 0.0f;
+            to.d[lane] = u.d;
+            const bool some = __any(u.d != 1.0f);
+            if (lane == 0) to.taken_apart = some;
+        }
+    }
+    // Values times what their scales left out, in LDS, by all threads, before anybody works on the step.
+    static __device__ __forceinline__ void apart(chunk_tile<DP> &to)
+    {
+#pragma unroll 1
+        for (uint32_t n = threadIdx.x; n < DP * 8u; n += CH_THREADS) {
+            const uint32_t r = n / 8u, part = n % 8u, key = part / 2u * 16u + part % 2u * 4u;
+            uint32_t *const v = &to.v[(r * 8u + (part ^ ((r & 7u) ^ (r >> 3 & 3u)))) * 4u];
+#pragma unroll
+            for (uint32_t x = 0; x < 4; ++x) {
+                const float *const d = &to.d[key + x / 2u * 8u + x % 2u * 2u];
+                v[x] = Q::pack(Q::in_range(Q::lo(v[x]) * d[0]), Q::in_range(Q::hi(v[x]) * d[1]));
+            }
+        }
+        __syncthreads();
+    }
+    // The operands of a product: keys 32 kb + i against dims 16 st + 8 half .., and dims 32 dt + i against the x-th 16 of keys 32 kb ..
+    static __device__ __forceinline__ dl_u32x4 keys(const chunk_tile<DP> &in, uint32_t kb, uint32_t st, uint32_t i, uint32_t half)
+    {
+        const uint32_t key = 32u * kb + i;
+        return *(const dl_u32x4 *)&in.k[(key * PIECES + ((2u * st + half) ^ (key & 7u))) * 4u];
+    }
+    static __device__ __forceinline__ dl_u32x4 values(const chunk_tile<DP> &in, uint32_t kb, uint32_t x, uint32_t dt, uint32_t i, uint32_t half)
+    {
+        const uint32_t d = 32u * dt + i, c = (4u * kb + 2u * x + half) ^ ((d & 7u) ^ (d >> 3 & 3u));
+        return *(const dl_u32x4 *)&in.v[(d * 8u + c) * 4u];
+    }
+};
+
+// A row's sums, as lane (i, half) of a wavefront has them: dims 32 x + 8 (e / 4) + 4 half + e % 4.  They are what a piece leaves behind, or done.
+template <class Q, int DP>
+__device__ __forceinline__ void finish_row(const chunk_args &a, const chunk_place &at, const chunk_rows &t, uint32_t head, uint32_t my, uint32_t half, float r, float l,
+                                           const dl_f32x16 (&o)[DP / 32])
+{
+    l += __shfl_xor(l, 32);
+    if (my >= t.rows) return;
+    const uint32_t D = a.c.head_dim;
+    if (at.pieces > 1u) {
+        const uint64_t to = ((uint64_t)at.slot * a.c.heads + head) * a.tile_rows + (my - t.row0);
+        if (half == 0) a.rl[to] = dl_f32x2{r, l};
+#pragma unroll
+        for (int x = 0; x < DP / 32; ++x)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                const uint32_t d = 32u * x + 2u * e + 4u * half;
+                if (d < D) *(dl_f32x4 *)(a.partial + to * D + d) = dl_f32x4{o[x][e], o[x][e + 1], o[x][e + 2], o[x][e + 3]};
+            }
+        return;
+    }
+    const uint32_t j = dl_divide(my, a.groups), h = head * a.group + my - j * a.group;
+    const bool none = l == 0.0f;
+    const float f = none ? 0.0f : 1.0f / l;
+    char *const to = a.out + (uint64_t)(t.first + j) * a.out_token + h * a.out_head;
+#pragma unroll
+    for (int x = 0; x < DP / 32; ++x)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+            const uint32_t d = 32u * x + 2u * e + 4u * half;
+            if (d < D)
+                dl_store_at(to + 2u * d, none ? dl_u32x2{0, 0} : dl_u32x2{Q::pack(o[x][e] * f, o[x][e + 1] * f), Q::pack(o[x][e + 2] * f, o[x][e + 3] * f)});
+        }
+    if (a.lse && half == 0)
+        a.lse[(uint64_t)(t.first + j) * a.q_heads + h] = none ? -INFINITY : ((r == -INFINITY ? 0.0f : r) - Q::lift + log2f(l)) * DL_LN2;
+}
+
 template <class Q, class C, int DP>
 __global__ void __launch_bounds__(CH_THREADS, DP <= 128 ? 2 : 1) dl_chunk_kernel(const chunk_args a)
 {
-    constexpr uint32_t PIECES = DP / 8;                          // 16-byte pieces of a key's row
-    constexpr uint32_t K_LOADS = CH_KEYS * PIECES / CH_THREADS;  // of 8 codes
-    constexpr uint32_t V_ITEMS = 8 * (DP / 4);                   // 8 keys (half of 16) x 4 dims
-    constexpr uint32_t V_LOADS = (V_ITEMS + CH_THREADS - 1) / CH_THREADS;
+    using feed_t = chunk_feed<Q, C, DP>;
     __shared__ chunk_lds<DP> lds;
     auto &tiles = lds.tiles;
-    auto &rows_at = lds.rows_at;
-    auto &alive_at = lds.alive_at;
     const uint32_t lane = threadIdx.x % 64u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
     const uint32_t i = lane % 32u, half = lane / 32u, D = a.c.head_dim, head = blockIdx.x % a.c.heads;
     chunk_place at;
@@ -155,8 +339,7 @@ __global__ void __launch_bounds__(CH_THREADS, DP <= 128 ? 2 : 1) dl_chunk_kernel
     const chunk_rows t(a, at);
     const uint32_t first = at.piece * at.keys, end = min(first + at.keys, t.end);
     if (at.piece && first >= end) return;
-    const int32_t *const table = a.p.pages + at.b * a.p.pages_stride;
-    const char *const k_from = a.c.k + (int64_t)head * a.c.head_stride, *const v_from = a.c.v + (int64_t)head * a.c.head_stride;
+    feed_t feed(a, at.b, head, end, lane, wave);
 
     const uint32_t wave_row = t.row0 + wave * 32u, my = wave_row + i, row = min(my, t.rows - 1u);
     const uint32_t j = dl_divide(row, a.groups), h = head * a.group + row - j * a.group;
@@ -169,112 +352,11 @@ __global__ void __launch_bounds__(CH_THREADS, DP <= 128 ? 2 : 1) dl_chunk_kernel
 #pragma unroll
     for (int s = 0; s < DP / 16; ++s) qf[s] = 16u * s < D ? dl_load_at<dl_u32x4>(q + 2u * (16u * s + 8u * half)) : dl_u32x4{0, 0, 0, 0};
 
-    // a key's page: looked up by the first two wavefronts, for the keys' and the values' scales; the first hands the rows on
-    uint32_t looked_up = 0;
-    auto look_up = [&](uint32_t base) {
-        if (wave < 2) looked_up = (uint32_t)table[dl_divide(min(base + lane, end - 1u), a.c.page)];
-    };
-    float scale = 0.0f;
-    bool alive = false;
-    auto hand_on = [&](uint32_t base, uint32_t to) {  // what was looked up for the step at base
-        if (wave < 2) {
-            const uint32_t key = min(base + lane, end - 1u), in = key - dl_divide(key, a.c.page) * a.c.page.d;
-            alive = base + lane < end && looked_up < a.c.pages;
-            const uint64_t page = looked_up < a.c.pages ? looked_up : 0u;
-            if (wave == 0) {
-                rows_at[to][lane] = page * a.c.page_stride + (uint64_t)in * a.c.token_stride;
-                const unsigned long long all = __ballot(alive);
-                if (lane == 0) alive_at[to] = all;
-            }
-            scale = *(const float *)((const char *)(wave == 0 ? a.c.k_scale : a.c.v_scale) + (int64_t)head * a.c.scale_head_stride +
-                                     page * a.c.scale_page_stride + (uint64_t)in * a.c.scale_token_stride);
-        }
-    };
-    dl_words<8> kw[K_LOADS];
-    uint32_t vw[V_LOADS][8];
-    auto load = [&](uint32_t from) {
-#pragma unroll
-        for (uint32_t x = 0; x < K_LOADS; ++x) {
-            const uint32_t n = threadIdx.x + x * CH_THREADS, key = n / PIECES, d = n % PIECES * 8u;
-            kw[x] = dl_load_words<8>(k_from + rows_at[from][key] + min(d, D - 8u));
-        }
-#pragma unroll
-        for (uint32_t x = 0; x < V_LOADS; ++x) {
-            const uint32_t n = threadIdx.x + x * CH_THREADS, d = n % (DP / 4) * 4u, part = n / (DP / 4) % 8u;
-            const uint32_t key = part / 2u * 16u + part % 2u * 4u;
-#pragma unroll
-            for (uint32_t e = 0; e < 8; ++e)
-                vw[x][e] = dl_load_at<uint32_t>(v_from + rows_at[from][key + (e & 3u) + (e >> 2) * 8u] + min(d, D - 4u));
-        }
-    };
-    auto put = [&](uint32_t from) {  // what has been loaded, into the tile
-        chunk_tile<DP> &to = tiles[from];
-        const uint32_t all_lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)alive_at[from]);
-        const uint32_t all_hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(alive_at[from] >> 32));
-        const uint64_t all = (uint64_t)all_hi << 32 | all_lo;
-        if (all != ~0ull) {  // what is none counts as zero
-#pragma unroll
-            for (uint32_t x = 0; x < K_LOADS; ++x)
-                if (!(all >> ((threadIdx.x + x * CH_THREADS) / PIECES) & 1u)) kw[x] = dl_words<8>{};
-#pragma unroll
-            for (uint32_t x = 0; x < V_LOADS; ++x) {
-                const uint32_t part = (threadIdx.x + x * CH_THREADS) / (DP / 4) % 8u, key = part / 2u * 16u + part % 2u * 4u;
-#pragma unroll
-                for (uint32_t e = 0; e < 8; ++e)
-                    if (!(all >> (key + (e & 3u) + (e >> 2) * 8u) & 1u)) vw[x][e] = 0;
-            }
-        }
-#pragma unroll
-        for (uint32_t x = 0; x < K_LOADS; ++x) {
-            const uint32_t n = threadIdx.x + x * CH_THREADS, key = n / PIECES, c = n % PIECES;
-            const dl_u32x2 p = C::template spread<Q>(kw[x].w[0]), r = C::template spread<Q>(kw[x].w[1]);
-            *(dl_u32x4 *)&to.k[(key * PIECES + (c ^ (key & 7u))) * 4u] = dl_u32x4{p[0], p[1], r[0], r[1]};
-        }
-#pragma unroll
-        for (uint32_t x = 0; x < V_LOADS; ++x) {
-            const uint32_t n = threadIdx.x + x * CH_THREADS, d = n % (DP / 4) * 4u, part = n / (DP / 4) % 8u;
-            if (V_ITEMS % CH_THREADS && n >= V_ITEMS) continue;
-            dl_u32x2 four[2][4];
-#pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                const uint32_t w0 = vw[x][4 * g], w1 = vw[x][4 * g + 1], w2 = vw[x][4 * g + 2], w3 = vw[x][4 * g + 3];
-                const uint32_t a01 = __builtin_amdgcn_perm(w1, w0, 0x05010400u), a23 = __builtin_amdgcn_perm(w3, w2, 0x05010400u);
-                const uint32_t b01 = __builtin_amdgcn_perm(w1, w0, 0x07030602u), b23 = __builtin_amdgcn_perm(w3, w2, 0x07030602u);
-                four[g][0] = C::template spread<Q>(__builtin_amdgcn_perm(a23, a01, 0x05040100u));
-                four[g][1] = C::template spread<Q>(__builtin_amdgcn_perm(a23, a01, 0x07060302u));
-                four[g][2] = C::template spread<Q>(__builtin_amdgcn_perm(b23, b01, 0x05040100u));
-                four[g][3] = C::template spread<Q>(__builtin_amdgcn_perm(b23, b01, 0x07060302u));
-            }
-#pragma unroll
-            for (uint32_t f = 0; f < 4; ++f) {
-                const uint32_t r = d + f, c = part ^ ((r & 7u) ^ (r >> 3 & 3u));
-                *(dl_u32x4 *)&to.v[(r * 8u + c) * 4u] = dl_u32x4{four[0][f][0], four[0][f][1], four[1][f][0], four[1][f][1]};
-            }
-        }
-        if (wave == 0) {
-            to.ks[lane] = alive ? scale * a.scale : 0.0f;
-        } else if (wave == 1) {
-            const dl_value_scale<Q> u(scale);
-            to.lu[lane] = alive ? u.log2_c() : -INFINITY;
-            to.iu[lane] = alive ? u.over_c() : 0.0f;
-            to.d[lane] = u.d;
-            const bool some = __any(u.d != 1.0f);
-            if (lane == 0) to.taken_apart = some;
-        }
-    };
-    // Values times what their scales left out, in LDS, by all threads, before anybody works on the step.
-    auto apart = [&](chunk_tile<DP> &to) {
-#pragma unroll 1
-        for (uint32_t n = threadIdx.x; n < DP * 8u; n += CH_THREADS) {
-            const uint32_t r = n / 8u, part = n % 8u, key = part / 2u * 16u + part % 2u * 4u;
-            uint32_t *const v = &to.v[(r * 8u + (part ^ ((r & 7u) ^ (r >> 3 & 3u)))) * 4u];
-#pragma unroll
-            for (uint32_t x = 0; x < 4; ++x) {
-                const float *const d = &to.d[key + x / 2u * 8u + x % 2u * 2u];
-                v[x] = Q::pack(Q::in_range(Q::lo(v[x]) * d[0]), Q::in_range(Q::hi(v[x]) * d[1]));
-            }
-        }
-        __syncthreads();
+    auto hand_on = [&](uint32_t base, uint32_t to) { feed.hand_on(a, base, lds.rows_at[to], lds.alive_at[to]); };
+    auto put = [&](uint32_t to) {
+        feed.clear(lds.alive_at[to]);
+        feed.put_codes(tiles[to]);
+        feed.put_scales(a, tiles[to]);
     };
 
     dl_f32x16 o[DP / 32];
@@ -285,11 +367,11 @@ __global__ void __launch_bounds__(CH_THREADS, DP <= 128 ? 2 : 1) dl_chunk_kernel
         for (int e = 0; e < 16; ++e) o[x][e] = 0.0f;
 
     if (first < end) {
-        look_up(first);
+        feed.look_up(a, first);
         hand_on(first, 0);
         __syncthreads();
-        load(0);
-        look_up(first + CH_KEYS);
+        feed.load(a, lds.rows_at[0]);
+        feed.look_up(a, first + CH_KEYS);
         put(0);
         hand_on(first + CH_KEYS, 1);
         __syncthreads();
@@ -297,10 +379,10 @@ __global__ void __launch_bounds__(CH_THREADS, DP <= 128 ? 2 : 1) dl_chunk_kernel
     uint32_t now = 0;
     for (uint32_t base = first; base < end; base += CH_KEYS, now ^= 1u) {
         const bool more = base + CH_KEYS < end;
-        if (__builtin_amdgcn_readfirstlane((int)tiles[now].taken_apart)) apart(tiles[now]);
+        if (__builtin_amdgcn_readfirstlane((int)tiles[now].taken_apart)) feed_t::apart(tiles[now]);
         if (more) {
-            load(now ^ 1u);
-            look_up(base + 2 * CH_KEYS);
+            feed.load(a, lds.rows_at[now ^ 1u]);
+            feed.look_up(a, base + 2 * CH_KEYS);
         }
         const chunk_tile<DP> &in = tiles[now];
 #pragma unroll 1
@@ -311,12 +393,8 @@ __global__ void __launch_bounds__(CH_THREADS, DP <= 128 ? 2 : 1) dl_chunk_kernel
             dl_f32x16 s;
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[e] = 0.0f;
-            const uint32_t key = 32u * kb + i;
 #pragma unroll
-            for (uint32_t st = 0; st < DP / 16; ++st) {
-                const dl_u32x4 kf = *(const dl_u32x4 *)&in.k[(key * PIECES + ((2u * st + half) ^ (key & 7u))) * 4u];
-                s = Q::mfma32(kf, qf[st], s);
-            }
+            for (uint32_t st = 0; st < DP / 16; ++st) s = Q::mfma32(feed_t::keys(in, kb, st, i, half), qf[st], s);
             float ks[16], lu[16], iu[16];
 #pragma unroll
             for (int e = 0; e < 16; e += 4) {
@@ -360,11 +438,7 @@ __global__ void __launch_bounds__(CH_THREADS, DP <= 128 ? 2 : 1) dl_chunk_kernel
 #pragma unroll
             for (uint32_t x = 0; x < 2; ++x)
 #pragma unroll
-                for (uint32_t dt = 0; dt < DP / 32; ++dt) {
-                    const uint32_t d = 32u * dt + i, c = (4u * kb + 2u * x + half) ^ ((d & 7u) ^ (d >> 3 & 3u));
-                    const dl_u32x4 vf = *(const dl_u32x4 *)&in.v[(d * 8u + c) * 4u];
-                    o[dt] = Q::mfma32(vf, pf[x], o[dt]);
-                }
+                for (uint32_t dt = 0; dt < DP / 32; ++dt) o[dt] = Q::mfma32(feed_t::values(in, kb, x, dt, i, half), pf[x], o[dt]);
         }
         if (more) {
             put(now ^ 1u);
@@ -372,33 +446,230 @@ __global__ void __launch_bounds__(CH_THREADS, DP <= 128 ? 2 : 1) dl_chunk_kernel
         }
         __syncthreads();
     }
-    l += __shfl_xor(l, 32);
-    if (my >= t.rows) return;
-    if (at.pieces > 1u) {
-        const uint64_t to = ((uint64_t)at.slot * a.c.heads + head) * CH_ROWS + (my - t.row0);
-        if (half == 0) a.rl[to] = dl_f32x2{r, l};
+    finish_row<Q, DP>(a, at, t, head, my, half, r, l, o);
+}
+
+// Many rows: 64 a wavefront, one wavefront a SIMD.  An operand read from LDS then serves two products, and codes are turned into elements once for
+// 256 rows.  What a second wavefront would overlap is interleaved here: while the scores of 32 keys become weights, the products of the next
+// 32 keys are under way, and while those weights meet the values, the next scores are scaled and the next step's codes go to LDS.  Three
+// tiles in LDS: one that is worked on, the next one, and the one that is filled while somebody may still be at the first; a barrier a step.
+template <int DP>
+struct wide_lds {
+    chunk_tile<DP> tiles[3];
+    uint64_t rows_at[2][CH_KEYS];
+    uint64_t alive_at[2];
+};
+template <class Q, class C, int DP>
+__global__ void __launch_bounds__(CH_THREADS, DP <= 64 ? 2 : 1) dl_chunk_wide_kernel(const chunk_args a)
+{
+    using feed_t = chunk_feed<Q, C, DP>;
+    __shared__ wide_lds<DP> lds;
+    const uint32_t lane = threadIdx.x % 64u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
+    const uint32_t i = lane % 32u, half = lane / 32u, D = a.c.head_dim, head = blockIdx.x % a.c.heads;
+    chunk_place at;
+    if (!chunk_unit<false>(a, blockIdx.x / a.c.heads, &at)) return;
+    const chunk_rows t(a, at);
+    const uint32_t first = at.piece * at.keys, end = min(first + at.keys, t.end);
+    if (at.piece && first >= end) return;
+    feed_t feed(a, at.b, head, end, lane, wave);
+    const uint32_t wave_row = t.row0 + wave * 64u;
+    // keys before whole_end are seen by all rows of the wavefront
+    const uint32_t whole_end = wave_row < t.rows ? t.seen_by(a, wave_row) : 0u;
+    int32_t last[2];
+    dl_u32x4 qf[2][DP / 16];
 #pragma unroll
-        for (int x = 0; x < DP / 32; ++x)
+    for (int n = 0; n < 2; ++n) {
+        const uint32_t row = min(wave_row + 32u * n + i, t.rows - 1u), j = dl_divide(row, a.groups), h = head * a.group + row - j * a.group;
+        last[n] = t.ahead + (int32_t)j - 4 * (int32_t)half;
+        const char *const q = a.q + (uint64_t)(t.first + j) * a.q_token + h * a.q_head;
 #pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-                const uint32_t d = 32u * x + 2u * e + 4u * half;
-                if (d < D) *(dl_f32x4 *)(a.partial + to * D + d) = dl_f32x4{o[x][e], o[x][e + 1], o[x][e + 2], o[x][e + 3]};
-            }
-        return;
+        for (int s = 0; s < DP / 16; ++s) qf[n][s] = 16u * s < D ? dl_load_at<dl_u32x4>(q + 2u * (16u * s + 8u * half)) : dl_u32x4{0, 0, 0, 0};
     }
-    const bool none = l == 0.0f;
-    const float f = none ? 0.0f : 1.0f / l;
-    char *const to = a.out + (uint64_t)(t.first + j) * a.out_token + h * a.out_head;
+    dl_f32x16 o[2][DP / 32], x[2];
+    float r[2] = {-INFINITY, -INFINITY}, low[2] = {-Q::lift, -Q::lift}, l[2] = {0.0f, 0.0f}, top[2];
 #pragma unroll
-    for (int x = 0; x < DP / 32; ++x)
+    for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int e = 0; e < 16; e += 4) {
-            const uint32_t d = 32u * x + 2u * e + 4u * half;
-            if (d < D)
-                dl_store_at(to + 2u * d, none ? dl_u32x2{0, 0} : dl_u32x2{Q::pack(o[x][e] * f, o[x][e + 1] * f), Q::pack(o[x][e + 2] * f, o[x][e + 3] * f)});
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[n][d][e] = 0.0f;
+
+    // scores of a block of 32 keys: rows of the product are keys (8 (e / 4) + 4 half + e % 4), its columns queries (i)
+    dl_f32x16 zero;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) zero[e] = 0.0f;
+    // what is not seen, and the reference, which follows the largest only where that is 2^8 times above it
+    auto settle = [&](uint32_t key0) {
+        if (key0 + 32u > whole_end) {
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                top[n] = -INFINITY;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    if (2 * (e & ~3) + (e & 3) > last[n] - (int32_t)key0) x[n][e] = -INFINITY;
+                    top[n] = fmaxf(top[n], x[n][e]);
+                }
+            }
         }
-    if (a.lse && half == 0)
-        a.lse[(uint64_t)(t.first + j) * a.q_heads + h] = none ? -INFINITY : ((r == -INFINITY ? 0.0f : r) - Q::lift + log2f(l)) * DL_LN2;
+        if (__any(top[0] > r[0] + 8.0f || top[1] > r[1] + 8.0f)) {
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                const auto swapped = __builtin_amdgcn_permlane32_swap(dl_bits<uint32_t>(top[n]), dl_bits<uint32_t>(top[n]), false, false);
+                const float most = fmaxf(r[n], fmaxf(dl_bits<float>((uint32_t)swapped[0]), dl_bits<float>((uint32_t)swapped[1])));
+                const float ref = most == -INFINITY ? 0.0f : most, fade = __builtin_amdgcn_exp2f(r[n] - ref);
+                r[n] = most;
+                low[n] = ref - Q::lift;
+                l[n] *= fade;
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d) o[n][d] *= fade;
+            }
+        }
+    };
+    // The loop's two parts, in STEPS steps of two products each.  What a step does beside its products is a share of the other work, and what it
+    // reads from LDS has been asked for two steps before (operands, in a ring of four) or one (scales), across the parts' borders; the steps'
+    // order is the compiler's no more.
+    constexpr uint32_t STEPS = DP / 16;
+    dl_u32x4 pf[2][2], ring[4];
+    dl_f32x16 s[2];
+    dl_f32x4 iu, ks, lu;
+    auto inverse = [&](const chunk_tile<DP> &of, uint32_t kb, uint32_t quad) { iu = *(const dl_f32x4 *)&of.iu[32u * kb + 8u * quad + 4u * half]; };
+    auto scales = [&](const chunk_tile<DP> &of, uint32_t kb, uint32_t quad) {
+        ks = *(const dl_f32x4 *)&of.ks[32u * kb + 8u * quad + 4u * half];
+        lu = *(const dl_f32x4 *)&of.lu[32u * kb + 8u * quad + 4u * half];
+    };
+    // The scores x of block kb of `in` become weights pf, while the products of block kb_then of `then` are taken.
+    auto weights_and_products = [&](const chunk_tile<DP> &in, uint32_t kb, const chunk_tile<DP> &then, uint32_t kb_then) {
+        constexpr uint32_t EACH = 8 / STEPS;
+#pragma unroll
+        for (uint32_t st = 0; st < STEPS; ++st) {
+            ring[(st + 2) % 4] = st + 2 < STEPS ? feed_t::keys(then, kb_then, st + 2, i, half)
+                                                : feed_t::values(in, kb, (st + 2 - STEPS) / (DP / 32), (st + 2 - STEPS) % (DP / 32), i, half);
+#pragma unroll
+            for (int n = 0; n < 2; ++n) s[n] = Q::mfma32(ring[st % 4], qf[n][st], st ? s[n] : zero);
+#pragma unroll
+            for (uint32_t g = st * EACH; g < st * EACH + EACH; ++g) {
+                const uint32_t n = g % 2, e = 4 * (g / 2);
+                float w[4];
+#pragma unroll
+                for (int f = 0; f < 4; ++f) {
+                    w[f] = __builtin_amdgcn_exp2f(x[n][e + f] - low[n]);
+                    l[n] = fmaf(w[f], iu[f], l[n]);
+                }
+                pf[n][e / 8][e % 8 / 2] = Q::pack(w[0], w[1]);
+                pf[n][e / 8][e % 8 / 2 + 1] = Q::pack(w[2], w[3]);
+                if (n && e < 12) inverse(in, kb, e / 4 + 1);
+            }
+            if (st + 1 == STEPS) scales(then, kb_then, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // The weights of block kb of `in` meet its values, while the scores of block kb_then of `scored` are scaled and the codes that have come go
+    // to tile `then` (PUT) or the next ones are asked for.
+    auto sums_and_scores = [&](const chunk_tile<DP> &in, uint32_t kb, const chunk_tile<DP> &scored, uint32_t kb_then, chunk_tile<DP> &then, const uint64_t (&rows_at)[CH_KEYS],
+                               auto with_put) {
+        constexpr bool PUT = decltype(with_put)::value;
+        constexpr uint32_t LEFT = STEPS - 1;  // (the last of the products is not done before the first step's)
+        uint64_t from[2] = {};
+#pragma unroll
+        for (uint32_t st = 0; st < STEPS; ++st) {
+            if (st + 2 < STEPS)
+                ring[(st + 2) % 4] = feed_t::values(in, kb, (st + 2) / (DP / 32), (st + 2) % (DP / 32), i, half);
+            else if (!PUT)
+                ring[(st + 2) % 4] = feed_t::keys(then, 1, st + 2 - STEPS, i, half);
+#pragma unroll
+            for (int n = 0; n < 2; ++n) o[n][st % (DP / 32)] = Q::mfma32(ring[st % 4], pf[n][st / (DP / 32)], o[n][st % (DP / 32)]);
+            if constexpr (PUT) {
+#pragma unroll
+                for (uint32_t n = st * feed_t::PUT_PARTS / STEPS; n < (st + 1) * feed_t::PUT_PARTS / STEPS; ++n) feed.put_part(then, n);
+            } else {
+                // (rows a step before the loads from there)
+                constexpr uint32_t MOST = (feed_t::LOAD_PARTS + LEFT - 1) / LEFT;
+                static_assert(MOST <= 2 || DP < 128, "two rows on their way");
+                if (st)
+#pragma unroll
+                    for (uint32_t n = 0; n < MOST; ++n)
+                        if ((st - 1) * MOST + n < feed_t::LOAD_PARTS) feed.load_part(a, n < 2 ? from[n] : feed_t::load_from(rows_at, (st - 1) * MOST + n), (st - 1) * MOST + n);
+#pragma unroll
+                for (uint32_t n = 0; n < 2; ++n)
+                    if (st < LEFT && n < MOST && st * MOST + n < feed_t::LOAD_PARTS) from[n] = feed_t::load_from(rows_at, st * MOST + n);
+            }
+            if (st) {
+#pragma unroll
+                for (uint32_t g = (st - 1) * 8 / LEFT; g < st * 8 / LEFT; ++g) {
+                    const uint32_t n = g % 2, e = 4 * (g / 2);
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) {
+                        x[n][e + f] = fmaf(s[n][e + f], ks[f], lu[f]);
+                        top[n] = f || e ? fmaxf(top[n], x[n][e + f]) : x[n][e + f];
+                    }
+                    if (n && e < 12) scales(scored, kb_then, e / 4 + 1);
+                }
+            }
+            if (st + 1 == STEPS) {
+                if (PUT)
+                    inverse(in, 1, 0);
+                else
+                    inverse(then, 0, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+
+    if (first < end) {
+        feed.look_up(a, first);
+        feed.hand_on(a, first, lds.rows_at[0], lds.alive_at[0]);
+        __syncthreads();
+        feed.load(a, lds.rows_at[0]);
+        feed.look_up(a, first + CH_KEYS);
+        feed.clear(lds.alive_at[0]);
+        feed.put_codes(lds.tiles[0]);
+        feed.put_scales(a, lds.tiles[0]);
+        feed.hand_on(a, first + CH_KEYS, lds.rows_at[1], lds.alive_at[1]);
+        __syncthreads();
+        feed.load(a, lds.rows_at[1]);
+        feed.look_up(a, first + 2 * CH_KEYS);
+        if (__builtin_amdgcn_readfirstlane((int)lds.tiles[0].taken_apart)) feed_t::apart(lds.tiles[0]);
+        inverse(lds.tiles[0], 0, 0);
+#pragma unroll
+        for (uint32_t st = 0; st < 2; ++st) ring[st] = feed_t::keys(lds.tiles[0], 1, st, i, half);
+#pragma unroll
+        for (uint32_t st = 0; st < DP / 16; ++st)
+#pragma unroll
+            for (int n = 0; n < 2; ++n) s[n] = Q::mfma32(feed_t::keys(lds.tiles[0], 0, st, i, half), qf[n][st], st ? s[n] : zero);
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const uint32_t key = 8u * (e / 4) + 4u * half + e % 4;
+                x[n][e] = fmaf(s[n][e], lds.tiles[0].ks[key], lds.tiles[0].lu[key]);
+                top[n] = e ? fmaxf(top[n], x[n][e]) : x[n][e];
+            }
+    }
+    uint32_t now = 0, slot = 0;
+    for (uint32_t base = first; base < end; base += CH_KEYS) {
+        // (behind the last step whatever lies in the next tile is worked on, and not used)
+        const uint32_t next = now == 2u ? 0u : now + 1u;
+        chunk_tile<DP> &in = lds.tiles[now], &then = lds.tiles[next];
+        feed.clear(lds.alive_at[slot ^ 1u]);
+        settle(base);
+        weights_and_products(in, 0, in, 1);
+        // (the scores are those of this tile's second block; what goes to the next tile is its codes)
+        sums_and_scores(in, 0, in, 1, then, lds.rows_at[slot], std::true_type{});
+        feed.put_scales(a, then);
+        feed.hand_on(a, base + 2 * CH_KEYS, lds.rows_at[slot], lds.alive_at[slot]);
+        __syncthreads();
+#pragma unroll
+        for (uint32_t st = 0; st < 2; ++st) ring[st] = feed_t::keys(then, 0, st, i, half);
+        feed.look_up(a, base + 3 * CH_KEYS);
+        if (base + CH_KEYS < end && __builtin_amdgcn_readfirstlane((int)then.taken_apart)) feed_t::apart(then);
+        settle(base + 32u);
+        weights_and_products(in, 1, then, 0);
+        sums_and_scores(in, 1, then, 0, then, lds.rows_at[slot], std::false_type{});
+        now = next;
+        slot ^= 1u;
+    }
+#pragma unroll
+    for (int n = 0; n < 2; ++n) finish_row<Q, DP>(a, at, t, head, wave_row + 32u * n + i, half, r[n], l[n], o[n]);
 }
 
 // Joins the pieces of tiles that are cut.  A workgroup has 32 rows of one; DP / 4 lanes hold a row's sums, four each.
@@ -408,9 +679,9 @@ __global__ void __launch_bounds__(CH_THREADS) dl_chunk_join_kernel(const chunk_a
 {
     constexpr uint32_t LANES = DP / 4, AT_ONCE = CH_THREADS / LANES, AHEAD = 4;
     const uint32_t D = a.c.head_dim, d0 = threadIdx.x % LANES * 4u;
-    const uint32_t part = blockIdx.x % (CH_ROWS / JOIN_ROWS), head = blockIdx.x / (CH_ROWS / JOIN_ROWS) % a.c.heads;
+    const uint32_t parts = a.tile_rows / JOIN_ROWS, part = blockIdx.x % parts, head = blockIdx.x / parts % a.c.heads;
     chunk_place at;
-    if (!chunk_unit<true>(a, blockIdx.x / (CH_ROWS / JOIN_ROWS) / a.c.heads, &at)) return;
+    if (!chunk_unit<true>(a, blockIdx.x / parts / a.c.heads, &at)) return;
     const chunk_rows t(a, at);
     const uint32_t pieces = max((t.end + at.keys - 1u) / at.keys, 1u);
     for (uint32_t in = part * JOIN_ROWS + threadIdx.x / LANES; in < (part + 1u) * JOIN_ROWS; in += AT_ONCE) {
@@ -423,7 +694,7 @@ __global__ void __launch_bounds__(CH_THREADS) dl_chunk_join_kernel(const chunk_a
             dl_f32x4 x[AHEAD];
 #pragma unroll
             for (uint32_t k = 0; k < AHEAD; ++k) {
-                const uint64_t from = ((uint64_t)(at.slot + min(p0 + k, pieces - 1u)) * a.c.heads + head) * CH_ROWS + in;
+                const uint64_t from = ((uint64_t)(at.slot + min(p0 + k, pieces - 1u)) * a.c.heads + head) * a.tile_rows + in;
                 rl[k] = a.rl[from];
                 x[k] = d0 < D ? *(const dl_f32x4 *)(a.partial + from * D + d0) : dl_f32x4{0, 0, 0, 0};
                 if (p0 + k >= pieces) rl[k] = dl_f32x2{-INFINITY, 0.0f}, x[k] = dl_f32x4{0, 0, 0, 0};
@@ -456,27 +727,29 @@ __global__ void __launch_bounds__(CH_THREADS) dl_chunk_join_kernel(const chunk_a
 struct chunk_shape {
     uint64_t units;   // at most so many pieces a head, over all sequences
     uint32_t target;  // 0: nothing is cut
+    uint32_t tile_rows;
 };
 
 int chunk_sizes(const dl_kv_cache *cache, const dl_chunk_attention_args *args, dl_cache_view *view, chunk_shape *sh)
 {
     const int rc = dl_packed_sizes(cache, args, view);
     if (rc != DL_OK) return rc;
-    *sh = chunk_shape{0, 0};
+    *sh = chunk_shape{};
     if (!args->tokens || !args->q_heads || !args->batch) return DL_OK;
     const uint64_t rows = (uint64_t)args->tokens * (uint32_t)(args->q_heads / cache->heads);
     // every sequence begins a tile of its own
-    uint64_t tiles = rows / CH_ROWS + (uint64_t)args->batch;
+    sh->tile_rows = cache->head_dim <= 128 && rows >= 1024u * (uint64_t)args->batch ? 64u * CH_WAVES : 32u * CH_WAVES;
+    uint64_t tiles = rows / sh->tile_rows + (uint64_t)args->batch;
     if (tiles > rows) tiles = rows;
     const uint64_t most = (uint64_t)args->max_pages * (uint32_t)cache->page_tokens;
     // Workgroups at once, by the registers and LDS: two a compute unit up to head_dim 128, one above.
-    const uint32_t slots = cache->head_dim > 128 ? 256u : 512u, round = slots / (uint32_t)cache->heads;
+    const uint32_t slots = cache->head_dim > 128 || (cache->head_dim > 64 && sh->tile_rows > 32u * CH_WAVES) ? 256u : 512u, round = slots / (uint32_t)cache->heads;
     if (most > LEAST_STEPS * CH_KEYS && round > 1u) sh->target = round;
     sh->units = tiles + sh->target;
     return DL_OK;
 }
 
-size_t chunk_slots(const chunk_shape &sh, uint32_t heads) { return (size_t)2 * sh.target * heads * CH_ROWS; }
+size_t chunk_slots(const chunk_shape &sh, uint32_t heads) { return (size_t)2 * sh.target * heads * sh.tile_rows; }
 
 }  // namespace
 
@@ -516,6 +789,7 @@ extern "C" int dl_chunk_attention(const dl_kv_cache *cache, const dl_chunk_atten
     a.q_heads = (uint32_t)args->q_heads;
     a.group = a.q_heads / a.c.heads;
     a.groups = dl_make_divider(a.group ? a.group : 1u);
+    a.tile_rows = sh.tile_rows;
     a.target = sh.target;
     a.scale = args->scale * DL_LOG2E;
     const uint64_t grid = sh.units * a.c.heads;
@@ -525,10 +799,15 @@ extern "C" int dl_chunk_attention(const dl_kv_cache *cache, const dl_chunk_atten
         auto go = [&](auto dp) {
             constexpr int DP = decltype(dp)::value;
             dl_with_format(cache->format, [&](auto c) {
+                if constexpr (DP <= 128)
+                    if (sh.tile_rows > 32u * CH_WAVES) {
+                        hipLaunchKernelGGL((dl_chunk_wide_kernel<decltype(q), decltype(c), DP>), dim3((uint32_t)grid), dim3(CH_THREADS), 0, hs, a);
+                        return;
+                    }
                 hipLaunchKernelGGL((dl_chunk_kernel<decltype(q), decltype(c), DP>), dim3((uint32_t)grid), dim3(CH_THREADS), 0, hs, a);
             });
             if (sh.target)
-                hipLaunchKernelGGL((dl_chunk_join_kernel<decltype(q), DP>), dim3(sh.target * a.c.heads * (CH_ROWS / JOIN_ROWS)), dim3(CH_THREADS), 0, hs, a);
+                hipLaunchKernelGGL((dl_chunk_join_kernel<decltype(q), DP>), dim3(sh.target * a.c.heads * (sh.tile_rows / JOIN_ROWS)), dim3(CH_THREADS), 0, hs, a);
         };
         if (a.c.head_dim <= 64)
             go(std::integral_constant<int, 64>{});

@@ -262,8 +262,9 @@ __global__ void __launch_bounds__(MANY_THREADS, DP <= 128 ? 4 : 2) dl_weigh_many
                         const uint32_t piece = 2u * (2u * (x / 2) + half) + x % 2u;
                         s = Q::mfma32(kf[x], *(const dl_u32x4 *)&tiles[now][(i * PIECES + (piece ^ (i & 7u))) * 4u], s);
                     }
-                    const int32_t seen = ahead + (int32_t)(dl_divide(r0 + i, a.groups)) - (int32_t)base;
-                    add_weights(s, scales[wave], lses[now][i], r0 < whole, seen, half, sum);
+                    const bool masked = r0 < whole;
+                    const int32_t seen = masked ? ahead + (int32_t)dl_divide(r0 + i, a.groups) - (int32_t)base : 0;
+                    add_weights(s, scales[wave], lses[now][i], masked, seen, half, sum);
                 }
                 if (more) put(now ^ 1u);
                 __syncthreads();
