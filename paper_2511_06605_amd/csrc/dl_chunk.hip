@@ -121,10 +121,13 @@ struct chunk_rows {
     __device__ __forceinline__ uint32_t seen_by(const chunk_args &a, uint32_t row) const { return (uint32_t)max(ahead + (int32_t)(dl_divide(row, a.groups)) + 1, 0); }
 };
 
+// Operands lie in rows with 16 bytes between them, so that eight neighbouring lanes, a row each, use all banks, and a lane's addresses
+// differ by constants.
 template <int DP>
 struct alignas(16) chunk_tile {  // (reads of 16 bytes that lie at fours take twice as long)
-    uint32_t k[CH_KEYS * DP / 2];  // key, dim
-    uint32_t v[CH_KEYS * DP / 2];  // dim, key: of each 16 keys 0 - 3, 8 - 11, 4 - 7, 12 - 15
+    static constexpr uint32_t K_ROW = DP / 2 + 4, V_ROW = CH_KEYS / 2 + 4;
+    uint32_t k[CH_KEYS * K_ROW];  // key, dim
+    uint32_t v[DP * V_ROW];       // dim, key: of each 16 keys 0 - 3, 8 - 11, 4 - 7, 12 - 15
     float ks[CH_KEYS], lu[CH_KEYS], iu[CH_KEYS], d[CH_KEYS];
     uint32_t taken_apart;  // some value's d is not 1
 };
@@ -135,13 +138,12 @@ struct chunk_lds {
     uint64_t alive_at[2];          // bit k: key k is one of the piece, in a page of the pool
 };
 
-// Codes on their way into a tile.  Operands lie in rows of 16-byte pieces, whose places are exchanged (by an exclusive or with the row's
-// number) so that eight neighbouring lanes use all banks, in reads and in writes.
+// Codes on their way into a tile.
 template <class Q, class C, int DP>
 struct chunk_feed {
     static constexpr uint32_t PIECES = DP / 8;                          // 16-byte pieces of a key's row
     static constexpr uint32_t K_LOADS = CH_KEYS * PIECES / CH_THREADS;  // of 8 codes
-    static constexpr uint32_t V_ITEMS = 8 * (DP / 4);                   // 8 keys (half of 16) x 4 dims
+    static constexpr uint32_t V_ITEMS = 8 * (DP / 4);                   // 8 keys (half of 16) x 4 dims; eight neighbouring lanes fill a row
     static constexpr uint32_t V_LOADS = (V_ITEMS + CH_THREADS - 1) / CH_THREADS;
     const int32_t *table;
     const char *k_from, *v_from, *scales;
@@ -185,7 +187,7 @@ struct chunk_feed {
     static __device__ __forceinline__ uint64_t load_from(const uint64_t (&rows_at)[CH_KEYS], uint32_t part_of)
     {
         if (part_of < K_LOADS) return rows_at[(threadIdx.x + part_of * CH_THREADS) / PIECES];
-        const uint32_t x = (part_of - K_LOADS) / 8u, e = (part_of - K_LOADS) % 8u, part = (threadIdx.x + x * CH_THREADS) / (DP / 4) % 8u;
+        const uint32_t e = (part_of - K_LOADS) % 8u, part = threadIdx.x % 8u;
         return rows_at[part / 2u * 16u + part % 2u * 4u + (e & 3u) + (e >> 2) * 8u];
     }
     __device__ __forceinline__ void load_part(const chunk_args &a, uint64_t from, uint32_t part_of)
@@ -195,7 +197,7 @@ struct chunk_feed {
             kw[part_of] = dl_load_words<8>(k_from + from + min((threadIdx.x + part_of * CH_THREADS) % PIECES * 8u, D - 8u));
         } else {
             const uint32_t x = (part_of - K_LOADS) / 8u, e = (part_of - K_LOADS) % 8u;
-            vw[x][e] = dl_load_at<uint32_t>(v_from + from + min((threadIdx.x + x * CH_THREADS) % (DP / 4) * 4u, D - 4u));
+            vw[x][e] = dl_load_at<uint32_t>(v_from + from + min((threadIdx.x + x * CH_THREADS) / 8u * 4u, D - 4u));
         }
     }
     __device__ __forceinline__ void load(const chunk_args &a, const uint64_t (&rows_at)[CH_KEYS])
@@ -215,7 +217,7 @@ struct chunk_feed {
             if (!(all >> ((threadIdx.x + x * CH_THREADS) / PIECES) & 1u)) kw[x] = dl_words<8>{};
 #pragma unroll
         for (uint32_t x = 0; x < V_LOADS; ++x) {
-            const uint32_t part = (threadIdx.x + x * CH_THREADS) / (DP / 4) % 8u, key = part / 2u * 16u + part % 2u * 4u;
+            const uint32_t part = threadIdx.x % 8u, key = part / 2u * 16u + part % 2u * 4u;
 #pragma unroll
             for (uint32_t e = 0; e < 8; ++e)
                 if (!(all >> (key + (e & 3u) + (e >> 2) * 8u) & 1u)) vw[x][e] = 0;
@@ -228,11 +230,11 @@ struct chunk_feed {
         if (part_of < K_LOADS) {
             const uint32_t x = part_of, n = threadIdx.x + x * CH_THREADS, key = n / PIECES, c = n % PIECES;
             const dl_u32x2 p = C::template spread<Q>(kw[x].w[0]), r = C::template spread<Q>(kw[x].w[1]);
-            *(dl_u32x4 *)&to.k[(key * PIECES + (c ^ (key & 7u))) * 4u] = dl_u32x4{p[0], p[1], r[0], r[1]};
+            *(dl_u32x4 *)&to.k[key * chunk_tile<DP>::K_ROW + c * 4u] = dl_u32x4{p[0], p[1], r[0], r[1]};
             return;
         }
         const uint32_t x = (part_of - K_LOADS) / 4u, f = (part_of - K_LOADS) % 4u;
-        const uint32_t n = threadIdx.x + x * CH_THREADS, d = n % (DP / 4) * 4u, part = n / (DP / 4) % 8u;
+        const uint32_t n = threadIdx.x + x * CH_THREADS, d = n / 8u * 4u, part = n % 8u;
         if (V_ITEMS % CH_THREADS && n >= V_ITEMS) return;
         dl_u32x2 two[2];
 #pragma unroll
@@ -241,8 +243,7 @@ struct chunk_feed {
             const uint32_t a01 = __builtin_amdgcn_perm(vw[x][4 * g + 1], vw[x][4 * g], pick), a23 = __builtin_amdgcn_perm(vw[x][4 * g + 3], vw[x][4 * g + 2], pick);
             two[g] = C::template spread<Q>(__builtin_amdgcn_perm(a23, a01, f % 2 ? 0x07060302u : 0x05040100u));
         }
-        const uint32_t r = d + f, c = part ^ ((r & 7u) ^ (r >> 3 & 3u));
-        *(dl_u32x4 *)&to.v[(r * 8u + c) * 4u] = dl_u32x4{two[0][0], two[0][1], two[1][0], two[1][1]};
+        *(dl_u32x4 *)&to.v[(d + f) * chunk_tile<DP>::V_ROW + part * 4u] = dl_u32x4{two[0][0], two[0][1], two[1][0], two[1][1]};
     }
     __device__ __forceinline__ void put_codes(chunk_tile<DP> &to)
     {
@@ -268,7 +269,7 @@ struct chunk_feed {
 #pragma unroll 1
         for (uint32_t n = threadIdx.x; n < DP * 8u; n += CH_THREADS) {
             const uint32_t r = n / 8u, part = n % 8u, key = part / 2u * 16u + part % 2u * 4u;
-            uint32_t *const v = &to.v[(r * 8u + (part ^ ((r & 7u) ^ (r >> 3 & 3u)))) * 4u];
+            uint32_t *const v = &to.v[r * chunk_tile<DP>::V_ROW + part * 4u];
 #pragma unroll
             for (uint32_t x = 0; x < 4; ++x) {
                 const float *const d = &to.d[key + x / 2u * 8u + x % 2u * 2u];
@@ -280,13 +281,11 @@ struct chunk_feed {
     // The operands of a product: keys 32 kb + i against dims 16 st + 8 half .., and dims 32 dt + i against the x-th 16 of keys 32 kb ..
     static __device__ __forceinline__ dl_u32x4 keys(const chunk_tile<DP> &in, uint32_t kb, uint32_t st, uint32_t i, uint32_t half)
     {
-        const uint32_t key = 32u * kb + i;
-        return *(const dl_u32x4 *)&in.k[(key * PIECES + ((2u * st + half) ^ (key & 7u))) * 4u];
+        return *(const dl_u32x4 *)&in.k[(32u * kb + i) * chunk_tile<DP>::K_ROW + (2u * st + half) * 4u];
     }
     static __device__ __forceinline__ dl_u32x4 values(const chunk_tile<DP> &in, uint32_t kb, uint32_t x, uint32_t dt, uint32_t i, uint32_t half)
     {
-        const uint32_t d = 32u * dt + i, c = (4u * kb + 2u * x + half) ^ ((d & 7u) ^ (d >> 3 & 3u));
-        return *(const dl_u32x4 *)&in.v[(d * 8u + c) * 4u];
+        return *(const dl_u32x4 *)&in.v[(32u * dt + i) * chunk_tile<DP>::V_ROW + (4u * kb + 2u * x + half) * 4u];
     }
 };
 
@@ -560,8 +559,15 @@ __global__ void __launch_bounds__(CH_THREADS, DP <= 64 ? 2 : 1) dl_chunk_wide_ke
                 if (n && e < 12) inverse(in, kb, e / 4 + 1);
             }
             if (st + 1 == STEPS) scales(then, kb_then, 0);
+            // (here, and not where they are needed)
+#pragma unroll
+            for (int n = 0; n < 2; ++n) asm volatile("" : "+v"(l[n]));
             __builtin_amdgcn_sched_barrier(0);
         }
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int p = 0; p < 2; ++p) asm volatile("" : "+v"(pf[n][p]));
     };
     // The weights of block kb of `in` meet its values, while the scores of block kb_then of `scored` are scaled and the codes that have come go
     // to tile `then` (PUT) or the next ones are asked for.
@@ -650,9 +656,9 @@ __global__ void __launch_bounds__(CH_THREADS, DP <= 64 ? 2 : 1) dl_chunk_wide_ke
         // (behind the last step whatever lies in the next tile is worked on, and not used)
         const uint32_t next = now == 2u ? 0u : now + 1u;
         chunk_tile<DP> &in = lds.tiles[now], &then = lds.tiles[next];
-        feed.clear(lds.alive_at[slot ^ 1u]);
         settle(base);
         weights_and_products(in, 0, in, 1);
+        feed.clear(lds.alive_at[slot ^ 1u]);
         // (the scores are those of this tile's second block; what goes to the next tile is its codes)
         sums_and_scores(in, 0, in, 1, then, lds.rows_at[slot], std::true_type{});
         feed.put_scales(a, then);
