@@ -29,55 +29,80 @@ struct chunk_args {
     int64_t q_token, q_head, out_token, out_head;  // bytes
     uint32_t q_heads, group;
     dl_divider groups;  // by group
-    uint32_t tile_rows;  // 32 or 64 a wavefront
-    uint32_t target;     // see chunk_unit; 0: a piece a tile
+    uint32_t tile_rows;           // 32 or 64 a wavefront
+    uint32_t most_cut;            // 0: nothing is cut
+    float round;                  // workgroups at once, by the heads
+    uint32_t *size;               // what the pieces' size has come to, for the join
     float scale;         // times log2 e
 };
 
-// The key axis of a sequence is cut into pieces where there are few tiles, by the lengths, which only the device knows: into pieces of as
-// many steps as share the steps of all tiles out over `target` pieces.  All tiles of a sequence are cut alike, at multiples of `keys`; a
-// tile whose rows end before a piece begins has nothing of it.  With T steps in all a piece has T / target or more, so tiles that are
-// cut have no more than 2 target pieces between them: as many slots there are, and no more than target such tiles.
+// The key axis of a sequence is cut into pieces where there are few tiles, by the lengths, which only the device knows: into pieces of at most
+// `size` steps.  All tiles of a sequence are cut alike, at multiples of `keys`; a tile whose rows end before a piece begins has nothing of
+// it.  What leaves something behind for the join are the pieces of sequences that are cut: no more than `most_cut` over all of them, and so
+// no more than half as many tiles.
+// Which size: a round of workgroups takes as long as the steps of one and START more, a piece costs the join JOIN steps; a lane of a
+// wavefront looks at the size that cuts the longest sequence into its number + 1 pieces.  Batches of more than SEARCH_MAX sequences are not
+// looked at one by one: with T steps of all tiles, T / (most_cut / 2), so that those that are cut have at most twice as many pieces.
 // Every wavefront works this out from the lengths for itself.
-constexpr uint32_t LEAST_STEPS = 4;
+constexpr float START = 3.0f, JOIN = 0.1f;
+constexpr uint32_t SEARCH_MAX = 16;
 
 struct chunk_place {
     uint32_t b, tile, piece, pieces, keys;
     uint32_t slot;  // of this piece; the others of the tile lie next to it
+    uint32_t size;
+    uint32_t first, queries, len;  // of the sequence: its first row of q
 };
-__device__ __forceinline__ uint32_t tiles_of(const chunk_args &a, uint32_t b)
-{
-    const uint32_t first = a.p.start(b);
-    return (a.p.queries(b, first) * a.group + a.tile_rows - 1u) / a.tile_rows;
-}
-__device__ __forceinline__ uint32_t steps_of(const chunk_args &a, uint32_t b) { return (a.p.len(b) + CH_KEYS - 1u) / CH_KEYS; }
-
 // The unit-th piece of all (CUT: the unit-th tile of those that are cut, its first piece); false: there is none.
 template <bool CUT>
 __device__ __forceinline__ bool chunk_unit(const chunk_args &a, uint32_t unit, chunk_place *at)
 {
     const uint32_t lane = threadIdx.x % 64u;
     uint32_t size = 1u << 26, tiles = 0, steps = 0;
-    if (a.target) {
+    const bool at_once = a.p.batch <= 64u;
+    uint32_t first = 0, queries = 0, len = 0;
+    auto look = [&](uint32_t b0) {
+        const uint32_t b = min(b0 + lane, a.p.batch - 1u);
+        first = a.p.start(b);
+        queries = b0 + lane < a.p.batch ? a.p.queries(b, first) : 0u;
+        len = a.p.len(b);
+        tiles = (queries * a.group + a.tile_rows - 1u) / a.tile_rows;
+        steps = (len + CH_KEYS - 1u) / CH_KEYS;
+    };
+    if (at_once) look(0);
+    if (CUT) {
+        size = max(*a.size, 1u);
+    } else if (a.most_cut && a.p.batch <= SEARCH_MAX) {
+        uint32_t longest = 1;
+        auto of = [&](uint32_t x, uint32_t b) { return (uint32_t)__builtin_amdgcn_readlane((int)x, (int)b); };
+        for (uint32_t b = 0; b < a.p.batch; ++b) longest = of(tiles, b) ? max(longest, of(steps, b)) : longest;
+        // (whole numbers far below 2^24: with half a unit in front of the quotient its rounding makes no difference)
+        const float mine = ceilf(((float)longest - 0.5f) * __builtin_amdgcn_rcpf((float)(lane + 1u))), over = __builtin_amdgcn_rcpf(mine);
+        float units = 0.0f, cut = 0.0f, most = 1.0f;
+        for (uint32_t b = 0; b < a.p.batch; ++b) {
+            const float its = (float)of(tiles, b), pieces = fmaxf(ceilf(((float)of(steps, b) - 0.5f) * over), 1.0f);
+            units = fmaf(its, pieces, units);
+            cut += pieces > 1.0f ? its * pieces : 0.0f;
+            most = its > 0.0f ? fmaxf(most, pieces) : most;
+        }
+        float cost = ceilf(units / a.round) * (mine + START) + (most > 1.0f ? JOIN * most : 0.0f);
+        if (cut > (float)a.most_cut) cost = INFINITY;
+        const uint32_t least = ~dl_largest(~dl_bits<uint32_t>(cost));  // (costs are positive: in order as whole numbers)
+        size = (uint32_t)of((uint32_t)mine, (uint32_t)__ffsll((long long)__ballot(dl_bits<uint32_t>(cost) == least)) - 1u);
+    } else if (a.most_cut) {
         uint64_t all = 0;
         for (uint32_t b0 = 0; b0 < a.p.batch; b0 += 64u) {
-            const bool there = b0 + lane < a.p.batch;
-            tiles = there ? tiles_of(a, b0 + lane) : 0u;
-            steps = there ? steps_of(a, b0 + lane) : 0u;
+            if (!at_once) look(b0);
             uint64_t x = (uint64_t)tiles * steps;
 #pragma unroll
             for (int d = 1; d < 64; d *= 2) x += (uint64_t)__shfl_xor((unsigned long long)x, d);
             all += x;
         }
-        size = max((uint32_t)((all + a.target - 1u) / a.target), LEAST_STEPS);
+        size = max((uint32_t)((all + a.most_cut / 2u - 1u) / (a.most_cut / 2u)), 1u);
     }
     uint32_t before = 0, slots = 0;
     for (uint32_t b0 = 0; b0 < a.p.batch; b0 += 64u) {
-        if (a.p.batch > 64u || !a.target) {
-            const bool there = b0 + lane < a.p.batch;
-            tiles = there ? tiles_of(a, b0 + lane) : 0u;
-            steps = there ? steps_of(a, b0 + lane) : 0u;
-        }
+        if (!at_once) look(b0);
         const uint32_t pieces = max((steps + size - 1u) / size, 1u), cut = pieces > 1u ? tiles * pieces : 0u;
         const uint32_t counted = CUT ? (pieces > 1u ? tiles : 0u) : tiles * pieces;
         const uint32_t up_to = before + dl_sum_up_to(counted), slots_up_to = slots + dl_sum_up_to(cut);
@@ -95,6 +120,10 @@ __device__ __forceinline__ bool chunk_unit(const chunk_args &a, uint32_t unit, c
             at->tile = of(tiles) - 1u - (CUT ? n : n / its);
             at->piece = CUT ? 0u : n % its;
             at->slot = of(slots_up_to) - of(cut) + (CUT ? n * its : n);
+            at->size = size;
+            at->first = of(first);
+            at->queries = of(queries);
+            at->len = of(len);
             return true;
         }
         before = (uint32_t)__builtin_amdgcn_readlane((int)up_to, 63);
@@ -111,11 +140,10 @@ struct chunk_rows {
 
     __device__ __forceinline__ chunk_rows(const chunk_args &a, const chunk_place &at)
     {
-        first = a.p.start(at.b);
-        const uint32_t n = a.p.queries(at.b, first), len = a.p.len(at.b);
-        rows = n * a.group;
+        first = at.first;
+        rows = at.queries * a.group;
         row0 = at.tile * a.tile_rows;
-        ahead = (int32_t)len - (int32_t)n;
+        ahead = (int32_t)at.len - (int32_t)at.queries;
         end = seen_by(a, min(row0 + a.tile_rows, rows) - 1u);
     }
     __device__ __forceinline__ uint32_t seen_by(const chunk_args &a, uint32_t row) const { return (uint32_t)max(ahead + (int32_t)(dl_divide(row, a.groups)) + 1, 0); }
@@ -335,6 +363,7 @@ __global__ void __launch_bounds__(CH_THREADS, DP <= 128 ? 2 : 1) dl_chunk_kernel
     const uint32_t i = lane % 32u, half = lane / 32u, D = a.c.head_dim, head = blockIdx.x % a.c.heads;
     chunk_place at;
     if (!chunk_unit<false>(a, blockIdx.x / a.c.heads, &at)) return;
+    if (a.most_cut && blockIdx.x == 0 && threadIdx.x == 0) *a.size = at.size;
     const chunk_rows t(a, at);
     const uint32_t first = at.piece * at.keys, end = min(first + at.keys, t.end);
     if (at.piece && first >= end) return;
@@ -467,6 +496,7 @@ __global__ void __launch_bounds__(CH_THREADS, DP <= 64 ? 2 : 1) dl_chunk_wide_ke
     const uint32_t i = lane % 32u, half = lane / 32u, D = a.c.head_dim, head = blockIdx.x % a.c.heads;
     chunk_place at;
     if (!chunk_unit<false>(a, blockIdx.x / a.c.heads, &at)) return;
+    if (a.most_cut && blockIdx.x == 0 && threadIdx.x == 0) *a.size = at.size;
     const chunk_rows t(a, at);
     const uint32_t first = at.piece * at.keys, end = min(first + at.keys, t.end);
     if (at.piece && first >= end) return;
@@ -678,62 +708,62 @@ __global__ void __launch_bounds__(CH_THREADS, DP <= 64 ? 2 : 1) dl_chunk_wide_ke
     for (int n = 0; n < 2; ++n) finish_row<Q, DP>(a, at, t, head, wave_row + 32u * n + i, half, r[n], l[n], o[n]);
 }
 
-// Joins the pieces of tiles that are cut.  A workgroup has 32 rows of one; DP / 4 lanes hold a row's sums, four each.
-constexpr uint32_t JOIN_ROWS = 32;
+// Joins the pieces of tiles that are cut.  DP / 4 lanes hold a row's sums, four each, and a workgroup has as many rows as its lanes hold: what it
+// takes is the way to its pieces (9 of them 11.6 us with four times the rows a workgroup and half the loads at once).
+template <int DP>
+constexpr uint32_t JOIN_ROWS = CH_THREADS / (DP / 4);
 template <class Q, int DP>
 __global__ void __launch_bounds__(CH_THREADS) dl_chunk_join_kernel(const chunk_args a)
 {
-    constexpr uint32_t LANES = DP / 4, AT_ONCE = CH_THREADS / LANES, AHEAD = 4;
+    constexpr uint32_t LANES = DP / 4, AHEAD = 8;
     const uint32_t D = a.c.head_dim, d0 = threadIdx.x % LANES * 4u;
-    const uint32_t parts = a.tile_rows / JOIN_ROWS, part = blockIdx.x % parts, head = blockIdx.x / parts % a.c.heads;
+    const uint32_t parts = a.tile_rows / JOIN_ROWS<DP>, part = blockIdx.x % parts, head = blockIdx.x / parts % a.c.heads;
     chunk_place at;
     if (!chunk_unit<true>(a, blockIdx.x / parts / a.c.heads, &at)) return;
     const chunk_rows t(a, at);
     const uint32_t pieces = max((t.end + at.keys - 1u) / at.keys, 1u);
-    for (uint32_t in = part * JOIN_ROWS + threadIdx.x / LANES; in < (part + 1u) * JOIN_ROWS; in += AT_ONCE) {
-        const uint32_t row = t.row0 + in;
-        if (row >= t.rows) return;
-        float r = -INFINITY, l = 0.0f;
-        dl_f32x4 o = {0, 0, 0, 0};
-        for (uint32_t p0 = 0; p0 < pieces; p0 += AHEAD) {
-            dl_f32x2 rl[AHEAD];
-            dl_f32x4 x[AHEAD];
+    const uint32_t in = part * JOIN_ROWS<DP> + threadIdx.x / LANES, row = t.row0 + in;
+    if (row >= t.rows) return;
+    float r = -INFINITY, l = 0.0f;
+    dl_f32x4 o = {0, 0, 0, 0};
+    for (uint32_t p0 = 0; p0 < pieces; p0 += AHEAD) {
+        dl_f32x2 rl[AHEAD];
+        dl_f32x4 x[AHEAD];
 #pragma unroll
-            for (uint32_t k = 0; k < AHEAD; ++k) {
-                const uint64_t from = ((uint64_t)(at.slot + min(p0 + k, pieces - 1u)) * a.c.heads + head) * a.tile_rows + in;
-                rl[k] = a.rl[from];
-                x[k] = d0 < D ? *(const dl_f32x4 *)(a.partial + from * D + d0) : dl_f32x4{0, 0, 0, 0};
-                if (p0 + k >= pieces) rl[k] = dl_f32x2{-INFINITY, 0.0f}, x[k] = dl_f32x4{0, 0, 0, 0};
-            }
-            float now = r;
-#pragma unroll
-            for (uint32_t k = 0; k < AHEAD; ++k) now = fmaxf(now, rl[k][0]);
-            const float ref = now == -INFINITY ? 0.0f : now, fade = __builtin_amdgcn_exp2f(r - ref);
-            r = now;
-            l *= fade;
-            o *= fade;
-#pragma unroll
-            for (uint32_t k = 0; k < AHEAD; ++k) {
-                const float f = __builtin_amdgcn_exp2f(rl[k][0] - ref);
-                l = fmaf(rl[k][1], f, l);
-                o += x[k] * f;
-            }
+        for (uint32_t k = 0; k < AHEAD; ++k) {
+            const uint64_t from = ((uint64_t)(at.slot + min(p0 + k, pieces - 1u)) * a.c.heads + head) * a.tile_rows + in;
+            rl[k] = a.rl[from];
+            x[k] = d0 < D ? *(const dl_f32x4 *)(a.partial + from * D + d0) : dl_f32x4{0, 0, 0, 0};
+            if (p0 + k >= pieces) rl[k] = dl_f32x2{-INFINITY, 0.0f}, x[k] = dl_f32x4{0, 0, 0, 0};
         }
-        const bool none = l == 0.0f;
-        const uint32_t j = dl_divide(row, a.groups), h = head * a.group + row - j * a.group;
-        const float f = none ? 0.0f : 1.0f / l;
-        if (d0 < D)
-            dl_store_at(a.out + (uint64_t)(t.first + j) * a.out_token + h * a.out_head + 2u * d0,
-                        none ? dl_u32x2{0, 0} : dl_u32x2{Q::pack(o[0] * f, o[1] * f), Q::pack(o[2] * f, o[3] * f)});
-        if (a.lse && d0 == 0)
-            a.lse[(uint64_t)(t.first + j) * a.q_heads + h] = none ? -INFINITY : ((r == -INFINITY ? 0.0f : r) - Q::lift + log2f(l)) * DL_LN2;
+        float now = r;
+#pragma unroll
+        for (uint32_t k = 0; k < AHEAD; ++k) now = fmaxf(now, rl[k][0]);
+        const float ref = now == -INFINITY ? 0.0f : now, fade = __builtin_amdgcn_exp2f(r - ref);
+        r = now;
+        l *= fade;
+        o *= fade;
+#pragma unroll
+        for (uint32_t k = 0; k < AHEAD; ++k) {
+            const float f = __builtin_amdgcn_exp2f(rl[k][0] - ref);
+            l = fmaf(rl[k][1], f, l);
+            o += x[k] * f;
+        }
     }
+    const bool none = l == 0.0f;
+    const uint32_t j = dl_divide(row, a.groups), h = head * a.group + row - j * a.group;
+    const float f = none ? 0.0f : 1.0f / l;
+    if (d0 < D)
+        dl_store_at(a.out + (uint64_t)(t.first + j) * a.out_token + h * a.out_head + 2u * d0,
+                    none ? dl_u32x2{0, 0} : dl_u32x2{Q::pack(o[0] * f, o[1] * f), Q::pack(o[2] * f, o[3] * f)});
+    if (a.lse && d0 == 0)
+        a.lse[(uint64_t)(t.first + j) * a.q_heads + h] = none ? -INFINITY : ((r == -INFINITY ? 0.0f : r) - Q::lift + log2f(l)) * DL_LN2;
 }
 
 struct chunk_shape {
-    uint64_t units;   // at most so many pieces a head, over all sequences
-    uint32_t target;  // 0: nothing is cut
-    uint32_t tile_rows;
+    uint64_t units;     // at most so many pieces a head, over all sequences
+    uint32_t most_cut;  // of them of sequences that are cut
+    uint32_t tile_rows, slots;
 };
 
 int chunk_sizes(const dl_kv_cache *cache, const dl_chunk_attention_args *args, dl_cache_view *view, chunk_shape *sh)
@@ -748,14 +778,17 @@ int chunk_sizes(const dl_kv_cache *cache, const dl_chunk_attention_args *args, d
     uint64_t tiles = rows / sh->tile_rows + (uint64_t)args->batch;
     if (tiles > rows) tiles = rows;
     const uint64_t most = (uint64_t)args->max_pages * (uint32_t)cache->page_tokens;
-    // Workgroups at once, by the registers and LDS: two a compute unit up to head_dim 128, one above.
-    const uint32_t slots = cache->head_dim > 128 || (cache->head_dim > 64 && sh->tile_rows > 32u * CH_WAVES) ? 256u : 512u, round = slots / (uint32_t)cache->heads;
-    if (most > LEAST_STEPS * CH_KEYS && round > 1u) sh->target = round;
-    sh->units = tiles + sh->target;
+    // Workgroups at once, by the registers and LDS: two a compute unit up to head_dim 128 (64 where there are many rows), one above.
+    sh->slots = cache->head_dim > 128 || (cache->head_dim > 64 && sh->tile_rows > 32u * CH_WAVES) ? 256u : 512u;
+    // Two rounds of pieces at most, and no more than a step each.
+    uint64_t cut = 2u * sh->slots / (uint32_t)cache->heads;
+    if (cut > tiles * ((most + CH_KEYS - 1u) / CH_KEYS)) cut = tiles * ((most + CH_KEYS - 1u) / CH_KEYS);
+    if (most > CH_KEYS && cut > 1u) sh->most_cut = (uint32_t)cut;
+    sh->units = tiles + sh->most_cut;
     return DL_OK;
 }
 
-size_t chunk_slots(const chunk_shape &sh, uint32_t heads) { return (size_t)2 * sh.target * heads * sh.tile_rows; }
+size_t chunk_slots(const chunk_shape &sh, uint32_t heads) { return (size_t)sh.most_cut * heads * sh.tile_rows; }
 
 }  // namespace
 
@@ -765,7 +798,7 @@ extern "C" int64_t dl_chunk_attention_workspace(const dl_kv_cache *cache, const 
     chunk_shape sh;
     const int rc = chunk_sizes(cache, args, &view, &sh);
     if (rc != DL_OK) return rc;
-    return (int64_t)(DL_CONTROL_BYTES + chunk_slots(sh, view.heads) * (sizeof(dl_f32x2) + view.head_dim * sizeof(float)));
+    return (int64_t)(DL_CONTROL_BYTES + 16u + chunk_slots(sh, view.heads) * (sizeof(dl_f32x2) + view.head_dim * sizeof(float)));
 }
 
 extern "C" int dl_chunk_attention(const dl_kv_cache *cache, const dl_chunk_attention_args *args, void *stream)
@@ -786,7 +819,8 @@ extern "C" int dl_chunk_attention(const dl_kv_cache *cache, const dl_chunk_atten
     a.q = (const char *)args->q;
     a.out = (char *)args->out;
     a.lse = args->lse;
-    a.rl = (dl_f32x2 *)((char *)args->workspace + DL_CONTROL_BYTES);
+    a.size = (uint32_t *)((char *)args->workspace + DL_CONTROL_BYTES);
+    a.rl = (dl_f32x2 *)(a.size + 4);
     a.partial = (float *)(a.rl + chunk_slots(sh, a.c.heads));
     a.q_token = 2 * args->q_token_stride;
     a.q_head = 2 * args->q_head_stride;
@@ -796,7 +830,8 @@ extern "C" int dl_chunk_attention(const dl_kv_cache *cache, const dl_chunk_atten
     a.group = a.q_heads / a.c.heads;
     a.groups = dl_make_divider(a.group ? a.group : 1u);
     a.tile_rows = sh.tile_rows;
-    a.target = sh.target;
+    a.most_cut = sh.most_cut;
+    a.round = (float)sh.slots / (float)a.c.heads;
     a.scale = args->scale * DL_LOG2E;
     const uint64_t grid = sh.units * a.c.heads;
     if (grid >= (1ull << 32) / CH_THREADS) return DL_ERR_INVALID;
@@ -812,8 +847,8 @@ extern "C" int dl_chunk_attention(const dl_kv_cache *cache, const dl_chunk_atten
                     }
                 hipLaunchKernelGGL((dl_chunk_kernel<decltype(q), decltype(c), DP>), dim3((uint32_t)grid), dim3(CH_THREADS), 0, hs, a);
             });
-            if (sh.target)
-                hipLaunchKernelGGL((dl_chunk_join_kernel<decltype(q), DP>), dim3(sh.target * a.c.heads * (sh.tile_rows / JOIN_ROWS)), dim3(CH_THREADS), 0, hs, a);
+            if (sh.most_cut)
+                hipLaunchKernelGGL((dl_chunk_join_kernel<decltype(q), DP>), dim3((sh.most_cut + 1u) / 2u * a.c.heads * (sh.tile_rows / JOIN_ROWS<DP>)), dim3(CH_THREADS), 0, hs, a);
         };
         if (a.c.head_dim <= 64)
             go(std::integral_constant<int, 64>{});
