@@ -31,11 +31,37 @@ struct norm_args {
 
 constexpr uint32_t NORM_THREADS = 256;
 constexpr int NORM_ELEMENTS = 8;
-// From so many threads on, four rows of a thread are on their way at once and stores go past the caches.
-constexpr uint64_t NORM_MANY_THREADS = 1ull << 20;
+// From so many threads on, two rows of a thread are on their way at once and stores go past the caches; from so many bytes moved on, loads
+// too.  Measured with heads of 128 in 16 bits, one row and plain : two and plain loads : two and streaming loads : four and plain : four and
+// streaming, 20001 tokens of 32 heads (338 MB) 81.6 : 68.5 : 65.4 : 76.4 : 71.9 us, 20001 of 40 (420 MB) 103 : 85.1 : 82.7 : 88.0 : 83.2,
+// 8000 of 32 (135 MB) 29.7 : 26.1 : 28.1 : 26.5 : 31.3; plain stores cost 3.5 more.
+constexpr uint64_t NORM_MANY_THREADS = 1ull << 20, NORM_STREAM_BYTES = 256ull << 20;
 
-// A thread has ROWS heads of one side of one token, which share the token's cosines and sines and the side's weights.
-template <class T, int LANES, int ROWS, bool STREAM>
+// Eight elements of a row.  STREAM: past the caches.
+template <class T, bool STREAM>
+__device__ __forceinline__ void load_eight(const char *p, float (&x)[NORM_ELEMENTS])
+{
+    if constexpr (STREAM && T::size == 2) {
+        typedef dl_u32x4 anywhere __attribute__((aligned(1)));
+        const dl_u32x4 w = __builtin_nontemporal_load((const anywhere *)p);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[2 * j] = T::lo(w[j]), x[2 * j + 1] = T::hi(w[j]);
+    } else if constexpr (STREAM) {
+        typedef dl_f32x4 anywhere __attribute__((aligned(1)));
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const dl_f32x4 w = __builtin_nontemporal_load((const anywhere *)(p + 16 * h));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[4 * h + j] = w[j];
+        }
+    } else {
+        dl_load_row<T>(p, x);
+    }
+}
+
+// A thread has ROWS heads of one side of one token, which share the token's cosines and sines and the side's weights.  MODE: 0 all through the
+// caches, 1 stores past them, 2 both.
+template <class T, int LANES, int ROWS, int MODE>
 __global__ void __launch_bounds__(NORM_THREADS) dl_norm_rotate_kernel(const norm_args a)
 {
     constexpr int N = NORM_ELEMENTS;
@@ -57,7 +83,7 @@ __global__ void __launch_bounds__(NORM_THREADS) dl_norm_rotate_kernel(const norm
     for (int r = 0; r < ROWS; ++r) {
 #pragma unroll
         for (int i = 0; i < N; ++i) x[r][i] = 0.0f;
-        if (mine) dl_load_row<T>(s.x + token * s.token + min(h0 + r, s.heads - 1u) * s.head + (size_t)at * T::size, x[r]);
+        if (mine) load_eight<T, MODE == 2>(s.x + token * s.token + min(h0 + r, s.heads - 1u) * s.head + (size_t)at * T::size, x[r]);
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) w[i] = 1.0f, c[i] = 1.0f, z[i] = 0.0f;
@@ -106,7 +132,7 @@ __global__ void __launch_bounds__(NORM_THREADS) dl_norm_rotate_kernel(const norm
                 for (int i = 0; i < N; ++i) x[r][i] = fmaf(x[r][i], c[i], y[i] * z[i]);
             }
         }
-        if (live && h0 + r < s.heads) dl_store_row<T, STREAM>(s.y + token * s.out_token + (h0 + r) * s.out_head + (size_t)at * T::size, x[r]);
+        if (live && h0 + r < s.heads) dl_store_row<T, MODE != 0>(s.y + token * s.out_token + (h0 + r) * s.out_head + (size_t)at * T::size, x[r]);
     }
 }
 
@@ -159,25 +185,26 @@ extern "C" int dl_norm_rotate(const dl_norm_rotate_args *args, void *stream)
     dl_with_type(args->type, [&](auto t) {
         dl_with_lanes<NORM_ELEMENTS>(a.head_dim, [&](auto lanes) {
             constexpr int L = decltype(lanes)::value;
-            auto go = [&](auto rows, auto stream_stores) {
+            auto go = [&](auto rows, auto mode) {
                 constexpr int ROWS = decltype(rows)::value;
                 a.q_parts = (a.q.heads + ROWS - 1u) / ROWS;
                 const uint32_t parts = a.q_parts + (a.k.heads + ROWS - 1u) / ROWS;
                 a.parts = dl_make_divider(parts);
                 a.tasks = (uint32_t)args->tokens * parts;
-                hipLaunchKernelGGL((dl_norm_rotate_kernel<decltype(t), L, ROWS, decltype(stream_stores)::value>),
+                hipLaunchKernelGGL((dl_norm_rotate_kernel<decltype(t), L, ROWS, decltype(mode)::value>),
                                    dim3((a.tasks + NORM_THREADS / L - 1u) / (NORM_THREADS / L)), dim3(NORM_THREADS), 0, (hipStream_t)stream, a);
             };
-            // (heads of a side that do not fill a thread's rows cost it as much as if they were there)
-            auto filled = [&](uint32_t rows) { return 5u * (a.q.heads + a.k.heads) >= 4u * rows * ((a.q.heads + rows - 1u) / rows + (a.k.heads + rows - 1u) / rows); };
-            if ((uint64_t)args->tokens * (a.q.heads + a.k.heads) * L < NORM_MANY_THREADS)
-                go(std::integral_constant<int, 1>{}, std::false_type{});
-            else if (filled(4))
-                go(std::integral_constant<int, 4>{}, std::true_type{});
-            else if (filled(2))
-                go(std::integral_constant<int, 2>{}, std::true_type{});
+            const uint64_t rows = (uint64_t)args->tokens * (a.q.heads + a.k.heads);
+            // (a single head of a side, and the last of an odd number, cost a thread as much as two)
+            const bool paired = (a.q.heads + 1u) / 2u + (a.k.heads + 1u) / 2u <= (a.q.heads + a.k.heads) * 5u / 8u;
+            if (rows * L < NORM_MANY_THREADS)
+                go(std::integral_constant<int, 1>{}, std::integral_constant<int, 0>{});
+            else if (!paired)
+                go(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{});
+            else if (2u * rows * a.head_dim * decltype(t)::size < NORM_STREAM_BYTES)
+                go(std::integral_constant<int, 2>{}, std::integral_constant<int, 1>{});
             else
-                go(std::integral_constant<int, 1>{}, std::true_type{});
+                go(std::integral_constant<int, 2>{}, std::integral_constant<int, 2>{});
         });
     });
     DL_HIP(hipGetLastError());
