@@ -31,6 +31,7 @@ struct chunk_args {
     dl_divider groups;  // by group
     uint32_t tile_rows;           // 32 or 64 a wavefront
     uint32_t most_cut;            // 0: nothing is cut
+    bool search;                  // see chunk_unit
     float round;                  // workgroups at once, by the heads
     uint32_t *size;               // what the pieces' size has come to, for the join
     float scale;         // times log2 e
@@ -41,8 +42,8 @@ struct chunk_args {
 // it.  What leaves something behind for the join are the pieces of sequences that are cut: no more than `most_cut` over all of them, and so
 // no more than half as many tiles.
 // Which size: a round of workgroups takes as long as the steps of one and START more, a piece costs the join JOIN steps; a lane of a
-// wavefront looks at the size that cuts the longest sequence into its number + 1 pieces.  Batches of more than SEARCH_MAX sequences are not
-// looked at one by one: with T steps of all tiles, T / (most_cut / 2), so that those that are cut have at most twice as many pieces.
+// wavefront looks at the size that cuts the longest sequence into its number + 1 pieces.  Batches of more than SEARCH_MAX sequences, and tables
+// with room for more than 2^20 steps, are not looked at one by one: with T steps of all tiles, T / (most_cut / 2), so that those that are cut have at most twice as many pieces.
 // Every wavefront works this out from the lengths for itself.
 constexpr float START = 3.0f, JOIN = 0.1f;
 constexpr uint32_t SEARCH_MAX = 16;
@@ -72,11 +73,11 @@ __device__ __forceinline__ bool chunk_unit(const chunk_args &a, uint32_t unit, c
     if (at_once) look(0);
     if (CUT) {
         size = max(*a.size, 1u);
-    } else if (a.most_cut && a.p.batch <= SEARCH_MAX) {
+    } else if (a.search) {
         uint32_t longest = 1;
         auto of = [&](uint32_t x, uint32_t b) { return (uint32_t)__builtin_amdgcn_readlane((int)x, (int)b); };
         for (uint32_t b = 0; b < a.p.batch; ++b) longest = of(tiles, b) ? max(longest, of(steps, b)) : longest;
-        // (whole numbers far below 2^24: with half a unit in front of the quotient its rounding makes no difference)
+        // (whole numbers up to 2^20: with half a unit in front of the quotient its rounding makes no difference)
         const float mine = ceilf(((float)longest - 0.5f) * __builtin_amdgcn_rcpf((float)(lane + 1u))), over = __builtin_amdgcn_rcpf(mine);
         float units = 0.0f, cut = 0.0f, most = 1.0f;
         for (uint32_t b = 0; b < a.p.batch; ++b) {
@@ -764,6 +765,7 @@ struct chunk_shape {
     uint64_t units;     // at most so many pieces a head, over all sequences
     uint32_t most_cut;  // of them of sequences that are cut
     uint32_t tile_rows, slots;
+    bool search;
 };
 
 int chunk_sizes(const dl_kv_cache *cache, const dl_chunk_attention_args *args, dl_cache_view *view, chunk_shape *sh)
@@ -784,6 +786,7 @@ int chunk_sizes(const dl_kv_cache *cache, const dl_chunk_attention_args *args, d
     uint64_t cut = 2u * sh->slots / (uint32_t)cache->heads;
     if (cut > tiles * ((most + CH_KEYS - 1u) / CH_KEYS)) cut = tiles * ((most + CH_KEYS - 1u) / CH_KEYS);
     if (most > CH_KEYS && cut > 1u) sh->most_cut = (uint32_t)cut;
+    sh->search = sh->most_cut && args->batch <= (int32_t)SEARCH_MAX && most <= (uint64_t)CH_KEYS << 20;
     sh->units = tiles + sh->most_cut;
     return DL_OK;
 }
@@ -831,6 +834,7 @@ extern "C" int dl_chunk_attention(const dl_kv_cache *cache, const dl_chunk_atten
     a.groups = dl_make_divider(a.group ? a.group : 1u);
     a.tile_rows = sh.tile_rows;
     a.most_cut = sh.most_cut;
+    a.search = sh.search;
     a.round = (float)sh.slots / (float)a.c.heads;
     a.scale = args->scale * DL_LOG2E;
     const uint64_t grid = sh.units * a.c.heads;

@@ -65,7 +65,7 @@ template <class T, int LANES, int ROWS, int MODE>
 __global__ void __launch_bounds__(NORM_THREADS) dl_norm_rotate_kernel(const norm_args a)
 {
     constexpr int N = NORM_ELEMENTS;
-    const uint32_t lane = threadIdx.x % LANES, task = blockIdx.x * (NORM_THREADS / LANES) + threadIdx.x / LANES;
+    const uint32_t lane = threadIdx.x % LANES, task = (blockIdx.y * gridDim.x + blockIdx.x) * (NORM_THREADS / LANES) + threadIdx.x / LANES;
     const uint32_t at = lane * (uint32_t)N, half = a.rotary / 2u;
     const bool mine = at < a.head_dim, turned = at < a.rotary;
     // which pairs: of the lane's elements as first or second of theirs, or its own neighbours
@@ -191,8 +191,10 @@ extern "C" int dl_norm_rotate(const dl_norm_rotate_args *args, void *stream)
                 const uint32_t parts = a.q_parts + (a.k.heads + ROWS - 1u) / ROWS;
                 a.parts = dl_make_divider(parts);
                 a.tasks = (uint32_t)args->tokens * parts;
-                hipLaunchKernelGGL((dl_norm_rotate_kernel<decltype(t), L, ROWS, decltype(mode)::value>),
-                                   dim3((a.tasks + NORM_THREADS / L - 1u) / (NORM_THREADS / L)), dim3(NORM_THREADS), 0, (hipStream_t)stream, a);
+                // (rows of 256 elements may be one workgroup more than a grid is wide, 2^32 threads)
+                const uint32_t blocks = (a.tasks + NORM_THREADS / L - 1u) / (NORM_THREADS / L), high = (blocks + (1u << 23) - 1u) >> 23;
+                hipLaunchKernelGGL((dl_norm_rotate_kernel<decltype(t), L, ROWS, decltype(mode)::value>), dim3((blocks + high - 1u) / high, high),
+                                   dim3(NORM_THREADS), 0, (hipStream_t)stream, a);
             };
             const uint64_t rows = (uint64_t)args->tokens * (a.q.heads + a.k.heads);
             // (a single head of a side, and the last of an odd number, cost a thread as much as two)

@@ -122,6 +122,48 @@ def test_two_rows_a_thread():
             assert torch.equal(again[0], outs[0][part]) and torch.equal(again[1], outs[1][part])
 
 
+def test_past_the_caches():
+    """From 256 MiB moved on: the same bits as in parts that stay in them."""
+    for dtype, neighbours in ((torch.bfloat16, False), (torch.float32, True)):
+        rng = np.random.default_rng(2)
+        T, dim = (280_001, 80) if dtype == torch.bfloat16 else (140_001, 80)
+        g = torch.Generator(device="cuda").manual_seed(1)
+        q, k = (torch.randn((T, h, dim), device="cuda", generator=g).to(dtype) for h in (2, 1))
+        assert 2 * T * 3 * dim * q.element_size() >= 256 << 20
+        w = 1 + 0.1 * torch.randn(dim, device="cuda", generator=g)
+        table, positions = table_of(500, 48, rng), torch.randint(-1, 501, (T,), device="cuda", generator=g)
+        outs = torch.full_like(q, 7.0), torch.full_like(k, 7.0)
+        run_it = lambda a, b, c, d, p: dl.dl_norm_rotate(  # noqa: E731
+            dl.NormRotate(a, b, c, d, q_weight=w, k_weight=w, table=table, positions=p, neighbours=neighbours), torch.cuda.current_stream())
+        run_it(q, k, *outs, positions)
+        for t0 in range(0, T, 30_000):
+            part = slice(t0, min(T, t0 + 30_000))
+            again = torch.full_like(q[part], 7.0), torch.full_like(k[part], 7.0)
+            run_it(q[part], k[part], *again, positions[part].contiguous())
+            assert torch.equal(again[0], outs[0][part]) and torch.equal(again[1], outs[1][part])
+
+
+def test_captured_and_replayed():
+    """Positions are read when the kernel runs; on a stream of its own."""
+    rng = np.random.default_rng(5)
+    q = torch.randn((7, 3, 64), device="cuda").half()
+    out, positions = torch.full_like(q, 7.0), torch.zeros(7, dtype=torch.int64, device="cuda")
+    r = dl.NormRotate(q, None, out, q_weight=torch.ones(64, device="cuda"), table=table_of(30, 64, rng), positions=positions)
+    graph = torch.cuda.CUDAGraph()
+    stream = torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=stream):
+        dl.dl_norm_rotate(r, stream)
+    for n in range(4):
+        positions.copy_(torch.randint(0, 30, (7,)))
+        out.fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        dl.dl_norm_rotate(r, torch.cuda.current_stream())
+        torch.cuda.synchronize()
+        assert torch.equal(got, out) and not (got == 7).all()
+
+
 def test_a_row_of_zeros_and_one_that_is_not_finite():
     q = torch.randn((4, 1, 64), device="cuda")
     q[0] = 0
