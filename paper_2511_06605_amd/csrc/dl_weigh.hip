@@ -46,14 +46,10 @@ __device__ __forceinline__ float over_lanes(float (&x)[16], uint32_t i)
 
 // A tile's scores s: rows are keys (8 (e / 4) + 4 half + e % 4, with the scales ks), columns queries.  lse in units of ln 2; masked: keys from
 // `seen` + 1 on are not seen by the lane's query.
-__device__ __forceinline__ void add_weights(dl_f32x16 &s, const float *ks, float lse, bool masked, int32_t seen, uint32_t half, float (&sum)[16])
+__device__ __forceinline__ void add_weights(dl_f32x16 &s, const dl_f32x4 (&ks)[4], float lse, bool masked, int32_t seen, uint32_t half, float (&sum)[16])
 {
 #pragma unroll
-    for (int e = 0; e < 16; e += 4) {
-        const dl_f32x4 k = *(const dl_f32x4 *)&ks[2u * e + 4u * half];
-#pragma unroll
-        for (int f = 0; f < 4; ++f) s[e + f] = fmaf(s[e + f], k[f], -lse);
-    }
+    for (int e = 0; e < 16; ++e) s[e] = fmaf(s[e], ks[e / 4][e % 4], -lse);
     if (masked) {
 #pragma unroll
         for (int e = 0; e < 16; ++e)
@@ -152,7 +148,10 @@ __global__ void __launch_bounds__(64 * FEW_WAVES, DP <= 128 ? 4 : 2) dl_weigh_fe
                 }
                 // the next rows are on their way while this one's weights are taken
                 if (r0 + 32u < rows) load_queries(r0 + 32u);
-                add_weights(s, sums[wave], lse, r0 < whole, seen, half, sum);
+                dl_f32x4 ks[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) ks[e] = *(const dl_f32x4 *)&sums[wave][8u * e + 4u * half];
+                add_weights(s, ks, lse, r0 < whole, seen, half, sum);
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
@@ -171,16 +170,16 @@ __global__ void __launch_bounds__(64 * FEW_WAVES, DP <= 128 ? 4 : 2) dl_weigh_fe
 }
 
 // Many queries: a workgroup's wavefronts have keys of their own and take the same rows of the same head at a time, which go through LDS once for
-// all of them: in registers a lane would load a row's pieces, and every load touch as many lines as there are rows.  Rows lie in 16-byte
-// pieces whose places are exchanged by an exclusive or with the row's number; while a tile of 32 rows is worked on, the next one is on its
-// way, and so are the keys of the next head from the first tile of this one on.
+// all of them: in registers a lane would load a row's pieces, and every load touch as many lines as there are rows.  Rows lie 16 bytes apart,
+// so that eight neighbouring lanes, a row each, use all banks; while a tile of 32 rows is worked on, the next one is on its way.  What a product needs from LDS is asked for two products before.
 constexpr uint32_t MANY_THREADS = 512, MANY_KEYS = 32 * MANY_THREADS / 64;
 constexpr uint32_t MANY_BLOCKS = 2048;  // heads are shared out up to so many workgroups
 template <class Q, class C, int DP>
 __global__ void __launch_bounds__(MANY_THREADS, DP <= 128 ? 4 : 2) dl_weigh_many_kernel(const weigh_args a)
 {
     constexpr uint32_t PAIRS = DP / 32, PIECES = DP / 8, LOADS = (32 * PIECES + MANY_THREADS - 1) / MANY_THREADS;
-    __shared__ __align__(16) uint32_t tiles[2][32 * PIECES * 4];
+    constexpr uint32_t ROW = PIECES * 4 + 4;
+    __shared__ __align__(16) uint32_t tiles[2][32 * ROW];
     __shared__ float lses[2][32];
     __shared__ __align__(16) float scales[MANY_THREADS / 64][32];
     const uint32_t lane = threadIdx.x % 64u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
@@ -212,33 +211,28 @@ __global__ void __launch_bounds__(MANY_THREADS, DP <= 128 ? 4 : 2) dl_weigh_many
             }
             if (threadIdx.x < 32u) {
                 const uint32_t row = min(r0 + i, rows - 1u), j = dl_divide(row, a.groups);
-                const float given = a.lse[(uint64_t)(first + j) * a.q_heads + head * a.group + row - j * a.group];
-                staged_lse = r0 + i < rows && fabsf(given) < INFINITY ? given * DL_LOG2E : INFINITY;
+                staged_lse = r0 + i < rows ? a.lse[(uint64_t)(first + j) * a.q_heads + head * a.group + row - j * a.group] : INFINITY;
             }
         };
         auto put = [&](uint32_t to) {
 #pragma unroll
             for (uint32_t x = 0; x < LOADS; ++x) {
                 const uint32_t n = threadIdx.x + x * MANY_THREADS, row = n / PIECES, piece = n % PIECES;
-                if (32u * PIECES % MANY_THREADS == 0 || n < 32u * PIECES) *(dl_u32x4 *)&tiles[to][(row * PIECES + (piece ^ (row & 7u))) * 4u] = staged[x];
+                if (32u * PIECES % MANY_THREADS == 0 || n < 32u * PIECES) *(dl_u32x4 *)&tiles[to][row * ROW + piece * 4u] = staged[x];
             }
-            if (threadIdx.x < 32u) lses[to][i] = staged_lse;
-        };
-        dl_words<16> codes[PAIRS];
-        float scale = 0.0f;
-        auto load_keys = [&](uint32_t head) {
-#pragma unroll
-            for (uint32_t x = 0; x < PAIRS; ++x) codes[x] = dl_load_words<16>(key.codes + head * a.c.head_stride + min(16u * (2u * x + half), D - 16u));
-            scale = *(const float *)(key.scale + head * a.c.scale_head_stride);
+            if (threadIdx.x < 32u) lses[to][i] = fabsf(staged_lse) < INFINITY ? staged_lse * DL_LOG2E : INFINITY;
         };
         dl_u32x4 kf[2 * PAIRS];
-        load_keys(head0);
         stage(head0, row0);
         put(0);
         __syncthreads();
         uint32_t now = 0;
 #pragma unroll 1
         for (uint32_t head = head0; head < heads_end; ++head) {
+            dl_words<16> codes[PAIRS];
+#pragma unroll
+            for (uint32_t x = 0; x < PAIRS; ++x) codes[x] = dl_load_words<16>(key.codes + head * a.c.head_stride + min(16u * (2u * x + half), D - 16u));
+            const float scale = *(const float *)(key.scale + head * a.c.scale_head_stride);
 #pragma unroll
             for (uint32_t x = 0; x < 2 * PAIRS; ++x) {
                 const dl_u32x2 lo = C::template spread<Q>(codes[x / 2].w[2 * (x % 2)]), hi = C::template spread<Q>(codes[x / 2].w[2 * (x % 2) + 1]);
@@ -248,7 +242,6 @@ __global__ void __launch_bounds__(MANY_THREADS, DP <= 128 ? 4 : 2) dl_weigh_many
             if (half == 0) scales[wave][i] = key.alive ? scale * a.scale : 0.0f;
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
-            if (head + 1u < heads_end) load_keys(head + 1u);
 #pragma unroll 1
             for (uint32_t r0 = row0; r0 < rows; r0 += 32u, now ^= 1u) {
                 const bool same_head = r0 + 32u < rows, more = same_head || head + 1u < heads_end;
@@ -257,14 +250,22 @@ __global__ void __launch_bounds__(MANY_THREADS, DP <= 128 ? 4 : 2) dl_weigh_many
                     dl_f32x16 s;
 #pragma unroll
                     for (int e = 0; e < 16; ++e) s[e] = 0.0f;
+                    auto operand = [&](uint32_t x) { return *(const dl_u32x4 *)&tiles[now][i * ROW + (2u * (2u * (x / 2) + half) + x % 2u) * 4u]; };
+                    dl_u32x4 ring[3];
+#pragma unroll
+                    for (uint32_t x = 0; x < 2; ++x) ring[x] = operand(x);
+                    const float lse = lses[now][i];
+                    dl_f32x4 ks[4];
 #pragma unroll
                     for (uint32_t x = 0; x < 2 * PAIRS; ++x) {
-                        const uint32_t piece = 2u * (2u * (x / 2) + half) + x % 2u;
-                        s = Q::mfma32(kf[x], *(const dl_u32x4 *)&tiles[now][(i * PIECES + (piece ^ (i & 7u))) * 4u], s);
+                        if (x + 2 < 2 * PAIRS) ring[(x + 2) % 3] = operand(x + 2);
+                        if (x + 4 >= 2 * PAIRS) ks[x + 4 - 2 * PAIRS] = *(const dl_f32x4 *)&scales[wave][8u * (x + 4 - 2 * PAIRS) + 4u * half];
+                        s = Q::mfma32(kf[x], ring[x % 3], s);
+                        __builtin_amdgcn_sched_barrier(0);
                     }
                     const bool masked = r0 < whole;
                     const int32_t seen = masked ? ahead + (int32_t)dl_divide(r0 + i, a.groups) - (int32_t)base : 0;
-                    add_weights(s, scales[wave], lses[now][i], masked, seen, half, sum);
+                    add_weights(s, ks, lse, masked, seen, half, sum);
                 }
                 if (more) put(now ^ 1u);
                 __syncthreads();
