@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(64 * FEW_WAVES, DP <= 128 ? 4 : 2) dl_weigh_fe
 // all of them: in registers a lane would load a row's pieces, and every load touch as many lines as there are rows.  Rows lie 16 bytes apart,
 // so that eight neighbouring lanes, a row each, use all banks; while a tile of 32 rows is worked on, the next one is on its way.  What a product needs from LDS is asked for two products before.
 constexpr uint32_t MANY_THREADS = 512, MANY_KEYS = 32 * MANY_THREADS / 64;
-constexpr uint32_t MANY_BLOCKS = 2048;  // heads are shared out up to so many workgroups
+constexpr uint32_t MANY_BLOCKS = 1024;  // heads are shared out up to so many workgroups
 template <class Q, class C, int DP>
 __global__ void __launch_bounds__(MANY_THREADS, DP <= 128 ? 4 : 2) dl_weigh_many_kernel(const weigh_args a)
 {
