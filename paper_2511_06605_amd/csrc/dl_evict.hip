@@ -15,6 +15,10 @@ constexpr uint32_t DIGIT_BITS = 8, DIGITS = 1u << DIGIT_BITS;
 // Counts of a digit that lanes take in turn: weights share their upper bits, and counts at one address wait for each other.
 constexpr uint32_t COPIES = 16;
 constexpr uint32_t MOVE_THREADS = 256;
+// From so many bytes of codes on, stores go past the caches; less stays there, for the attention that follows.  Two rows a thread.  Measured, the
+// whole call, one row and plain : two and plain : two and streaming stores : two, loads as well : four and streaming, buffers in turn that no cache
+// holds: 139 MB read and written 57.4 : 53.5 : 48.5 : 49.7 : 50.9 us, 132 MB in 8 sequences 51.0 : 47.3 : 42.2 : 43.6 : 44.5; 4 MB 13.3 - 14.8 all.
+constexpr uint64_t MOVE_STREAM_BYTES = 32ull << 20;
 
 struct evict_args {
     dl_cache_view c;
@@ -189,7 +193,7 @@ __global__ void __launch_bounds__(PICK_THREADS) dl_evict_pick_kernel(const evict
 }
 
 // blockIdx.y: 0 keys, 1 values.  The first head's keys take a token's weight along.
-template <int ROWS>
+template <int ROWS, bool STREAM>
 __global__ void __launch_bounds__(MOVE_THREADS) dl_evict_move_kernel(const evict_args a)
 {
     const uint32_t lane = threadIdx.x & (a.lanes - 1u), per = MOVE_THREADS / a.lanes;
@@ -238,7 +242,7 @@ __global__ void __launch_bounds__(MOVE_THREADS) dl_evict_move_kernel(const evict
 #pragma unroll
     for (int r = 0; r < ROWS; ++r)
         if (page[r] < a.c.pages && to_page[r] < a.c.pages) {
-            if (mine) dl_store_at(codes + (uint64_t)to_page[r] * a.c.page_stride + (uint64_t)to_in[r] * a.c.token_stride + head[r] * a.c.head_stride + 16u * lane, w[r]);
+            if (mine) dl_put<STREAM>(codes + (uint64_t)to_page[r] * a.c.page_stride + (uint64_t)to_in[r] * a.c.token_stride + head[r] * a.c.head_stride + 16u * lane, w[r]);
             if (lane == 0)
                 *(float *)(scales + (uint64_t)to_page[r] * a.c.scale_page_stride + (uint64_t)to_in[r] * a.c.scale_token_stride + head[r] * a.c.scale_head_stride) = scale[r];
         }
@@ -303,7 +307,9 @@ extern "C" int dl_kv_evict(const dl_kv_cache *cache, const dl_kv_evict_args *arg
     if (a.rows) {
         constexpr int ROWS = 2;
         const uint32_t per = MOVE_THREADS / a.lanes * ROWS;
-        hipLaunchKernelGGL((dl_evict_move_kernel<ROWS>), dim3((a.rows + per - 1u) / per, 2), dim3(MOVE_THREADS), 0, (hipStream_t)stream, a);
+        dl_with_bool(2ull * a.rows * a.c.head_dim >= MOVE_STREAM_BYTES, [&](auto streaming) {
+            hipLaunchKernelGGL((dl_evict_move_kernel<ROWS, decltype(streaming)::value>), dim3((a.rows + per - 1u) / per, 2), dim3(MOVE_THREADS), 0, (hipStream_t)stream, a);
+        });
     }
     DL_HIP(hipGetLastError());
     t_dl_last.mode = DL_MODE_ONESHOT;

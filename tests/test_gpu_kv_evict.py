@@ -101,6 +101,12 @@ def test_long_sequences(workspace, n, keep):
     check(workspace, [n, n // 3], keep, first=4, recent=64, heads=1, dim=16)
 
 
+def test_moves_past_the_caches(workspace):
+    """32 MiB of codes and more."""
+    assert 2 * 9000 * 8 * 240 >= 32 << 20
+    check(workspace, [9500], 9000, first=1, recent=30, heads=8, dim=240, kind="int8")
+
+
 def test_equal_weights(workspace):
     rng = np.random.default_rng(0)
     for values in ([1.0], [0.0, -0.0], [0.0, 1.0], [2.0, 2.0 + 2.0 ** -22], [1e-40, 0.0, -1e-40]):
