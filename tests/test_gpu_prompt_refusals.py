@@ -95,6 +95,16 @@ def test_evict(field, value):
     assert (r._tensors[4] == 7).all() and (r._tensors[5] == 7).all()
 
 
+def test_evict_into_what_it_reads():
+    r = evict()
+    r.desc.kept_lens = r.desc.lens
+    refused(dl.dl_kv_evict, r)
+    r = evict()
+    r.desc.kept_weights = r.desc.weights
+    refused(dl.dl_kv_evict, r)
+    assert (r._tensors[4] == 7).all() and (r._tensors[5] == 7).all()
+
+
 def test_null_structs_and_caches_without_codes():
     L, s = dl.binding.lib(), torch.cuda.current_stream().cuda_stream
     assert L.dl_norm_rotate(None, s) == dl.DL_ERR_INVALID
