@@ -4,10 +4,18 @@
 // w = 2^(s + log2 c - r) <= 2^(8 + lift), O += w d V, l += w / c, with a reference r that follows the largest s + log2 c.
 //
 // The queries that share a head of the cache are the rows of a sequence: row j * group + g is query j in the g-th of those heads.  A
-// workgroup has a tile of 128 rows (32 a wavefront) and walks the keys that its last row sees in steps of 64, which its wavefronts share:
-// codes are turned into elements of Q once, on their way into LDS, keys as rows and values transposed, so that every operand of the
-// 32 x 32 x 16 products is one 16-byte read.  While a step is worked on, the next one's codes are on their way to registers and the pages
-// of the one after it are looked up.  Masks cost something only where a wavefront's rows end.
+// workgroup has a tile of rows and walks the keys that its last row sees in steps of 64, which its wavefronts share: codes are turned into
+// elements of Q once, on their way into LDS, keys as rows and values transposed (by byte permutes while they are bytes), so that every
+// operand of the 32 x 32 x 16 products is one 16-byte read.  While a step is worked on, the next one's codes are on their way to registers
+// and the pages of the one after it are looked up.  Masks cost something only where a wavefront's rows end.  128 rows a tile, two workgroups
+// a compute unit; 256 from 1024 rows a sequence on and up to head_dim 128 (dl_chunk_wide_kernel).  Where there are few tiles their keys are
+// cut into pieces, which a second launch joins (chunk_unit).
+//
+// Measured (8 heads of 128, 32 query heads, bfloat16 on fp8, unless said otherwise): 2048 queries behind 30 720 tokens 1100 - 1128 us, 1065 GFLOP,
+// 0.94 - 0.97 PFLOP/s where a large matrix product reaches 1.34 (128 rows a tile: 1319); a prompt of 8192 617 - 627 us, 0.88 - 0.89; three
+// documents with up to 512 queries on up to 16 400 (4 heads, 28 query heads, float16 on int8) 217 - 234 us, 0.6, 18 of it the join; 16 queries
+// behind 500 13.3 us, 5 sequences of up to 101 behind up to 777 (12 heads of 64) 18 us, both two launches.  A workgroup of the former is at work
+// for 6 us: 1.4 until it knows its piece, 0.6 until it knows its pages, 1.1 for the codes, 1.7 for the step, 0.9 for what it leaves; one of the join 2.5.
 #include "dl_codes.h"
 #include "dl_internal.h"
 #include "dl_packed.h"
@@ -482,6 +490,12 @@ __global__ void __launch_bounds__(CH_THREADS, DP <= 128 ? 2 : 1) dl_chunk_kernel
 // 256 rows.  What a second wavefront would overlap is interleaved here: while the scores of 32 keys become weights, the products of the next
 // 32 keys are under way, and while those weights meet the values, the next scores are scaled and the next step's codes go to LDS.  Three
 // tiles in LDS: one that is worked on, the next one, and the one that is filled while somebody may still be at the first; a barrier a step.
+//
+// What bounds it is the issue of instructions: a lone wavefront issues one in about 7 cycles (two of them one in 3.5), and a step of 64 keys is
+// about 630 of them (450 vector ones, 64 products, 75 for LDS), 4400 of the 5060 cycles that it takes (counted over 2048 queries on 30 720 tokens),
+// 2050 of which the matrix units work.  So what counts is their number: operands in padded rows, whose addresses differ by constants, instead of
+// places exchanged by an exclusive or 1230 -> 1127 us.  The same code with 32 rows a wavefront and eight of them, two a SIMD: 1317 (twice the reads
+// from LDS); operands a step further ahead and all scales a part ahead: 1160.
 template <int DP>
 struct wide_lds {
     chunk_tile<DP> tiles[3];
@@ -556,8 +570,8 @@ __global__ void __launch_bounds__(CH_THREADS, DP <= 64 ? 2 : 1) dl_chunk_wide_ke
         }
     };
     // The loop's two parts, in STEPS steps of two products each.  What a step does beside its products is a share of the other work, and what it
-    // reads from LDS has been asked for two steps before (operands, in a ring of four) or one (scales), across the parts' borders; the steps'
-    // order is the compiler's no more.
+    // reads from LDS has been asked for two steps before (operands, in a ring of four) or one (scales), across the parts' borders.  The steps'
+    // order is kept (left to the compiler, all weights come first and the products behind them).
     constexpr uint32_t STEPS = DP / 16;
     dl_u32x4 pf[2][2], ring[4];
     dl_f32x16 s[2];
@@ -776,6 +790,9 @@ int chunk_sizes(const dl_kv_cache *cache, const dl_chunk_attention_args *args, d
     if (!args->tokens || !args->q_heads || !args->batch) return DL_OK;
     const uint64_t rows = (uint64_t)args->tokens * (uint32_t)(args->q_heads / cache->heads);
     // every sequence begins a tile of its own
+    // 256 rows a tile from 1024 rows a sequence on.  256 : 128, us, 8 heads of 128, 32 query heads: on 30 720 tokens 256 queries (1024 rows) 167 : 190, 512
+    // 305 : 351; 8 sequences on 4000 with up to 128, 192, 256, 384 queries 89 : 86, 100 : 108, 140 : 147, 173 : 191; 8 prompts of up to 256 and 512 with nothing
+    // before them 30 : 26 and 49 : 42.  So where contexts are short 128 would be better for longer, which the host does not know.
     sh->tile_rows = cache->head_dim <= 128 && rows >= 1024u * (uint64_t)args->batch ? 64u * CH_WAVES : 32u * CH_WAVES;
     uint64_t tiles = rows / sh->tile_rows + (uint64_t)args->batch;
     if (tiles > rows) tiles = rows;

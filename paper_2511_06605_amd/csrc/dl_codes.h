@@ -282,6 +282,7 @@ static inline void dl_with_bool(bool b, F f)
     else
         f(std::false_type{});
 }
+
 // Calls f with the types that belong to a dl_kv_format / to a 16-bit dl_type.
 template <class F>
 static inline void dl_with_format(int32_t format, F f)
