@@ -228,31 +228,3 @@ def test_as_dl_prefix_attention_has_it(workspace):
         # each weight and each output rounded once on either side
         assert (other.flatten(0, 1).float() - out.float()).abs().max() <= 4 * unit * out.float().abs().max()
         assert (other_lse.flatten(0, 1) - lse).abs().max() <= 2.0 ** -15 * (1 + lse.abs().max())
-
-
-def test_captured_and_replayed_as_lengths_grow(workspace):
-    p = Packed([(8, 200), (3, 90)], heads=2, group=2, spare=3)
-    for b in range(2):  # (pages for what is to come)
-        used = -(-p.sizes[b][1] // 16)
-        p.table[b, used:] = p.table[b, 0]
-    starts, pages, lens = p.plan()
-    lens.fill_(5)
-    r = request(p, workspace, plan=(starts, pages, lens))
-    stream = torch.cuda.Stream()
-    stream.wait_stream(torch.cuda.current_stream())
-    with torch.cuda.stream(stream):
-        dl.dl_chunk_attention(r, stream)
-    torch.cuda.current_stream().wait_stream(stream)
-    graph = torch.cuda.CUDAGraph()
-    with torch.cuda.graph(graph):
-        dl.dl_chunk_attention(r, torch.cuda.current_stream())
-    for a, b in ((8, 3), (100, 50), (200, 90), (150, 0), (200, 90)):
-        lens.copy_(torch.tensor([a, b], dtype=torch.int32))
-        p.out.fill_(7)
-        graph.replay()
-        torch.cuda.synchronize()
-        got, got_lse = p.out.clone(), p.lse.clone()
-        dl.dl_chunk_attention(r, torch.cuda.current_stream())
-        torch.cuda.synchronize()
-        assert torch.equal(got, p.out) and torch.equal(got_lse, p.lse)
-    p.check_attention(p.out, p.lse)

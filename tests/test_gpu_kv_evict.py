@@ -160,25 +160,3 @@ def test_lengths_beyond_the_table(workspace):
     dl.dl_kv_evict(r, torch.cuda.current_stream())
     assert lens.tolist() == [10, 0] and kept[1].tolist() == [-1] * 10
     assert kept[0].tolist() == prompt_ref.evicted(weights[0].cpu().numpy(), 48, 10, 0, 0)
-
-
-def test_captured_and_replayed(workspace):
-    p = Packed([(0, 300), (0, 90)], more_pages=8)
-    weights = torch.rand((2, p.table.shape[1] * 16), device="cuda")
-    kept, kept_lens = torch.zeros((2, 50), dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
-    lens = torch.zeros(2, dtype=torch.int32, device="cuda")
-    r = dl.KvEvict(p.cache(), weights, p.put(p.table), lens, p.put(p.free[:8].reshape(2, 4)), kept, kept_lens, first=3, recent=7)
-    r.use_workspace(workspace)
-    graph = torch.cuda.CUDAGraph()
-    with torch.cuda.graph(graph):
-        dl.dl_kv_evict(r, torch.cuda.current_stream())
-    for a, b in ((300, 90), (20, 51), (0, 50), (299, 89)):
-        lens.copy_(torch.tensor([a, b], dtype=torch.int32))
-        weights.uniform_()
-        kept.fill_(7)
-        graph.replay()
-        torch.cuda.synchronize()
-        for row, n, w in zip(kept.tolist(), (a, b), weights.cpu().numpy()):
-            stay = prompt_ref.evicted(w, n, 50, 3, 7)
-            assert row == stay + [-1] * (50 - len(stay))
-        assert kept_lens.tolist() == [min(a, 50), min(b, 50)]

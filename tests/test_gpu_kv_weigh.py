@@ -153,25 +153,3 @@ def test_the_same_bits_again(workspace):
         dl.dl_kv_weigh(r, torch.cuda.current_stream())
         said.append(weights)
     assert all(torch.equal(said[0], w) for w in said)
-
-
-def test_captured_and_replayed_as_lengths_grow(workspace):
-    for sizes, group in (([(4, 300), (2, 90)], 2), ([(40, 300), (20, 90)], 4)):  # both kernels
-        p = Packed(sizes, heads=2, group=group)
-        starts, pages, lens = p.plan()
-        lse = p.put(p.exact_lse()).float()
-        weights = torch.zeros((2, p.table.shape[1] * 16), device="cuda")
-        r = dl.KvWeigh(p.cache(), p.q, lse, starts, pages, lens, weights, scale=p.scale)
-        r.use_workspace(workspace)
-        graph = torch.cuda.CUDAGraph()
-        with torch.cuda.graph(graph):
-            dl.dl_kv_weigh(r, torch.cuda.current_stream())
-        for a, b in ((40, 20), (300, 0), (100, 90), (300, 90)):
-            lens.copy_(torch.tensor([a, b], dtype=torch.int32))
-            weights.fill_(7)
-            graph.replay()
-            torch.cuda.synchronize()
-            got = weights.clone()
-            dl.dl_kv_weigh(r, torch.cuda.current_stream())
-            torch.cuda.synchronize()
-            assert torch.equal(got, weights)

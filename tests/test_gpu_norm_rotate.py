@@ -143,27 +143,6 @@ def test_past_the_caches():
             assert torch.equal(again[0], outs[0][part]) and torch.equal(again[1], outs[1][part])
 
 
-def test_captured_and_replayed():
-    """Positions are read when the kernel runs; on a stream of its own."""
-    rng = np.random.default_rng(5)
-    q = torch.randn((7, 3, 64), device="cuda").half()
-    out, positions = torch.full_like(q, 7.0), torch.zeros(7, dtype=torch.int64, device="cuda")
-    r = dl.NormRotate(q, None, out, q_weight=torch.ones(64, device="cuda"), table=table_of(30, 64, rng), positions=positions)
-    graph = torch.cuda.CUDAGraph()
-    stream = torch.cuda.Stream()
-    with torch.cuda.graph(graph, stream=stream):
-        dl.dl_norm_rotate(r, stream)
-    for n in range(4):
-        positions.copy_(torch.randint(0, 30, (7,)))
-        out.fill_(7)
-        graph.replay()
-        torch.cuda.synchronize()
-        got = out.clone()
-        dl.dl_norm_rotate(r, torch.cuda.current_stream())
-        torch.cuda.synchronize()
-        assert torch.equal(got, out) and not (got == 7).all()
-
-
 def test_a_row_of_zeros_and_one_that_is_not_finite():
     q = torch.randn((4, 1, 64), device="cuda")
     q[0] = 0

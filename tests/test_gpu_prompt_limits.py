@@ -109,23 +109,3 @@ def test_many_heads(library):
     r.use_workspace(torch.zeros(dl.dl_chunk_attention_workspace(r), dtype=torch.uint8, device="cuda"))
     dl.dl_chunk_attention(r, torch.cuda.current_stream())
     p.check_attention(out, lse)
-
-
-@pytest.mark.gpu
-def test_calls_on_two_streams_at_once(library):
-    """Each with a workspace of its own."""
-    ps = [Packed([(40, 900), (9, 30)], heads=2, group=2, seed=s) for s in range(2)]
-    streams = [torch.cuda.Stream() for _ in ps]
-    asked = []
-    for p in ps:
-        p.out, p.lse = torch.empty_like(p.q), torch.empty(p.q.shape[:2], device="cuda")
-        r = dl.ChunkAttention(p.cache(), p.q, p.out, *p.plan(), lse=p.lse, scale=p.scale)
-        r.use_workspace(torch.zeros(dl.dl_chunk_attention_workspace(r), dtype=torch.uint8, device="cuda"))
-        asked.append(r)
-    torch.cuda.synchronize()
-    for _ in range(20):
-        for r, s in zip(asked, streams):
-            dl.dl_chunk_attention(r, s)
-    torch.cuda.synchronize()
-    for p in ps:
-        p.check_attention(p.out, p.lse)
