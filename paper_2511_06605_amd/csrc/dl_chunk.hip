@@ -389,8 +389,9 @@ __global__ void __launch_bounds__(CH_THREADS, DP <= 128 ? 2 : 1) dl_chunk_kernel
 #pragma unroll
     for (int s = 0; s < DP / 16; ++s) qf[s] = 16u * s < D ? dl_load_at<dl_u32x4>(q + 2u * (16u * s + 8u * half)) : dl_u32x4{0, 0, 0, 0};
 
-    auto hand_on = [&](uint32_t base, uint32_t to) { feed.hand_on(a, base, lds.rows_at[to], lds.alive_at[to]); };
-    auto put = [&](uint32_t to) {
+    // (inlined whatever they cost: a call wants `feed` in memory, codes and all)
+    auto hand_on = [&](uint32_t base, uint32_t to) __attribute__((always_inline)) { feed.hand_on(a, base, lds.rows_at[to], lds.alive_at[to]); };
+    auto put = [&](uint32_t to) __attribute__((always_inline)) {
         feed.clear(lds.alive_at[to]);
         feed.put_codes(tiles[to]);
         feed.put_scales(a, tiles[to]);
