@@ -11,9 +11,9 @@
 // a compute unit; 256 from 1024 rows a sequence on and up to head_dim 128 (dl_chunk_wide_kernel).  Where there are few tiles their keys are
 // cut into pieces, which a second launch joins (chunk_unit).
 //
-// Measured (8 heads of 128, 32 query heads, bfloat16 on fp8, unless said otherwise): 2048 queries behind 30 720 tokens 1100 - 1128 us, 1065 GFLOP,
-// 0.94 - 0.97 PFLOP/s where a large matrix product reaches 1.34 (128 rows a tile: 1319); a prompt of 8192 617 - 627 us, 0.88 - 0.89; three
-// documents with up to 512 queries on up to 16 400 (4 heads, 28 query heads, float16 on int8) 217 - 234 us, 0.6, 18 of it the join; 16 queries
+// Measured (8 heads of 128, 32 query heads, bfloat16 on fp8, unless said otherwise): 2048 queries behind 30 720 tokens 1100 - 1160 us, 1065 GFLOP,
+// 0.92 - 0.97 PFLOP/s where a large matrix product reaches 1.34 (128 rows a tile: 1319); a prompt of 8192 617 - 638 us, 0.86 - 0.89; three
+// documents with up to 512 queries on up to 16 400 (4 heads, 28 query heads, float16 on int8) 216 - 235 us, 0.6, 18 of it the join; 16 queries
 // behind 500 13.3 us, 5 sequences of up to 101 behind up to 777 (12 heads of 64) 18 us, both two launches.  A workgroup of the former is at work
 // for 6 us: 1.4 until it knows its piece, 0.6 until it knows its pages, 1.1 for the codes, 1.7 for the step, 0.9 for what it leaves; one of the join 2.5.
 #include "dl_codes.h"
