@@ -8,7 +8,7 @@
 // elements of Q once, on their way into LDS, keys as rows and values transposed (by byte permutes while they are bytes), so that every
 // operand of the 32 x 32 x 16 products is one 16-byte read.  While a step is worked on, the next one's codes are on their way to registers
 // and the pages of the one after it are looked up.  Masks cost something only where a wavefront's rows end.  128 rows a tile, two workgroups
-// a compute unit; 256 from 1024 rows a sequence on and up to head_dim 128 (dl_chunk_wide_kernel).  Where there are few tiles their keys are
+// a compute unit; 256 for many rows and up to head_dim 128 (dl_chunk_wide_kernel).  Where there are few tiles their keys are
 // cut into pieces, which a second launch joins (chunk_unit).
 //
 // Measured (8 heads of 128, 32 query heads, bfloat16 on fp8, unless said otherwise): 2048 queries behind 30 720 tokens 1100 - 1160 us, 1065 GFLOP,
@@ -791,13 +791,14 @@ int chunk_sizes(const dl_kv_cache *cache, const dl_chunk_attention_args *args, d
     if (!args->tokens || !args->q_heads || !args->batch) return DL_OK;
     const uint64_t rows = (uint64_t)args->tokens * (uint32_t)(args->q_heads / cache->heads);
     // every sequence begins a tile of its own
-    // 256 rows a tile from 1024 rows a sequence on.  256 : 128, us, 8 heads of 128, 32 query heads: on 30 720 tokens 256 queries (1024 rows) 167 : 190, 512
-    // 305 : 351; 8 sequences on 4000 with up to 128, 192, 256, 384 queries 89 : 86, 100 : 108, 140 : 147, 173 : 191; 8 prompts of up to 256 and 512 with nothing
-    // before them 30 : 26 and 49 : 42.  So where contexts are short 128 would be better for longer, which the host does not know.
-    sh->tile_rows = cache->head_dim <= 128 && rows >= 1024u * (uint64_t)args->batch ? 64u * CH_WAVES : 32u * CH_WAVES;
+    // 256 rows a tile from 1024 rows a sequence on, where the table holds 2048 tokens and more.  256 : 128, us, 8 heads of 128, 32 query heads: on 30 720
+    // tokens 256 queries (1024 rows) 167 : 190, 512 305 : 351; 8 sequences on 4000 with up to 128, 192, 256, 384 queries 89 : 86, 100 : 108, 140 : 147, 173 :
+    // 191.  Prompts with nothing before them, 300, 750, 1024, 1500, 2048, 4096 tokens: 26 : 23, 42 : 39, 49 : 51, 76 : 73, 90 : 94, 184 : 207; four of up to that:
+    // 34 : 31, 69 : 46, 57 : 58, 92 : 87, 132 : 134; 750 queries on 1500 tokens 72 : 74.
+    const uint64_t most = (uint64_t)args->max_pages * (uint32_t)cache->page_tokens;
+    sh->tile_rows = cache->head_dim <= 128 && rows >= 1024u * (uint64_t)args->batch && most >= 2048u ? 64u * CH_WAVES : 32u * CH_WAVES;
     uint64_t tiles = rows / sh->tile_rows + (uint64_t)args->batch;
     if (tiles > rows) tiles = rows;
-    const uint64_t most = (uint64_t)args->max_pages * (uint32_t)cache->page_tokens;
     // Workgroups at once, by the registers and LDS: two a compute unit up to head_dim 128 (64 where there are many rows), one above.
     sh->slots = cache->head_dim > 128 || (cache->head_dim > 64 && sh->tile_rows > 32u * CH_WAVES) ? 256u : 512u;
     // Two rounds of pieces at most, and no more than a step each.

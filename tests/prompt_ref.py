@@ -44,11 +44,11 @@ class Packed:
     """A cache whose unused places hold NaN (as far as its codes have one) and scales of NaN, and packed sequences (new, all tokens) on it."""
 
     def __init__(self, sizes, heads=2, group=1, dim=64, page=16, dtype=torch.bfloat16, kind="fp8", seed=0, spread=1.0, q_size=1.0, spare=0, gaps=0,
-                 order=(0, 1, 2), more_pages=0):
+                 order=(0, 1, 2), more_pages=0, room=0):
         rng = self.rng = np.random.default_rng(seed)
         self.sizes, self.heads, self.group, self.dim, self.page, self.dtype, self.kind = list(sizes), heads, group, dim, page, dtype, kind
         B = len(self.sizes)
-        wide = max(1, max([-(-n // page) for _, n in self.sizes], default=1) + spare)
+        wide = max(1, max([-(-n // page) for _, n in self.sizes], default=1) + spare, -(-room // page))  # (room: tokens that a row of the table has room for)
         need = [-(-n // page) for _, n in self.sizes]
         pages = sum(need) + 2 + more_pages
         ids = rng.permutation(pages)

@@ -83,32 +83,33 @@ def test_batches_of_more_than_64_that_are_cut(workspace):
 @pytest.mark.parametrize("dim,heads,group,sizes", [
     (64, 1, 16, [(64, 64)]), (128, 1, 16, [(70, 200)]), (80, 2, 20, [(52, 700)]), (16, 1, 64, [(17, 20), (20, 1)]), (128, 1, 32, [(33, 33), (40, 1500), (30, 64)]),
     (96, 1, 100, [(11, 129)]), (48, 1, 128, [(8, 65), (9, 128), (0, 40), (15, 13)])])
-def test_many_rows(workspace, dtype, kind, dim, heads, group, sizes):
-    """Enough rows a sequence for the kernel with 256 rows a tile."""
+@pytest.mark.parametrize("room", [0, 2048])
+def test_many_rows(workspace, dtype, kind, dim, heads, group, sizes, room):
+    """Enough rows a sequence for the kernel with 256 rows a tile, which tables of 2048 tokens and more have."""
     assert sum(m for m, _ in sizes) * group >= 1024 * len(sizes) or len(sizes) > 3
-    check(Packed(sizes, heads=heads, group=group, dim=dim, dtype=dtype, kind=kind, seed=dim, gaps=1), workspace)
+    check(Packed(sizes, heads=heads, group=group, dim=dim, dtype=dtype, kind=kind, seed=dim, gaps=1, room=room), workspace)
 
 
 @pytest.mark.parametrize("page", [1, 5, 24, 128])
 def test_many_rows_and_pages_that_end_anywhere(workspace, page):
-    check(Packed([(35, 300), (33, 40)], page=page, group=32, heads=1, dim=32, seed=page, spare=2), workspace)
+    check(Packed([(35, 300), (33, 40)], page=page, group=32, heads=1, dim=32, seed=page, room=2100), workspace)
 
 
 def test_many_rows_and_what_is_none(workspace):
-    p = Packed([(40, 300)], heads=1, group=32, dim=32)
+    p = Packed([(40, 300)], heads=1, group=32, dim=32, room=2048)
     p.table[0, 1], p.table[0, 7], p.table[0, 18] = -1, 1 << 30, -1
     check(p, workspace, dead=[(0, 1), (0, 7), (0, 18)])
     for side in ("k_scale", "v_scale"):
-        p = Packed([(40, 300)], heads=1, group=32, dim=32)
+        p = Packed([(40, 300)], heads=1, group=32, dim=32, room=2048)
         getattr(p, side)[int(p.table[0, 280 // 16]), 280 % 16, 0] = float("nan")
         out, _ = check(p, workspace)
         assert torch.isnan(out).any() and torch.isfinite(out[:19]).all()
     for dtype, kind in TYPES:
-        p = Packed([(33, 200)], heads=1, group=32, dim=32, dtype=dtype, kind=kind)
+        p = Packed([(33, 200)], heads=1, group=32, dim=32, dtype=dtype, kind=kind, room=2048)
         for n, t in enumerate((3, 60, 140, 199)):
             p.v_scale[int(p.table[0, t // 16]), t % 16, 0] *= (2.0 ** -90, 2.0 ** -60, 2.0 ** -45, 0.0)[n]
         check(p, workspace)
-    check(Packed([(40, 500)], heads=1, group=32, dim=32, q_size=12.0, spread=1.5), workspace)
+    check(Packed([(40, 500)], heads=1, group=32, dim=32, q_size=12.0, spread=1.5, room=2048), workspace)
 
 
 @pytest.mark.parametrize("order", [(0, 1, 2), (0, 2, 1), (2, 0, 1), (1, 0, 2)])
