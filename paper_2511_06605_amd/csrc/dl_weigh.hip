@@ -49,10 +49,15 @@ __device__ __forceinline__ float over_lanes(float (&x)[16], uint32_t i)
     return x[0] + __shfl_xor(x[0], 16);
 }
 
-// A tile's scores s: rows are keys (8 (e / 4) + 4 half + e % 4, with the scales ks), columns queries.  lse in units of ln 2; masked: keys from
-// `seen` + 1 on are not seen by the lane's query.
+// A tile's scores s: rows are keys (8 (e / 4) + 4 half + e % 4, with the scales ks), columns queries.  lse in units of ln 2, infinite for a query
+// that gives nothing: its scores, which may be no numbers either, count as 0.  masked: keys from `seen` + 1 on are not seen by the lane's query.
 __device__ __forceinline__ void add_weights(dl_f32x16 &s, const dl_f32x4 (&ks)[4], float lse, bool masked, int32_t seen, uint32_t half, float (&sum)[16])
 {
+    const bool nothing = lse == INFINITY;
+    if (__any(nothing)) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = nothing ? 0.0f : s[e];
+    }
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] = fmaf(s[e], ks[e / 4][e % 4], -lse);
     if (masked) {
