@@ -19,6 +19,7 @@
 #include "dl_codes.h"
 #include "dl_internal.h"
 #include "dl_packed.h"
+#include "dl_pieces.h"
 
 namespace {
 
@@ -51,7 +52,8 @@ struct chunk_args {
 // no more than half as many tiles.
 // Which size: a round of workgroups takes as long as the steps of one and START more, a piece costs the join JOIN steps; a lane of a
 // wavefront looks at the size that cuts the longest sequence into its number + 1 pieces.  Batches of more than SEARCH_MAX sequences, and tables
-// with room for more than 2^20 steps, are not looked at one by one: with T steps of all tiles, T / (most_cut / 2), so that those that are cut have at most twice as many pieces.
+// with room for more than 2^20 steps, are not looked at one by one: with T steps of all tiles, T / (most_cut / 2), so that those that are cut
+// have at most twice as many pieces (dl_piece_steps).
 // Every wavefront works this out from the lengths for itself.
 constexpr float START = 3.0f, JOIN = 0.1f;
 constexpr uint32_t SEARCH_MAX = 16;
@@ -67,7 +69,7 @@ template <bool CUT>
 __device__ __forceinline__ bool chunk_unit(const chunk_args &a, uint32_t unit, chunk_place *at)
 {
     const uint32_t lane = threadIdx.x % 64u;
-    uint32_t size = 1u << 26, tiles = 0, steps = 0;
+    uint32_t size = DL_UNCUT, tiles = 0, steps = 0;
     const bool at_once = a.p.batch <= 64u;
     uint32_t first = 0, queries = 0, len = 0;
     auto look = [&](uint32_t b0) {
@@ -107,7 +109,7 @@ __device__ __forceinline__ bool chunk_unit(const chunk_args &a, uint32_t unit, c
             for (int d = 1; d < 64; d *= 2) x += (uint64_t)__shfl_xor((unsigned long long)x, d);
             all += x;
         }
-        size = max((uint32_t)((all + a.most_cut / 2u - 1u) / (a.most_cut / 2u)), 1u);
+        size = dl_piece_steps(all, a.most_cut);
     }
     uint32_t before = 0, slots = 0;
     for (uint32_t b0 = 0; b0 < a.p.batch; b0 += 64u) {
