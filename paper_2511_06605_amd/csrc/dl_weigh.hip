@@ -49,15 +49,20 @@ __device__ __forceinline__ float over_lanes(float (&x)[16], uint32_t i)
     return x[0] + __shfl_xor(x[0], 16);
 }
 
-// A tile's scores s: rows are keys (8 (e / 4) + 4 half + e % 4, with the scales ks), columns queries.  lse in units of ln 2, infinite for a query
-// that gives nothing: its scores, which may be no numbers either, count as 0.  masked: keys from `seen` + 1 on are not seen by the lane's query.
-__device__ __forceinline__ void add_weights(dl_f32x16 &s, const dl_f32x4 (&ks)[4], float lse, bool masked, int32_t seen, uint32_t half, float (&sum)[16])
+// A query's lse in units of ln 2: infinite where it is no finite number.
+__device__ __forceinline__ float lse_of(float given) { return fabsf(given) < INFINITY ? given * DL_LOG2E : INFINITY; }
+
+// A tile's scores s: rows are keys (8 (e / 4) + 4 half + e % 4, with the scales ks), columns queries.  lse: by lse_of; the scores of a query
+// that gives nothing may be no numbers either, and count as 0.  Lanes that have no row have the last one's scores and lse.  masked: keys from
+// `seen` + 1 on are not seen by the lane's query.
+__device__ __forceinline__ void add_weights(dl_f32x16 &s, const dl_f32x4 (&ks)[4], float lse, bool row, bool masked, int32_t seen, uint32_t half, float (&sum)[16])
 {
     const bool nothing = lse == INFINITY;
     if (__any(nothing)) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[e] = nothing ? 0.0f : s[e];
     }
+    if (!row) lse = INFINITY;
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] = fmaf(s[e], ks[e / 4][e % 4], -lse);
     if (masked) {
@@ -139,8 +144,7 @@ __global__ void __launch_bounds__(64 * FEW_WAVES, DP <= 128 ? 4 : 2) dl_weigh_fe
             __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
             for (uint32_t r0 = row0; r0 < rows; r0 += 32u) {
-                // (a row that is none, or whose lse is no number: nothing is left of it)
-                const float lse = r0 + i < rows && fabsf(given) < INFINITY ? given * DL_LOG2E : INFINITY;
+                const float lse = lse_of(given);
                 const int32_t seen = last;
                 // (elements and scales are made and read anew for each tile: kept, they would cost half the wavefronts)
 #pragma unroll
@@ -161,7 +165,7 @@ __global__ void __launch_bounds__(64 * FEW_WAVES, DP <= 128 ? 4 : 2) dl_weigh_fe
                 dl_f32x4 ks[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) ks[e] = *(const dl_f32x4 *)&sums[wave][8u * e + 4u * half];
-                add_weights(s, ks, lse, r0 < whole, seen, half, sum);
+                add_weights(s, ks, lse, r0 + i < rows, r0 < whole, seen, half, sum);
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
@@ -223,7 +227,7 @@ __global__ void __launch_bounds__(MANY_THREADS, DP <= 128 ? 4 : 2) dl_weigh_many
             }
             if (threadIdx.x < 32u) {
                 const uint32_t row = min(r0 + i, rows - 1u), j = dl_divide(row, a.groups);
-                staged_lse = r0 + i < rows ? a.lse[(uint64_t)(first + j) * a.q_heads + head * a.group + row - j * a.group] : INFINITY;
+                staged_lse = a.lse[(uint64_t)(first + j) * a.q_heads + head * a.group + row - j * a.group];
             }
         };
         auto put = [&](uint32_t to) {
@@ -232,7 +236,7 @@ __global__ void __launch_bounds__(MANY_THREADS, DP <= 128 ? 4 : 2) dl_weigh_many
                 const uint32_t n = threadIdx.x + x * MANY_THREADS, row = n / PIECES, piece = n % PIECES;
                 if (32u * PIECES % MANY_THREADS == 0 || n < 32u * PIECES) *(dl_u32x4 *)&tiles[to][row * ROW + piece * 4u] = staged[x];
             }
-            if (threadIdx.x < 32u) lses[to][i] = fabsf(staged_lse) < INFINITY ? staged_lse * DL_LOG2E : INFINITY;
+            if (threadIdx.x < 32u) lses[to][i] = lse_of(staged_lse);
         };
         dl_u32x4 kf[2 * PAIRS];
         stage(head0, row0);
@@ -277,7 +281,7 @@ __global__ void __launch_bounds__(MANY_THREADS, DP <= 128 ? 4 : 2) dl_weigh_many
                     }
                     const bool masked = r0 < whole;
                     const int32_t seen = masked ? ahead + (int32_t)dl_divide(r0 + i, a.groups) - (int32_t)base : 0;
-                    add_weights(s, ks, lse, masked, seen, half, sum);
+                    add_weights(s, ks, lse, r0 + i < rows, masked, seen, half, sum);
                 }
                 if (more) put(now ^ 1u);
                 __syncthreads();
