@@ -371,10 +371,10 @@ __global__ void __launch_bounds__(CH_THREADS, DP <= 128 ? 2 : 1) dl_chunk_kernel
     __shared__ chunk_lds<DP> lds;
     auto &tiles = lds.tiles;
     const uint32_t lane = threadIdx.x % 64u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
-    const uint32_t i = lane % 32u, half = lane / 32u, D = a.c.head_dim, head = blockIdx.x % a.c.heads;
+    const uint32_t i = lane % 32u, half = lane / 32u, D = a.c.head_dim, head = blockIdx.x, unit = blockIdx.z * gridDim.y + blockIdx.y;
     chunk_place at;
-    if (!chunk_unit<false>(a, blockIdx.x / a.c.heads, &at)) return;
-    if (a.most_cut && blockIdx.x == 0 && threadIdx.x == 0) *a.size = at.size;
+    if (!chunk_unit<false>(a, unit, &at)) return;
+    if (a.most_cut && unit == 0 && head == 0 && threadIdx.x == 0) *a.size = at.size;
     const chunk_rows t(a, at);
     const uint32_t first = at.piece * at.keys, end = min(first + at.keys, t.end);
     if (at.piece && first >= end) return;
@@ -511,10 +511,10 @@ __global__ void __launch_bounds__(CH_THREADS, DP <= 64 ? 2 : 1) dl_chunk_wide_ke
     using feed_t = chunk_feed<Q, C, DP>;
     __shared__ wide_lds<DP> lds;
     const uint32_t lane = threadIdx.x % 64u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
-    const uint32_t i = lane % 32u, half = lane / 32u, D = a.c.head_dim, head = blockIdx.x % a.c.heads;
+    const uint32_t i = lane % 32u, half = lane / 32u, D = a.c.head_dim, head = blockIdx.x, unit = blockIdx.z * gridDim.y + blockIdx.y;
     chunk_place at;
-    if (!chunk_unit<false>(a, blockIdx.x / a.c.heads, &at)) return;
-    if (a.most_cut && blockIdx.x == 0 && threadIdx.x == 0) *a.size = at.size;
+    if (!chunk_unit<false>(a, unit, &at)) return;
+    if (a.most_cut && unit == 0 && head == 0 && threadIdx.x == 0) *a.size = at.size;
     const chunk_rows t(a, at);
     const uint32_t first = at.piece * at.keys, end = min(first + at.keys, t.end);
     if (at.piece && first >= end) return;
@@ -858,8 +858,9 @@ extern "C" int dl_chunk_attention(const dl_kv_cache *cache, const dl_chunk_atten
     a.search = sh.search;
     a.round = (float)sh.slots / (float)a.c.heads;
     a.scale = args->scale * DL_LOG2E;
-    const uint64_t grid = sh.units * a.c.heads;
-    if (grid >= (1ull << 32) / CH_THREADS) return DL_ERR_INVALID;
+    // (pieces may be more than a grid is high)
+    const uint32_t deep = (uint32_t)((sh.units + 65534u) / 65535u);
+    const dim3 grid(a.c.heads, (uint32_t)((sh.units + deep - 1u) / deep), deep);
     hipStream_t hs = (hipStream_t)stream;
     dl_with_16bit(args->type, [&](auto q) {
         auto go = [&](auto dp) {
@@ -867,10 +868,10 @@ extern "C" int dl_chunk_attention(const dl_kv_cache *cache, const dl_chunk_atten
             dl_with_format(cache->format, [&](auto c) {
                 if constexpr (DP <= 128)
                     if (sh.tile_rows > 32u * CH_WAVES) {
-                        hipLaunchKernelGGL((dl_chunk_wide_kernel<decltype(q), decltype(c), DP>), dim3((uint32_t)grid), dim3(CH_THREADS), 0, hs, a);
+                        hipLaunchKernelGGL((dl_chunk_wide_kernel<decltype(q), decltype(c), DP>), grid, dim3(CH_THREADS), 0, hs, a);
                         return;
                     }
-                hipLaunchKernelGGL((dl_chunk_kernel<decltype(q), decltype(c), DP>), dim3((uint32_t)grid), dim3(CH_THREADS), 0, hs, a);
+                hipLaunchKernelGGL((dl_chunk_kernel<decltype(q), decltype(c), DP>), grid, dim3(CH_THREADS), 0, hs, a);
             });
             if (sh.most_cut)
                 hipLaunchKernelGGL((dl_chunk_join_kernel<decltype(q), DP>), dim3((sh.most_cut + 1u) / 2u * a.c.heads * (sh.tile_rows / JOIN_ROWS<DP>)), dim3(CH_THREADS), 0, hs, a);
