@@ -41,7 +41,7 @@ __device__ __forceinline__ To dl_bits(From f)
     return __builtin_bit_cast(To, f);
 }
 
-// Division of whole numbers n < 2^31 by d in 1 .. 65536: n * m >> sh with sh = 31 + l, 2^l the power of two at or above d, and
+// Division of whole numbers n < 2^31 by d in 1 .. 2^17: n * m >> sh with sh = 31 + l, 2^l the power of two at or above d, and
 // m = 2^sh / d rounded up (< 2^32).  Exact: m d = 2^sh + e with e < d, so n m / 2^sh is n / d and less than n d / (d 2^sh) <= 1 / d more.
 struct dl_divider {
     uint32_t d, m, sh;
@@ -49,7 +49,7 @@ struct dl_divider {
 static inline dl_divider dl_make_divider(uint32_t d)
 {
     uint32_t l = 0;
-    while ((1u << l) < d) ++l;  // d <= 65536
+    while ((1u << l) < d) ++l;  // d <= 2^17
     const uint64_t two = 1ull << (31 + l);
     return {d, (uint32_t)((two + d - 1) / d), 31 + l};
 }

@@ -147,7 +147,7 @@ int norm_setup(const dl_norm_rotate_args *args, norm_args *a, bool *nothing)
     if (args->q_heads < 0 || args->k_heads < 0 || args->q_heads > 65535 || args->k_heads > 65535) return DL_ERR_INVALID;
     if (args->table_rows < 0 || args->table_rows > INT32_MAX) return DL_ERR_INVALID;
     const int64_t q_heads = args->q ? args->q_heads : 0, heads = q_heads + (args->k ? args->k_heads : 0);
-    if (heads > 65536 || args->tokens < 0 || args->tokens > DL_MAX_ROWS || args->tokens * heads > DL_MAX_ROWS) return DL_ERR_INVALID;
+    if (args->tokens < 0 || args->tokens > DL_MAX_ROWS || args->tokens * heads > DL_MAX_ROWS) return DL_ERR_INVALID;
     *nothing = args->tokens * heads == 0;
     if (*nothing) return DL_OK;
     if ((args->q && !args->q_out) || (args->k && !args->k_out)) return DL_ERR_INVALID;
