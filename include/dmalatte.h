@@ -784,15 +784,17 @@ int dl_kv_weigh(const dl_kv_cache *cache, const dl_kv_weigh_args *args, void *st
  * kept_lens[b] = m, kept_weights[b][j] = weights[b][kept[b][j]]; entries from m to keep - 1 become -1 and 0.
  * The pages that are written differ from each other and from all that are read.  A token whose page is none of the pool, in either
  * table, is not copied.  lens[b] counts as at least 0 and at most max_pages * page_tokens.
+ * kept, kept_lens and kept_weights overlap neither each other nor anything that is read.  Refused are calls where lens, kept and kept_lens do, and
+ * those where kept_weights is weights; other overlaps are not looked for.
  */
 typedef struct dl_kv_evict_args {
     const float *weights;         /* [batch][max_pages * page_tokens], weights_stride apart */
     const int32_t *pages;         /* [batch][max_pages], pages_stride apart */
-    const int32_t *lens;          /* [batch]; not kept_lens */
+    const int32_t *lens;          /* [batch] */
     const int32_t *to_pages;      /* [batch][keep / page_tokens, rounded up], to_pages_stride apart */
     int32_t *kept;                /* [batch][keep], contiguous */
     int32_t *kept_lens;           /* [batch] */
-    float *kept_weights;          /* [batch][keep], kept_weights_stride apart; or null; overlaps nothing that is read */
+    float *kept_weights;          /* [batch][keep], kept_weights_stride apart; or null */
     void *workspace;              /* dl_kv_evict_workspace() bytes, 16-byte aligned; see dl_prefix_attention_workspace */
     size_t workspace_bytes;
     int64_t max_pages;            /* max_pages * page_tokens <= 2^30 */

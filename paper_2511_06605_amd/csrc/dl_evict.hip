@@ -264,6 +264,11 @@ int evict_setup(const dl_kv_cache *cache, const dl_kv_evict_args *args, int side
     return DL_OK;
 }
 
+bool overlap(const int32_t *a, int64_t a_many, const int32_t *b, int64_t b_many)
+{
+    return (uint64_t)a < (uint64_t)b + 4u * (uint64_t)b_many && (uint64_t)b < (uint64_t)a + 4u * (uint64_t)a_many;
+}
+
 }  // namespace
 
 extern "C" int64_t dl_kv_evict_workspace(const dl_kv_cache *cache, const dl_kv_evict_args *args)
@@ -288,8 +293,11 @@ extern "C" int dl_kv_evict(const dl_kv_cache *cache, const dl_kv_evict_args *arg
          (uint64_t)args->kept_lens | (uint64_t)args->kept_weights) % 4u)
         return DL_ERR_INVALID;
     if (!args->workspace || (uint64_t)args->workspace % 16u || args->workspace_bytes < DL_CONTROL_BYTES) return DL_ERR_INVALID;
-    // (lengths and weights are read while what stays is written)
-    if (args->lens == args->kept_lens || (args->kept_weights && args->kept_weights == args->weights)) return DL_ERR_INVALID;
+    // (lengths and weights are read while what stays is written; lists without gaps are looked at as a whole)
+    const int64_t lists = args->batch, tokens = lists * args->keep;
+    if (overlap(args->lens, lists, args->kept_lens, lists) || overlap(args->lens, lists, args->kept, tokens) || overlap(args->kept_lens, lists, args->kept, tokens) ||
+        (args->kept_weights && args->kept_weights == args->weights))
+        return DL_ERR_INVALID;
     a.weights = args->weights;
     a.pages = args->pages;
     a.lens = args->lens;
