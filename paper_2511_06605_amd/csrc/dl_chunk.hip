@@ -494,9 +494,9 @@ __global__ void __launch_bounds__(CH_THREADS, DP <= 128 ? 2 : 1) dl_chunk_kernel
 // 32 keys are under way, and while those weights meet the values, the next scores are scaled and the next step's codes go to LDS.  Three
 // tiles in LDS: one that is worked on, the next one, and the one that is filled while somebody may still be at the first; a barrier a step.
 //
-// What bounds it is the issue of instructions: a lone wavefront issues one in about 7 cycles (two of them one in 3.5), and a step of 64 keys is
-// about 630 of them (450 vector ones, 64 products, 75 for LDS), 4400 of the 5060 cycles that it takes (counted over 2048 queries on 30 720 tokens),
-// 2050 of which the matrix units work.  So what counts is their number: operands in padded rows, whose addresses differ by constants, instead of
+// What bounds it is a lone wavefront's way through a step of 64 keys: about 630 instructions (450 vector ones, 64 products, 75 for LDS) in 5060
+// cycles, 60 % of which it issues, 28 % it waits for counters or at the barrier and 12 % for its turn (counted over 2048 queries on 30 720 tokens); the matrix
+// units work for 2050.  So the number of instructions counts: operands in padded rows, whose addresses differ by constants, instead of
 // places exchanged by an exclusive or 1230 -> 1127 us.  The same code with 32 rows a wavefront and eight of them, two a SIMD: 1317 (twice the reads
 // from LDS); operands a step further ahead and all scales a part ahead: 1160.
 template <int DP>
@@ -796,7 +796,8 @@ int chunk_sizes(const dl_kv_cache *cache, const dl_chunk_attention_args *args, d
     // 256 rows a tile from 1024 rows a sequence on, where the table holds 2048 tokens and more.  256 : 128, us, 8 heads of 128, 32 query heads: on 30 720
     // tokens 256 queries (1024 rows) 167 : 190, 512 305 : 351; 8 sequences on 4000 with up to 128, 192, 256, 384 queries 89 : 86, 100 : 108, 140 : 147, 173 :
     // 191.  Prompts with nothing before them, 300, 750, 1024, 1500, 2048, 4096 tokens: 26 : 23, 42 : 39, 49 : 51, 76 : 73, 90 : 94, 184 : 207; four of up to that:
-    // 34 : 31, 69 : 46, 57 : 58, 92 : 87, 132 : 134; 750 queries on 1500 tokens 72 : 74.
+    // 34 : 31, 69 : 46, 57 : 58, 92 : 87, 132 : 134; 750 queries on 1500 tokens 72 : 74.  (The table stands in for the contexts, which the host does not know: in
+    // wide tables such prompts have the former.)
     const uint64_t most = (uint64_t)args->max_pages * (uint32_t)cache->page_tokens;
     sh->tile_rows = cache->head_dim <= 128 && rows >= 1024u * (uint64_t)args->batch && most >= 2048u ? 64u * CH_WAVES : 32u * CH_WAVES;
     uint64_t tiles = rows / sh->tile_rows + (uint64_t)args->batch;

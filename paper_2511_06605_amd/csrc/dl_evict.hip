@@ -9,6 +9,8 @@
 // Measured: 4 sequences of up to 32 768 tokens cut to 8192 (8 heads of 128, 139 MB) 48 - 49 us, 17 to 23 of them the choice by 4 workgroups, 24 to 35 the
 // move, 4.7 TB/s on average; 3 of up to 2001 cut to 500 10.6 us, two launches.  Of a choice among 25 000 (13.4 us) the first look with its count takes 5,
 // each of two more digits 2.2, counting and placing 3.4.
+// Above 32 768 tokens the numbers do not fit LDS, and that one workgroup reads the weights once a digit and twice more: 4 of up to 32 769 cut to 8192 61 us, of
+// 131 072 124 (to 32 768, 557 MB: 217).
 #include "dl_codes.h"
 #include "dl_internal.h"
 

@@ -7,14 +7,14 @@
 //
 // Measured: one query of 32 heads on 5000 tokens (8 heads of 128, 5.3 MB) 5.4 - 5.7 us, a launch and the way from length to table to codes; the last 32
 // queries of 8 prompts of up to 16 400 (4 heads, 28 query heads, 48 MB, 11.5 GFLOP) 34 - 38 us in two launches (33 and 5), 2048 queries behind 2048
-// tokens (8 heads, 32 query heads) 180 us.  What bounds the second is vector instructions, 135 a tile of 32 x 32 besides its 8 products, and waiting: for
-// half of their time wavefronts wait for memory, LDS or each other, as few tiles a workgroup do not cover the way to the first.
+// tokens (8 heads, 32 query heads) 188 us.  What bounds the second is vector instructions, 139 a tile of 32 x 32 besides its 8 products, and waiting: for
+// half of their time wavefronts wait for memory, LDS or each other, as few tiles a workgroup do not cover the way to the first.  Four of the instructions
+// keep what is no number in a query out of the sums (without: 180 us; a first pass without and a second one where a sum is none: 185, and twice the code).
 #include "dl_codes.h"
 #include "dl_internal.h"
 #include "dl_packed.h"
 
 namespace {
-
 
 struct weigh_args {
     dl_cache_view c;
@@ -188,7 +188,7 @@ __global__ void __launch_bounds__(64 * FEW_WAVES, DP <= 128 ? 4 : 2) dl_weigh_fe
 // so that eight neighbouring lanes, a row each, use all banks; while a tile of 32 rows is worked on, the next one is on its way.  What a product needs from LDS is asked for two products before.
 constexpr uint32_t MANY_THREADS = 512, MANY_KEYS = 32 * MANY_THREADS / 64;
 // Heads are shared out up to so many workgroups.  512, 1024, 2048, 4096: 8 prompts (see the top) 38.8, 37.5, 38.8, 38.9 us; 4 of up to 16 400 tokens, 8 heads
-// 28.6, 27.7, 31.4, 31.4; one with 4 heads 16.7 - 16.9, one of 2048 queries 180 with any.
+// 28.6, 27.7, 31.4, 31.4; one with 4 heads 16.7 - 16.9, one of 2048 queries the same with any.
 constexpr uint32_t MANY_BLOCKS = 1024;
 template <class Q, class C, int DP>
 __global__ void __launch_bounds__(MANY_THREADS, DP <= 128 ? 4 : 2) dl_weigh_many_kernel(const weigh_args a)
