@@ -268,7 +268,7 @@ int evict_setup(const dl_kv_cache *cache, const dl_kv_evict_args *args, int side
 
 bool overlap(const int32_t *a, int64_t a_many, const int32_t *b, int64_t b_many)
 {
-    return (uint64_t)a < (uint64_t)b + 4u * (uint64_t)b_many && (uint64_t)b < (uint64_t)a + 4u * (uint64_t)a_many;
+    return a_many && b_many && (uint64_t)a < (uint64_t)b + 4u * (uint64_t)b_many && (uint64_t)b < (uint64_t)a + 4u * (uint64_t)a_many;
 }
 
 }  // namespace

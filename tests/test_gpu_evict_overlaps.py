@@ -49,3 +49,15 @@ def test_next_to_each_other(lens, kept, kept_lens):
     want[kept_lens:kept_lens + BATCH] = torch.tensor([0, 2, 3, 0], dtype=torch.int32)
     dl.dl_kv_evict(evict(room, lens, kept, kept_lens), torch.cuda.current_stream())
     assert torch.equal(room, want)
+
+
+def test_no_tokens_overlap_nothing():
+    """keep == 0: nothing is written to kept, wherever it points."""
+    room = torch.full((60,), 7, dtype=torch.int32, device="cuda")
+    r = evict(room, 20, 0, 40)
+    r.desc.keep = 0
+    for at in (20, 21, 40, 43):
+        r.desc.kept = room.data_ptr() + 4 * at
+        room[40:44] = 7
+        dl.dl_kv_evict(r, torch.cuda.current_stream())
+        assert room.tolist() == [7] * 40 + [0] * 4 + [7] * 16
